@@ -41,7 +41,7 @@ extern "C" {
 #endif
 
 enum { MOE_OK = 0, MOE_ERR_INVALID_ARG = -1, MOE_ERR_UNSUPPORTED = -2, MOE_ERR_WORKSPACE = -3, MOE_ERR_HIP = -4 };
-enum { MOE_F32 = 0, MOE_BF16 = 1 };
+enum { MOE_F32 = 0, MOE_BF16 = 1, MOE_E4M3 = 2 };   /* MOE_E4M3: 8-bit floats with 3 bits after the point, largest value 448; caches only */
 enum { MOE_GATE_TOPK = 0, MOE_GATE_HASH = 1 };
 
 typedef struct moe_cfg {
@@ -313,6 +313,85 @@ int moe_timer_reset(moe_timer* timer);
 int moe_timer_read(moe_timer* timer, float* ms, int32_t capacity_calls, int32_t* n_calls);
 int moe_layer_forward_timed(const moe_cfg* cfg, const void* x, const void* W_g, const float* gate_bias,
                             const void* W_packed, void* y, void* ws, void* stream, moe_timer* timer);
+
+/*
+ * Around the layer: what a decoder layer with this feed-forward layer runs for a token being generated.
+ *
+ * The conventions above hold (caller's buffers and streams, error codes, nothing allocated, kernel launches only, so the calls can
+ * be recorded into a graph), with these differences: the descriptions are the structs below; k, v and q may be rows of a wider
+ * matrix (a stride is given); values that are not finite spoil the outputs they enter into and no others.
+ * Every output is written completely and, for the same inputs, with the same bits in every call.
+ */
+
+/*
+ * Residual addition and root-mean-square norm:  s = x + residual,  n = s / sqrt(mean(s^2) + eps) * weight, in fp32 from the
+ * addition on; n is the norm of the sum itself, not of the sum rounded to dtype.
+ *   x, residual [T, d], weight [d]: device, dtype.  residual may be NULL (s = x).
+ *   sum [T, d]: dtype, s rounded; may be NULL.     y [T, d]: dtype, n rounded; may be NULL if q is not.
+ *   q [T, d]: e4m3 bytes, q_scale [T, d / q_group] (q_group 0: [T, 1]): fp32; both NULL or neither.
+ *     q_scale = max(max |n| over the row's group / 448, 2^-126), q = n / q_scale, so that q * q_scale stands for n.
+ *   x, residual, sum and y may be the same arrays (not: overlap in part).  All 16-byte aligned.
+ */
+typedef struct moe_norm_cfg {
+    int32_t T;        /* rows; 0 <= T < 2^22 */
+    int32_t d;        /* columns; a multiple of 8, at most 32768 */
+    int32_t dtype;    /* MOE_F32 | MOE_BF16 */
+    int32_t q_group;  /* columns that share a scale of q: 0 (all d), 32, 64 or 128 */
+    float eps;        /* > 0 */
+} moe_norm_cfg;
+int moe_add_norm(const moe_norm_cfg* cfg, const void* x, const void* residual, const void* weight, void* sum, void* y, void* q,
+                 float* q_scale, void* stream);
+
+/*
+ * A paged cache of keys and values.  k_pages, v_pages: device, [pages, heads, page_size, head_dim] in cache_dtype; with MOE_E4M3 also
+ * k_scales, v_scales: fp32 [pages, heads, page_size], one per row of a head (else NULL).  Token number i of a sequence lies in page
+ * table[i / page_size] of the sequence at place i % page_size; its slot is page * page_size + place.  16-byte aligned.
+ */
+typedef struct moe_kv_cfg {
+    int32_t pages;        /* pages * page_size < 2^31 */
+    int32_t page_size;    /* tokens; a power of two, 16 to 65536 */
+    int32_t heads;        /* key heads, 1 to 1024 */
+    int32_t head_dim;     /* a multiple of 16, 16 to 256 */
+    int32_t dtype;        /* of k, v, q and out: MOE_F32 | MOE_BF16 */
+    int32_t cache_dtype;  /* MOE_BF16 | MOE_E4M3, and MOE_F32 where dtype is MOE_F32 */
+} moe_kv_cfg;
+
+/*
+ * Writes n tokens' keys and values into their slots, rounded to cache_dtype to the nearest; MOE_E4M3: a row of a head is divided by its
+ * scale max(max |row| / 448, 2^-126) first.
+ *   k, v: device, dtype, token i's [heads, head_dim] at element i * stride (stride >= heads * head_dim, a multiple of 8).
+ *   slots [n] int32: device; a slot outside of [0, pages * page_size) is no place: that token is not written.  No slot twice.
+ */
+int moe_kv_write(const moe_kv_cfg* cfg, int32_t n, const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* slots,
+                 void* k_pages, void* v_pages, float* k_scales, float* v_scales, void* stream);
+
+/* The reverse: rows of the cache, times their scales, rounded to dtype.  A token whose slot is no place is read as zeros. */
+int moe_kv_read(const moe_kv_cfg* cfg, int32_t n, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                const int32_t* slots, void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream);
+
+/*
+ * Attention of one new token per sequence over the cache: query head j of sequence b attends, with the keys and values of head
+ * j / (q_heads / heads), to the last `window` (0: all) of the sequence's first lens[b] tokens:
+ *     l_t = scale * q . k_t,   out = sum_t exp(l_t) v_t / sum_t exp(l_t),   lse = log sum_t exp(l_t).
+ * The cache is read once, its length split over the whole device and the parts joined; what lies beyond lens[b] or before the window
+ * is not looked at, whatever it is.  Sums and statistics are fp32; with dtype MOE_BF16 the weights exp(l_t) enter the sum rounded to
+ * bf16.  lens[b] = 0: out 0 and lse -infinity.
+ *   q: device, dtype, sequence b's [q_heads, head_dim] at element b * q_stride.  out [B, q_heads, head_dim]: dtype, written.
+ *   table [B, table_pages] int32: device, the sequences' pages (only those of attended tokens are read; a page outside of
+ *   [0, pages) is taken as the nearest one that exists).  lens [B] int32: device, taken as within [0, table_pages * page_size].
+ *   lse [B, q_heads] fp32: written, may be NULL.  ws: moe_attn_workspace_bytes(), 256-byte aligned; nothing in it is kept between calls.
+ */
+typedef struct moe_attn_cfg {
+    int32_t B;            /* sequences, 0 to 4096 */
+    int32_t q_heads;      /* a multiple of heads, at most 1024 */
+    int32_t table_pages;  /* pages a row of table has room for; table_pages * page_size <= 2^24 */
+    int32_t window;       /* 0: attend to all tokens */
+    float scale;          /* 0: 1 / sqrt(head_dim) */
+} moe_attn_cfg;
+int moe_attn_workspace_bytes(const moe_kv_cfg* cfg, const moe_attn_cfg* attn, size_t* bytes);
+int moe_attn_decode(const moe_kv_cfg* cfg, const moe_attn_cfg* attn, const void* q, int64_t q_stride, const void* k_pages,
+                    const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens,
+                    void* out, float* lse, void* ws, void* stream);
 
 #ifdef __cplusplus
 }

@@ -7,7 +7,9 @@ from typing import Optional
 
 import torch
 
-MOE_F32, MOE_BF16 = 0, 1
+MOE_F32, MOE_BF16, MOE_E4M3 = 0, 1, 2
+_TORCH = {MOE_F32: torch.float32, MOE_BF16: torch.bfloat16, MOE_E4M3: torch.float8_e4m3fn}
+_CODE = {"f32": MOE_F32, "bf16": MOE_BF16, "e4m3": MOE_E4M3}
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB: Optional[C.CDLL] = None
 
@@ -33,6 +35,44 @@ class MoeCfg(C.Structure):
     @property
     def torch_dtype(self):
         return torch.bfloat16 if self.dtype == MOE_BF16 else torch.float32
+
+
+class NormCfg(C.Structure):
+    """moe_norm_cfg: rows, columns and types of moe_add_norm."""
+    _fields_ = [("T", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32), ("q_group", C.c_int32), ("eps", C.c_float)]
+
+    @classmethod
+    def make(cls, T, d, dtype="bf16", eps=1e-6, q_group=0) -> "NormCfg":
+        return cls(T, d, _CODE[dtype] if isinstance(dtype, str) else int(dtype), q_group, eps)
+
+
+class KvCfg(C.Structure):
+    """moe_kv_cfg: a paged cache of keys and values."""
+    _fields_ = [("pages", C.c_int32), ("page_size", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("cache_dtype", C.c_int32)]
+
+    @classmethod
+    def make(cls, pages, page_size, heads, head_dim, dtype="bf16", cache_dtype=None) -> "KvCfg":
+        code = _CODE[dtype] if isinstance(dtype, str) else int(dtype)
+        cache = code if cache_dtype is None else _CODE[cache_dtype] if isinstance(cache_dtype, str) else int(cache_dtype)
+        return cls(pages, page_size, heads, head_dim, code, cache)
+
+    def empty(self, device="cuda"):
+        """(k_pages, v_pages, k_scales, v_scales) of this cache, not filled; the scales are None unless it is an e4m3 cache."""
+        shape = (self.pages, self.heads, self.page_size, self.head_dim)
+        k, v = (torch.empty(shape, dtype=_TORCH[self.cache_dtype], device=device) for _ in range(2))
+        if self.cache_dtype != MOE_E4M3:
+            return k, v, None, None
+        return (k, v, *(torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in range(2)))
+
+
+class AttnCfg(C.Structure):
+    """moe_attn_cfg: the sequences and query heads of one moe_attn_decode."""
+    _fields_ = [("B", C.c_int32), ("q_heads", C.c_int32), ("table_pages", C.c_int32), ("window", C.c_int32), ("scale", C.c_float)]
+
+    @classmethod
+    def make(cls, B, q_heads, table_pages, scale=0.0, window=0) -> "AttnCfg":
+        return cls(B, q_heads, table_pages, window, scale)
 
 
 def lib_path() -> str:
@@ -82,6 +122,11 @@ def lib() -> C.CDLL:
             "moe_timer_reset": [p],
             "moe_timer_read": [p, C.POINTER(C.c_float), C.c_int32, C.POINTER(C.c_int32)],
             "moe_layer_forward_timed": [cfgp, p, p, f32p, p, p, p, p, p],
+            "moe_add_norm": [p] * 9,
+            "moe_kv_write": [p, C.c_int32, p, C.c_int64, p, C.c_int64, p, p, p, p, p, p],
+            "moe_kv_read": [p, C.c_int32, p, p, p, p, p, p, C.c_int64, p, C.c_int64, p],
+            "moe_attn_workspace_bytes": [p, p, C.POINTER(C.c_size_t)],
+            "moe_attn_decode": [p, p, p, C.c_int64, p, p, p, p, p, p, p, p, p, p],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -295,3 +340,75 @@ class Timer:
 def moe_layer_forward_timed(cfg, x, W_g, gate_bias, W_packed, y, ws, timer: Timer, stream=None) -> None:
     _check(lib().moe_layer_forward_timed(C.byref(cfg), _ptr(x), _ptr(W_g), _ptr(gate_bias), _ptr(W_packed), _ptr(y),
                                          _ptr(ws), _stream(stream), timer.handle))
+
+
+def _array(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int) -> Optional[int]:
+    """Address of a contiguous device tensor of this type and size (None stays None: the library says whether it may be)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
+        raise MoeError(f"{name} must be a contiguous {dtype} tensor of {numel} elements (got {t.dtype}, shape {tuple(t.shape)}, "
+                       f"strides {t.stride()})")
+    if not t.is_cuda:
+        raise MoeError(f"{name} must be in device memory")
+    return t.data_ptr()
+
+
+def _head_rows(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int, heads: int, dim: int):
+    """Address and row stride of [n, heads, dim] whose rows may be part of wider ones, each row contiguous."""
+    if t is None:
+        return None, heads * dim
+    if t.dtype != dtype or tuple(t.shape) != (n, heads, dim) or (n > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim))):
+        raise MoeError(f"{name} must be a {dtype} tensor [{n}, {heads}, {dim}] with contiguous rows (got {t.dtype}, shape "
+                       f"{tuple(t.shape)}, strides {t.stride()})")
+    if not t.is_cuda:
+        raise MoeError(f"{name} must be in device memory")
+    return t.data_ptr(), t.stride(0) if n > 1 else heads * dim
+
+
+def moe_add_norm(cfg: NormCfg, x, residual, weight, sum, y, q=None, q_scale=None, stream=None) -> None:
+    dt, n = _TORCH.get(cfg.dtype), cfg.T * cfg.d
+    groups = cfg.T * (cfg.d // cfg.q_group if cfg.q_group > 0 else 1)
+    _check(lib().moe_add_norm(C.addressof(cfg), _array(x, "x", dt, n), _array(residual, "residual", dt, n),
+                              _array(weight, "weight", dt, cfg.d), _array(sum, "sum", dt, n), _array(y, "y", dt, n),
+                              _array(q, "q", torch.float8_e4m3fn, n), _array(q_scale, "q_scale", torch.float32, groups),
+                              _stream(stream)))
+
+
+def _cache(cfg: KvCfg, k_pages, v_pages, k_scales, v_scales):
+    dt, rows = _TORCH.get(cfg.cache_dtype), cfg.pages * cfg.heads * cfg.page_size
+    return (_array(k_pages, "k_pages", dt, rows * cfg.head_dim), _array(v_pages, "v_pages", dt, rows * cfg.head_dim),
+            _array(k_scales, "k_scales", torch.float32, rows), _array(v_scales, "v_scales", torch.float32, rows))
+
+
+def moe_kv_write(cfg: KvCfg, k, v, slots, k_pages, v_pages, k_scales=None, v_scales=None, stream=None) -> None:
+    n, dt = slots.numel(), _TORCH.get(cfg.dtype)
+    kp, ks = _head_rows(k, "k", dt, n, cfg.heads, cfg.head_dim)
+    vp, vs = _head_rows(v, "v", dt, n, cfg.heads, cfg.head_dim)
+    _check(lib().moe_kv_write(C.addressof(cfg), n, kp, ks, vp, vs, _array(slots, "slots", torch.int32, n),
+                              *_cache(cfg, k_pages, v_pages, k_scales, v_scales), _stream(stream)))
+
+
+def moe_kv_read(cfg: KvCfg, k_pages, v_pages, k_scales, v_scales, slots, k, v, stream=None) -> None:
+    n, dt = slots.numel(), _TORCH.get(cfg.dtype)
+    kp, ks = _head_rows(k, "k", dt, n, cfg.heads, cfg.head_dim)
+    vp, vs = _head_rows(v, "v", dt, n, cfg.heads, cfg.head_dim)
+    _check(lib().moe_kv_read(C.addressof(cfg), n, *_cache(cfg, k_pages, v_pages, k_scales, v_scales),
+                             _array(slots, "slots", torch.int32, n), kp, ks, vp, vs, _stream(stream)))
+
+
+def moe_attn_workspace_bytes(cfg: KvCfg, attn: AttnCfg) -> int:
+    n = C.c_size_t(0)
+    _check(lib().moe_attn_workspace_bytes(C.addressof(cfg), C.addressof(attn), C.byref(n)))
+    return n.value
+
+
+def moe_attn_decode(cfg: KvCfg, attn: AttnCfg, q, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws, stream=None) -> None:
+    B, heads, dt = attn.B, attn.q_heads, _TORCH.get(cfg.dtype)
+    qp, qs = _head_rows(q, "q", dt, B, heads, cfg.head_dim)
+    if ws is not None and ws.numel() * ws.element_size() < moe_attn_workspace_bytes(cfg, attn):
+        raise MoeError("ws is smaller than moe_attn_workspace_bytes")
+    _check(lib().moe_attn_decode(C.addressof(cfg), C.addressof(attn), qp, qs, *_cache(cfg, k_pages, v_pages, k_scales, v_scales),
+                                 _array(table, "table", torch.int32, B * attn.table_pages), _array(lens, "lens", torch.int32, B),
+                                 _array(out, "out", dt, B * heads * cfg.head_dim), _array(lse, "lse", torch.float32, B * heads),
+                                 _ptr(ws), _stream(stream)))

@@ -11,7 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe355.so")
-SOURCES = ["api.hip", "route.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "combine.hip", "schedule.hip"]
+SOURCES = ["api.hip", "route.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "combine.hip", "schedule.hip",
+           "api_decoder.hip", "norm.hip", "kv.hip", "attn.hip"]
 # ffn.hip is compiled in parts, side by side: each of its large kernels is an object of its own.
 PARTS = {"ffn.hip": 5}
 UNITS = [(src, part) for src in SOURCES for part in range(PARTS.get(src, 1))]

@@ -146,11 +146,6 @@ struct moe_timer {
     hipEvent_t* ev = nullptr;     // [cap][kStageEvents]
 };
 
-#define REQUIRE(ptr, name) \
-    if ((ptr) == nullptr) return fail(MOE_ERR_INVALID_ARG, "%s is NULL", name)
-#define REQUIRE_ALIGNED(ptr, name) \
-    if (!aligned16(ptr)) return fail(MOE_ERR_INVALID_ARG, "%s must be 16-byte aligned", name)
-
 extern "C" {
 
 const char* moe_last_error(void) { return g_err; }

@@ -28,6 +28,11 @@ void clear_error();
             return ::moe::fail(MOE_ERR_HIP, "launch of %s failed: %s", name, hipGetErrorString(e_)); \
     } while (0)
 
+#define REQUIRE(ptr, name) \
+    if ((ptr) == nullptr) return fail(MOE_ERR_INVALID_ARG, "%s is NULL", name)
+#define REQUIRE_ALIGNED(ptr, name) \
+    if (!aligned16(ptr)) return fail(MOE_ERR_INVALID_ARG, "%s must be 16-byte aligned", name)
+
 int check_cfg(const moe_cfg* cfg);
 
 // What the launchers need to know about a device, looked up once per device (under a lock) and kept.
@@ -118,6 +123,18 @@ int plan_slots(const int32_t* order, int n, int K, int32_t* slot_expert, int64_t
                int32_t* slot_of, int32_t* load);
 // inv NULL: row a of Yp is assignment a.
 int launch_combine(const moe_cfg& c, const void* Yp, const int32_t* inv, const float* w, void* y, hipStream_t s);
+
+// ---- around the expert layer ----
+int launch_add_norm(const moe_norm_cfg& c, const void* x, const void* residual, const void* weight, void* sum, void* y, void* q,
+                    float* q_scale, hipStream_t s);
+int launch_kv_write(const moe_kv_cfg& c, int n, const void* k, long k_stride, const void* v, long v_stride, const int32_t* slots,
+                    void* k_pages, void* v_pages, float* k_scales, float* v_scales, hipStream_t s);
+int launch_kv_read(const moe_kv_cfg& c, int n, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                   const int32_t* slots, void* k, long k_stride, void* v, long v_stride, hipStream_t s);
+size_t attn_workspace_bytes(const moe_kv_cfg& kv, const moe_attn_cfg& c);
+int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* q, long q_stride, const void* k_pages, const void* v_pages,
+                       const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens, void* out, float* lse,
+                       void* ws, hipStream_t s);
 
 // Batches of at most kDirectRows assignments, by one wave (all lanes; lane = assignment): the lanes that hold the same expert as this one
 // (0 where there is no assignment).  Values out of range are clamped, as in the batching kernels.

@@ -1,0 +1,54 @@
+// Device helpers shared by the kernels around the expert layer: 16-byte pieces, bf16 and e4m3 conversions, sums and
+// maxima over neighbouring lanes.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace moe {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kE4M3Max = 448.f;
+constexpr float kMinScale = 0x1p-126f;      // a row of zeros has a scale too, and 1 / scale is finite
+
+// Two values to bf16, to the nearest, ties to even.
+__device__ inline uint32_t to_bf16x2(float lo, float hi) {
+    const bf16x2 r = {static_cast<__bf16>(lo), static_cast<__bf16>(hi)};
+    return __builtin_bit_cast(uint32_t, r);
+}
+__device__ inline float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ inline float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+
+// Four values to e4m3, to the nearest, ties to even; |v| may not pass 448 by more than rounding, NaN stays NaN.
+__device__ inline uint32_t to_e4m3x4(float a, float b, float c, float d) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
+}
+__device__ inline void from_e4m3x4(uint32_t u, float (&v)[4]) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(u), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(u), true);
+    v[0] = lo[0]; v[1] = lo[1]; v[2] = hi[0]; v[3] = hi[1];
+}
+
+// The scale of values whose largest magnitude is `top`.
+__device__ inline float e4m3_scale(float top) { return fmaxf(top / kE4M3Max, kMinScale); }
+
+// Sum and maximum over each run of N neighbouring lanes (N a power of two up to 64), in all of its lanes.
+template <int N>
+__device__ inline float lanes_sum(float v) {
+#pragma unroll
+    for (int o = 1; o < N; o *= 2) v += __shfl_xor(v, o);
+    return v;
+}
+template <int N>
+__device__ inline float lanes_max(float v) {
+#pragma unroll
+    for (int o = 1; o < N; o *= 2) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+}  // namespace moe

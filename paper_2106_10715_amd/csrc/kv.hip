@@ -1,0 +1,153 @@
+// Rows of keys and values into the pages of a cache and back, quantised to e4m3 with a scale per row on the way.
+#include "common.h"
+#include "convert.h"
+
+namespace moe {
+namespace {
+
+// Eight elements of a type as they lie in memory, and as floats.
+template <int TYPE>
+struct Eight;
+template <>
+struct Eight<MOE_BF16> {
+    u32x4 u;
+    __device__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { v[2 * c] = bf16_lo(u[c]); v[2 * c + 1] = bf16_hi(u[c]); }
+    }
+    __device__ void set(const float (&v)[8]) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) u[c] = to_bf16x2(v[2 * c], v[2 * c + 1]);
+    }
+};
+template <>
+struct Eight<MOE_F32> {
+    f32x4 lo, hi;
+    __device__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { v[c] = lo[c]; v[4 + c] = hi[c]; }
+    }
+    __device__ void set(const float (&v)[8]) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { lo[c] = v[c]; hi[c] = v[4 + c]; }
+    }
+};
+template <>
+struct Eight<MOE_E4M3> {
+    u32x2 u;
+    __device__ void get(float (&v)[8]) const {
+        float a[4], b[4];
+        from_e4m3x4(u[0], a);
+        from_e4m3x4(u[1], b);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { v[c] = a[c]; v[4 + c] = b[c]; }
+    }
+    __device__ void set(const float (&v)[8]) {
+        u[0] = to_e4m3x4(v[0], v[1], v[2], v[3]);
+        u[1] = to_e4m3x4(v[4], v[5], v[6], v[7]);
+    }
+};
+
+// One side of the copy: keys or values.
+struct Side {
+    void* rows;         // [n, heads, dim], tokens `stride` elements apart
+    long stride;
+    void* pages;        // [pages, heads, page, dim]
+    float* scales;      // [pages, heads, page], e4m3 only
+};
+
+// A row (token, head) is held by LANES lanes with eight elements each.
+template <int TYPE, int CACHE, int LANES, bool WRITE>
+__global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* __restrict__ slots, int n, int heads, int eights,
+                                                 int page_bits, int n_slots) {
+    const int lane = threadIdx.x % LANES;
+    const long total = static_cast<long>(n) * heads, step = static_cast<long>(gridDim.x) * (256 / LANES);
+    for (long row = static_cast<long>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES; row < total; row += step) {
+        const int token = static_cast<int>(row / heads), head = static_cast<int>(row - static_cast<long>(token) * heads);
+        const int slot = slots[token];
+        const bool there = slot >= 0 && slot < n_slots;          // others are nowhere: not written, read as zeros
+        if (WRITE && !there) continue;
+        const long page = slot >> page_bits, in_page = slot & ((1 << page_bits) - 1);
+        const long at = ((page * heads + head) << page_bits) + in_page;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const Side& side = which == 0 ? k : v;
+            Eight<TYPE>* out = reinterpret_cast<Eight<TYPE>*>(side.rows) + (token * side.stride) / 8 + head * eights + lane;
+            Eight<CACHE>* in = reinterpret_cast<Eight<CACHE>*>(side.pages) + at * eights + lane;
+            float f[8] = {};
+            if (WRITE) {
+                float top = 0.f;
+                if (lane < eights) {
+                    out->get(f);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(f[c]));
+                }
+                if (CACHE == MOE_E4M3) {
+                    const float scale = e4m3_scale(lanes_max<LANES>(top)), inv = 1.f / scale;
+                    if (lane == 0) side.scales[at] = scale;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) f[c] *= inv;
+                }
+                if (lane < eights) {
+                    Eight<CACHE> e;
+                    e.set(f);
+                    *in = e;
+                }
+            } else if (lane < eights) {
+                if (there) {
+                    in->get(f);
+                    if (CACHE == MOE_E4M3) {
+                        const float scale = side.scales[at];
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) f[c] *= scale;
+                    }
+                }
+                Eight<TYPE> e;
+                e.set(f);
+                *out = e;
+            }
+        }
+    }
+}
+
+template <int TYPE, int CACHE, bool WRITE>
+int launch(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int32_t* slots, hipStream_t s) {
+    const int eights = c.head_dim / 8, bits = __builtin_ctz(c.page_size);
+    const long rows = static_cast<long>(n) * c.heads;
+    auto run = [&](auto kernel, int lanes) {
+        const long blocks = (rows + 256 / lanes - 1) / (256 / lanes);
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, k, v, slots, n, c.heads,
+                           eights, bits, c.pages << bits);
+    };
+    if (eights <= 8) run(kv_kernel<TYPE, CACHE, 8, WRITE>, 8);
+    else if (eights <= 16) run(kv_kernel<TYPE, CACHE, 16, WRITE>, 16);
+    else run(kv_kernel<TYPE, CACHE, 32, WRITE>, 32);
+    MOE_LAUNCH_CHECK("kv_kernel");
+    return MOE_OK;
+}
+
+template <bool WRITE>
+int for_types(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int32_t* slots, hipStream_t s) {
+    if (c.dtype == MOE_BF16)
+        return c.cache_dtype == MOE_BF16 ? launch<MOE_BF16, MOE_BF16, WRITE>(c, n, k, v, slots, s)
+                                         : launch<MOE_BF16, MOE_E4M3, WRITE>(c, n, k, v, slots, s);
+    if (c.cache_dtype == MOE_F32) return launch<MOE_F32, MOE_F32, WRITE>(c, n, k, v, slots, s);
+    return c.cache_dtype == MOE_BF16 ? launch<MOE_F32, MOE_BF16, WRITE>(c, n, k, v, slots, s)
+                                     : launch<MOE_F32, MOE_E4M3, WRITE>(c, n, k, v, slots, s);
+}
+
+}  // namespace
+
+int launch_kv_write(const moe_kv_cfg& c, int n, const void* k, long k_stride, const void* v, long v_stride, const int32_t* slots,
+                    void* k_pages, void* v_pages, float* k_scales, float* v_scales, hipStream_t s) {
+    return for_types<true>(c, n, Side{const_cast<void*>(k), k_stride, k_pages, k_scales}, Side{const_cast<void*>(v), v_stride, v_pages, v_scales},
+                           slots, s);
+}
+
+int launch_kv_read(const moe_kv_cfg& c, int n, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                   const int32_t* slots, void* k, long k_stride, void* v, long v_stride, hipStream_t s) {
+    return for_types<false>(c, n, Side{k, k_stride, const_cast<void*>(k_pages), const_cast<float*>(k_scales)},
+                            Side{v, v_stride, const_cast<void*>(v_pages), const_cast<float*>(v_scales)}, slots, s);
+}
+
+}  // namespace moe
