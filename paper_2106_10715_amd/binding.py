@@ -149,9 +149,12 @@ def _ptr(t: Optional[torch.Tensor]):
     return C.c_void_p(t.data_ptr())
 
 
+# The current stream's handle without a Stream object around it (about a microsecond a call), where this torch has that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream(stream: Optional[torch.cuda.Stream]):
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return C.c_void_p(s.cuda_stream)
+    return stream.cuda_stream if stream is not None else _raw_stream(torch.cuda.current_device())
 
 
 def moe_workspace_bytes(cfg: MoeCfg) -> int:
@@ -346,24 +349,26 @@ def _array(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int)
     """Address of a contiguous device tensor of this type and size (None stays None: the library says whether it may be)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
-        raise MoeError(f"{name} must be a contiguous {dtype} tensor of {numel} elements (got {t.dtype}, shape {tuple(t.shape)}, "
-                       f"strides {t.stride()})")
-    if not t.is_cuda:
+    if t.dtype is dtype and t.numel() == numel and t.is_contiguous():
+        if t.is_cuda:
+            return t.data_ptr()
         raise MoeError(f"{name} must be in device memory")
-    return t.data_ptr()
+    raise MoeError(f"{name} must be a contiguous {dtype} tensor of {numel} elements (got {t.dtype}, shape {tuple(t.shape)}, "
+                   f"strides {t.stride()})")
 
 
 def _head_rows(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int, heads: int, dim: int):
     """Address and row stride of [n, heads, dim] whose rows may be part of wider ones, each row contiguous."""
     if t is None:
         return None, heads * dim
-    if t.dtype != dtype or tuple(t.shape) != (n, heads, dim) or (n > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim))):
-        raise MoeError(f"{name} must be a {dtype} tensor [{n}, {heads}, {dim}] with contiguous rows (got {t.dtype}, shape "
-                       f"{tuple(t.shape)}, strides {t.stride()})")
-    if not t.is_cuda:
-        raise MoeError(f"{name} must be in device memory")
-    return t.data_ptr(), t.stride(0) if n > 1 else heads * dim
+    if t.dtype is dtype and t.shape == (n, heads, dim):
+        row, head, one = t.stride()
+        if one == 1 and (head == dim or heads == 1) or n == 0:
+            if t.is_cuda:
+                return t.data_ptr(), row if n > 1 else heads * dim
+            raise MoeError(f"{name} must be in device memory")
+    raise MoeError(f"{name} must be a {dtype} tensor [{n}, {heads}, {dim}] with contiguous rows (got {t.dtype}, shape "
+                   f"{tuple(t.shape)}, strides {t.stride()})")
 
 
 def moe_add_norm(cfg: NormCfg, x, residual, weight, sum, y, q=None, q_scale=None, stream=None) -> None:
@@ -406,7 +411,7 @@ def moe_attn_workspace_bytes(cfg: KvCfg, attn: AttnCfg) -> int:
 def moe_attn_decode(cfg: KvCfg, attn: AttnCfg, q, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws, stream=None) -> None:
     B, heads, dt = attn.B, attn.q_heads, _TORCH.get(cfg.dtype)
     qp, qs = _head_rows(q, "q", dt, B, heads, cfg.head_dim)
-    if ws is not None and ws.numel() * ws.element_size() < moe_attn_workspace_bytes(cfg, attn):
+    if ws is not None and ws.nbytes < moe_attn_workspace_bytes(cfg, attn):
         raise MoeError("ws is smaller than moe_attn_workspace_bytes")
     _check(lib().moe_attn_decode(C.addressof(cfg), C.addressof(attn), qp, qs, *_cache(cfg, k_pages, v_pages, k_scales, v_scales),
                                  _array(table, "table", torch.int32, B * attn.table_pages), _array(lens, "lens", torch.int32, B),

@@ -5,16 +5,13 @@
 //
 // Both products are matrix instructions of 16 x 16 with the query heads of a key head as the 16 columns (idle columns of small groups
 // cost nothing where the cache's rows are what has to be waited for):
-//   S^T[token, head] = K Q^T   a lane's operands are 16-byte pieces of a row of K as they lie in memory,
+//   S^T[token, head] = K Q^T   rows of K come in whole runs of 16 tokens as they lie in memory and are turned to the operand's order
+//                              (lane = token) through LDS that belongs to the wave alone,
 //   O^T[dim, head] += V^T P^T  a lane's sums S are, of its head, the four tokens of its quarter of the wave: with two runs of 16 tokens it
 //                              holds eight of 32 tokens, just what this product wants of P^T in that lane, if V^T is given with its
 //                              tokens in the same order.  It is: a lane loads its pieces of those eight rows of V and swaps the
 //                              16-bit halves of pairs of rows.
-// So neither K, V nor P passes through the LDS.
-//
-// The work is the list of all (sequence, key head, run of 128 tokens); every block takes an equal stretch of it, found from the lengths on
-// the device, whatever they are.  A sequence's head that lies in several blocks' stretches is left by each as an unscaled sum with its
-// maximum and its weight, and joined by a second kernel in the order of the tokens.
+// So neither V nor P passes through the LDS, and no wave waits for another while it reads.
 #include <math.h>
 
 #include <algorithm>
@@ -25,8 +22,16 @@
 namespace moe {
 namespace {
 
-constexpr int kUnit = 128;          // tokens a block takes in one step: 32 per wave
+constexpr int kUnit = 128;          // tokens: the grain in which the work is shared out
+constexpr int kListed = 2048;       // up to so many sequences' lengths are kept in LDS (64 KB with what else is there)
 constexpr float kSlack = 8.f;       // the running maximum is raised only where a logit passes it by more than this (as a power of two)
+
+// An item of the work, a (sequence, key head), cut where a worker's stretch begins: written by that worker, for the join.
+struct Cut {
+    int rows;                       // its first query head's row of out and lse; -1: nothing is cut here, or not for the first time
+    int first, last;                // slot of its first part, worker of its last (in between: the slots 2 w)
+    int pad;
+};
 
 struct Attn {
     const void* q;
@@ -36,7 +41,8 @@ struct Attn {
     const int32_t *table, *lens;
     void* out;
     float* lse;
-    float *part_o, *part_ml;        // [workers][2][heads of an item][dim], [workers][2][heads of an item][2]
+    float *part_o, *part_ml;        // [workers][2][group][dim], [workers][2][group][2]: unscaled sums; their maximum and weight
+    Cut* cuts;                      // [workers]
     int B, heads, group, chunks, dim, pages, page_bits, table_pages, window;
     float scale;                    // times log2 e
 };
@@ -45,24 +51,38 @@ struct Attn {
 struct Span {
     int first, end, base, units;
 };
-__device__ inline Span span_of(const Attn& a, int b) {
+__device__ inline Span span_of(const Attn& a, int len) {
     Span s;
-    s.end = min(max(a.lens[b], 0), a.table_pages << a.page_bits);
+    s.end = min(max(len, 0), a.table_pages << a.page_bits);
     s.first = a.window > 0 ? max(0, s.end - a.window) : 0;
     s.base = s.first & ~15;
     s.units = (s.end - s.base + kUnit - 1) / kUnit;
     return s;
 }
 
-// Stretch `i` of `n` things cut into `w` stretches as even as can be, and the stretch thing r lies in.
-__device__ inline long cut_at(long n, int w, int i) {
-    const long q = n / w, rest = n - q * w;
-    return i * q + min(static_cast<long>(i), rest);
+// `n` things cut into `w` stretches as even as can be: where stretch i begins, and the stretch thing r lies in.
+struct Cuts {
+    long q, rest;
+    // n / d for n below 2^50 (a quotient of doubles is off by one at most)
+    __device__ static long over(long n, long d) {
+        long r = static_cast<long>(static_cast<double>(n) / static_cast<double>(d));
+        if (r * d > n) --r;
+        return r;
+    }
+    __device__ Cuts(long n, int w) : q(over(n, w)), rest(n - q * w) {}
+    __device__ long at(int i) const { return i * q + min(static_cast<long>(i), rest); }
+    __device__ int of(long r) const { return static_cast<int>(r < rest * (q + 1) ? over(r, q + 1) : rest + over(r - rest * (q + 1), q)); }
+};
+
+// Waves a SIMD holds of the kernels for heads of up to `dim` and one or two column tiles: what their registers come to (512 / waves), and
+// how many blocks of four waves a compute unit is given.
+constexpr int waves_of(bool f32, int dim, bool two) {
+    if (dim <= 64) return two || f32 ? 3 : 4;
+    if (dim <= 128) return two || f32 ? 2 : 3;
+    return 1;
 }
-__device__ inline int cut_of(long n, int w, long r) {
-    const long q = n / w, rest = n - q * w;
-    return static_cast<int>(r < rest * (q + 1) ? r / (q + 1) : rest + (r - rest * (q + 1)) / q);
-}
+
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // How a cache type and the arithmetic that goes with the activations' type lie in the lanes.
 template <bool F32, int CACHE, int DIM>
@@ -72,6 +92,8 @@ struct Layout {
     static constexpr int kPieces = DIM / (4 * kPiece);         // pieces of a row per lane: lane quarter g holds piece 4 i + g
     static constexpr int kHalves = DIM > 128 ? 2 : 1;          // V: a row is read in runs of up to 128 elements
     static constexpr int kOwn = DIM > 128 ? 8 : DIM / 16;      // of which each of 16 lanes holds this many
+    static constexpr int kRun = 16 * DIM * kWidth;             // bytes of 16 rows of K
+    static constexpr bool kStaged = kRun <= 8192;              // whether they pass through the LDS
 };
 
 template <int BYTES>
@@ -80,15 +102,21 @@ template <> struct Raw<4> { uint32_t w[1]; };
 template <> struct Raw<8> { uint32_t w[2]; };
 template <> struct Raw<16> { uint32_t w[4]; };
 template <> struct Raw<32> { uint32_t w[8]; };
+// `bytes` bytes of the cache from an address that is the same for the whole wave.  Loads from it take a lane's 32-bit offset and a wave's
+// without any arithmetic on pairs of registers, and give zeros past the end.  Non-temporal: the cache is read once.
+__device__ inline __amdgpu_buffer_rsrc_t stretch_of(const void* p, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
+}
 template <int BYTES>
-__device__ inline Raw<BYTES> load_raw(const char* p) {
+__device__ inline Raw<BYTES> load_raw(__amdgpu_buffer_rsrc_t from, uint32_t at, uint32_t wave_at) {
+    constexpr int kNonTemporal = 2;
     Raw<BYTES> r;
-    if constexpr (BYTES == 4) r.w[0] = *reinterpret_cast<const uint32_t*>(p);
-    if constexpr (BYTES == 8) { const u32x2 u = *reinterpret_cast<const u32x2*>(p); r.w[0] = u[0]; r.w[1] = u[1]; }
+    if constexpr (BYTES == 4) r.w[0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, wave_at, kNonTemporal);
+    if constexpr (BYTES == 8) { const u32x2 u = __builtin_amdgcn_raw_buffer_load_b64(from, at, wave_at, kNonTemporal); r.w[0] = u[0]; r.w[1] = u[1]; }
     if constexpr (BYTES >= 16)
 #pragma unroll
         for (int i = 0; i < BYTES / 16; ++i) {
-            const u32x4 u = reinterpret_cast<const u32x4*>(p)[i];
+            const u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(from, at + 16 * i, wave_at, kNonTemporal);
 #pragma unroll
             for (int c = 0; c < 4; ++c) r.w[4 * i + c] = u[c];
         }
@@ -144,6 +172,29 @@ struct Wave {
     f32x4 o[NT][L::kHalves][L::kOwn];                                               // O^T: dim 128 half + own (4 g + r) + j, head l % 16
     float m[NT], l[NT];                                                             // maximum (the same in all quarters), weight of the own tokens
 
+    uint32_t k_at[L::kPieces], k_in[L::kPieces], k_out[L::kPieces], v_at[L::kHalves];    // of this lane: bytes from a run's first row, bytes in the LDS
+    int row_bytes;
+
+    // What does not change from item to item.  Where rows are shorter than DIM, pieces past their end are taken from their last piece:
+    // Q has zeros there, and columns past the end are not stored.
+    __device__ void lay_out(const Attn& a, int lane) {
+        const int n = lane % 16, g = lane / 16, per = a.dim / L::kPiece;
+        row_bytes = a.dim * L::kWidth;
+#pragma unroll
+        for (int i = 0; i < L::kPieces; ++i) {
+            if constexpr (!L::kStaged) {
+                k_at[i] = n * row_bytes + 16 * min(4 * i + g, per - 1);
+                continue;
+            }
+            const int at = min(64 * i + lane, 16 * per - 1), token = at / per, piece = at - token * per;
+            k_at[i] = 16 * at;
+            k_in[i] = 16 * (token * 4 * L::kPieces + ((piece ^ token) & (4 * L::kPieces - 1)));          // 16 tokens' pieces: in 16 different places of a row
+            k_out[i] = 16 * (n * 4 * L::kPieces + ((min(4 * i + g, per - 1) ^ n) & (4 * L::kPieces - 1)));
+        }
+#pragma unroll
+        for (int hf = 0; hf < L::kHalves; ++hf) v_at[hf] = 4 * g * row_bytes + min(128 * hf + L::kOwn * n, a.dim - L::kOwn) * L::kWidth;
+    }
+
     // the query heads [head0, head0 + n_heads) of sequence b
     __device__ void start(const Attn& a, int b, int head0, int n_heads, int lane) {
         const int n = lane % 16, g = lane / 16;
@@ -181,36 +232,44 @@ struct Wave {
         }
     }
 
-    // Tokens [t0, t0 + 32) of sequence b and key head h, t0 a multiple of 16; those outside of the span weigh nothing.
-    __device__ void step(const Attn& a, const Span& span, int b, int h, int t0, int lane) {
-        const int n = lane % 16, g = lane / 16;
+    // The pages of the runs of up to 32 steps from token t0 on, `stride` tokens apart: lane 2 s + r holds that of run r of step s.
+    __device__ static int pages_of(const Attn& a, const Span& span, int b, int t0, int stride, int lane) {
+        const int t = min(t0 + (lane / 2) * stride + 16 * (lane % 2), (span.end - 1) & ~15);        // (past the end: a run that exists)
+        return min(max(a.table[static_cast<long>(b) * a.table_pages + (t >> a.page_bits)], 0), a.pages - 1);
+    }
+
+    // Tokens [t0, t0 + 32) of key head h, t0 a multiple of 16, step `at_step` of `ids`; those outside of the span weigh nothing.
+    // `mine`: a run of K in LDS that no other wave touches.
+    __device__ void step(char* mine, const Attn& a, const Span& span, int ids, int at_step, int h, int t0, int lane) {
+        const int g = lane / 16;
         constexpr int kRowBytes = L::kOwn * L::kWidth;
         Raw<16> k[2][L::kPieces];
         Raw<kRowBytes> v[2][4][L::kHalves];
         f32x4 ks[2], vs[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int t = min(t0 + 16 * r, (span.end - 1) & ~15);                // (past the end: any rows that exist)
-            const int page = min(max(a.table[static_cast<long>(b) * a.table_pages + (t >> a.page_bits)], 0), a.pages - 1);
+            const int t = min(t0 + 16 * r, (span.end - 1) & ~15), page = __builtin_amdgcn_readlane(ids, 2 * at_step + r);
             const long at = ((static_cast<long>(page) * a.heads + h) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
-            const char* kr = a.k_pages + at * a.dim * L::kWidth;
-            const char* vr = a.v_pages + at * a.dim * L::kWidth;
+            const auto kr = stretch_of(a.k_pages + at * row_bytes, 16 * row_bytes), vr = stretch_of(a.v_pages + at * row_bytes, 16 * row_bytes);
 #pragma unroll
-            for (int i = 0; i < L::kPieces; ++i) {
-                k[r][i] = Raw<16>{};
-                if ((4 * i + g) * L::kPiece < a.dim) k[r][i] = load_raw<16>(kr + (n * a.dim + (4 * i + g) * L::kPiece) * L::kWidth);
-            }
+            for (int i = 0; i < L::kPieces; ++i) k[r][i] = load_raw<16>(kr, k_at[i], 0);
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int hf = 0; hf < L::kHalves; ++hf) {
-                    v[r][c][hf] = Raw<kRowBytes>{};
-                    if (128 * hf + L::kOwn * n < a.dim)
-                        v[r][c][hf] = load_raw<kRowBytes>(vr + ((4 * g + c) * a.dim + 128 * hf + L::kOwn * n) * L::kWidth);
-                }
+                for (int hf = 0; hf < L::kHalves; ++hf) v[r][c][hf] = load_raw<kRowBytes>(vr, v_at[hf], c * row_bytes);
             if constexpr (CACHE == MOE_E4M3) {
-                ks[r] = *reinterpret_cast<const f32x4*>(a.k_scales + at + 4 * g);
-                vs[r] = *reinterpret_cast<const f32x4*>(a.v_scales + at + 4 * g);
+                ks[r] = __builtin_bit_cast(f32x4, load_raw<16>(stretch_of(a.k_scales + at, 64), 16 * g, 0));
+                vs[r] = __builtin_bit_cast(f32x4, load_raw<16>(stretch_of(a.v_scales + at, 64), 16 * g, 0));
+            }
+        }
+        if constexpr (L::kStaged) {
+            // (A wave's LDS operations are done in their order: it needs no barrier between what it writes and reads.)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                for (int i = 0; i < L::kPieces; ++i) *reinterpret_cast<u32x4*>(mine + k_in[i]) = __builtin_bit_cast(u32x4, k[r][i]);
+#pragma unroll
+                for (int i = 0; i < L::kPieces; ++i) k[r][i] = __builtin_bit_cast(Raw<16>, *reinterpret_cast<const u32x4*>(mine + k_out[i]));
             }
         }
 
@@ -333,12 +392,17 @@ struct Wave {
     }
 };
 
-// Heads of a work item and the LDS the waves' sums are joined in.
-template <int DIM, int NT>
-struct Join {
+// The LDS of a block: the waves' runs of K, then, where waves share an item, their sums.
+template <bool F32, int CACHE, int DIM, int NT, int TEAM>
+struct Lds {
     static constexpr int kCols = DIM > 128 ? 128 : DIM;
-    float o[4][16][kCols + 4];
-    float m[4][16 * NT], l[4][16 * NT];
+    struct Sums {
+        float o[4][16][kCols + 4];
+        float m[4][16 * NT], l[4][16 * NT];
+    };
+    using L = Layout<F32, CACHE, DIM>;
+    static constexpr size_t kRun = L::kStaged ? L::kRun : 0;                             // of one wave
+    static constexpr size_t kBytes = TEAM == 1 || 4 * kRun > sizeof(Sums) ? 4 * kRun : sizeof(Sums);
 };
 
 template <bool F32>
@@ -346,24 +410,165 @@ __device__ inline void store_out(const Attn& a, long at, float v) {
     if constexpr (F32) static_cast<float*>(a.out)[at] = v;
     else static_cast<__bf16*>(a.out)[at] = static_cast<__bf16>(v);
 }
+__device__ inline float natural_log_of_sum(float m, float weight) { return (m + __builtin_amdgcn_logf(weight)) * 0.6931471805599453f; }
 
-template <bool F32, int CACHE, int DIM, int NT>
-__global__ __launch_bounds__(256, 2) void attn_kernel(Attn a) {
+// One sequence and key head, units [u0, u1): all query heads over them, 16 * NT at a time, by the TEAM waves of a worker.  Results go to out
+// and lse where the units are all there are, else to part `slot`.
+template <bool F32, int CACHE, int DIM, int NT, int TEAM>
+__device__ void attend(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* lds, const Span& span, int b, int h, int u0, int u1, int chunk0, int chunk1,
+                       long slot, int wave, int lane) {
     using L = Layout<F32, CACHE, DIM>;
-    using J = Join<DIM, NT>;
-    constexpr int kHeads = 16 * NT;
-    extern __shared__ char lds[];
-    J& join = *reinterpret_cast<J*>(lds);
-    int* before = reinterpret_cast<int*>(lds + sizeof(J));            // [B + 1] units of the sequences before
-    __shared__ int wave_total[4];
-    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    using S = Lds<F32, CACHE, DIM, NT, TEAM>;
+    constexpr int kHeads = 16 * NT, kStride = 32 * TEAM;
+    char* mine = lds + wave * S::kRun;
+    const int n = lane % 16, g = lane / 16, q_heads = a.heads * a.group;
+    const bool whole = u0 == 0 && u1 == span.units;
+    for (int chunk = chunk0; chunk < chunk1; ++chunk) {
+        const int in_group = chunk * kHeads, head0 = h * a.group + in_group, n_heads = min(kHeads, a.group - in_group);
+        int t0 = span.base + u0 * kUnit + (TEAM > 1 ? 32 * wave : 0);
+        const int t_end = min(span.end, span.base + u1 * kUnit);
+        int ids = t0 < t_end ? w.pages_of(a, span, b, t0, kStride, lane) : 0;
+        w.start(a, b, head0, n_heads, lane);
+        while (t0 < t_end) {
+            const int steps = min(32, (t_end - t0 + kStride - 1) / kStride);
+            for (int s = 0; s < steps; ++s) w.step(mine, a, span, ids, s, h, t0 + s * kStride, lane);
+            t0 += steps * kStride;
+            if (t0 < t_end) ids = w.pages_of(a, span, b, t0, kStride, lane);
+        }
 
-    {                                                                 // the running sum of the sequences' units
-        const int per = (a.B + 255) / 256;
+        float l[NT], top[NT], weight[NT], factor[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            l[t] = quarters_sum(w.l[t]);
+            top[t] = w.m[t];
+            weight[t] = l[t];
+            factor[t] = 1.f;
+        }
+        if constexpr (TEAM > 1) {                              // the waves' sums of each head, by the largest of their maxima
+            auto& sums = *reinterpret_cast<typename S::Sums*>(lds);
+            __syncthreads();                                   // all waves are done with their runs of K
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                if (g == 0) {
+                    sums.m[wave][16 * t + n] = w.m[t];
+                    sums.l[wave][16 * t + n] = l[t];
+                }
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int c = 16 * t + n;
+                top[t] = fmaxf(fmaxf(sums.m[0][c], sums.m[1][c]), fmaxf(sums.m[2][c], sums.m[3][c]));
+                const float ref = top[t] == -INFINITY ? 0.f : top[t];
+                weight[t] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) weight[t] = fmaf(sums.l[i][c], __builtin_amdgcn_exp2f(sums.m[i][c] - ref), weight[t]);
+                factor[t] = __builtin_amdgcn_exp2f(w.m[t] - ref);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int head = 16 * t + n;                       // of the chunk
+            if (whole) factor[t] /= weight[t];
+            if ((TEAM == 1 || wave == 0) && g == 0 && head < n_heads) {
+                if (!whole) {
+                    a.part_ml[(slot * a.group + in_group + head) * 2] = top[t];
+                    a.part_ml[(slot * a.group + in_group + head) * 2 + 1] = weight[t];
+                } else if (a.lse != nullptr) {
+                    a.lse[static_cast<long>(b) * q_heads + head0 + head] = natural_log_of_sum(top[t], weight[t]);
+                }
+            }
+#pragma unroll
+            for (int hf = 0; hf < L::kHalves; ++hf) {
+                const long to_out = (static_cast<long>(b) * q_heads + head0) * a.dim + 128 * hf;
+                const long to_part = (slot * a.group + in_group) * a.dim + 128 * hf;
+                if constexpr (TEAM == 1) {
+                    if (head < n_heads)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int col = L::kOwn * (4 * g + r);
+                            if (128 * hf + col >= a.dim) continue;
+#pragma unroll
+                            for (int j = 0; j < L::kOwn; j += 4) {
+                                const float v[4] = {w.o[t][hf][j][r] * factor[t], w.o[t][hf][j + 1][r] * factor[t], w.o[t][hf][j + 2][r] * factor[t],
+                                                    w.o[t][hf][j + 3][r] * factor[t]};
+                                const long at = static_cast<long>(head) * a.dim + col + j;
+                                if (!whole) *reinterpret_cast<f32x4*>(a.part_o + to_part + at) = f32x4{v[0], v[1], v[2], v[3]};
+                                else if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to_out + at) = f32x4{v[0], v[1], v[2], v[3]};
+                                else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to_out + at) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+                            }
+                        }
+                } else {
+                    auto& sums = *reinterpret_cast<typename S::Sums*>(lds);
+                    if (t + hf > 0) __syncthreads();
+                    if (head < n_heads)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int j = 0; j < L::kOwn; ++j) sums.o[wave][n][L::kOwn * (4 * g + r) + j] = w.o[t][hf][j][r] * factor[t];
+                    __syncthreads();
+                    const int rows = min(16, n_heads - 16 * t), cols = min(S::kCols, a.dim - 128 * hf);
+                    for (int i = 64 * wave + lane; i < rows * S::kCols; i += 256) {
+                        const int row = i / S::kCols, col = i % S::kCols;
+                        if (col >= cols) continue;
+                        const float v = (sums.o[0][row][col] + sums.o[1][row][col]) + (sums.o[2][row][col] + sums.o[3][row][col]);
+                        const long at = static_cast<long>(16 * t + row) * a.dim + col;
+                        if (whole) store_out<F32>(a, to_out + at, v);
+                        else a.part_o[to_part + at] = v;
+                    }
+                }
+            }
+        }
+        if constexpr (TEAM > 1) __syncthreads();               // the LDS is K's again
+    }
+}
+
+// A sequence without tokens: this thread's share of its outputs.
+template <bool F32>
+__device__ inline void store_nothing(const Attn& a, int b, int head0, int n_heads, int tid) {
+    const long row = static_cast<long>(b) * a.heads * a.group + head0;
+    for (int i = tid; i < n_heads * a.dim; i += 256) store_out<F32>(a, row * a.dim + i, 0.f);
+    for (int i = tid; i < n_heads && a.lse != nullptr; i += 256) a.lse[row + i] = -INFINITY;
+}
+
+// Short sequences: a block for each sequence, key head and 16 * NT of its query heads; nothing is split.
+template <bool F32, int CACHE, int DIM, int NT>
+__global__ __launch_bounds__(256, waves_of(F32, DIM, NT == 2)) void attn_short_kernel(Attn a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
+    const int item = blockIdx.x / a.chunks, chunk = blockIdx.x - item * a.chunks, b = item / a.heads, h = item - b * a.heads;
+    Wave<F32, CACHE, DIM, NT> w;
+    w.lay_out(a, lane);
+    const Span span = span_of(a, a.lens[b]);
+    if (span.units == 0) {
+        store_nothing<F32>(a, b, h * a.group + chunk * 16 * NT, min(16 * NT, a.group - chunk * 16 * NT), threadIdx.x);
+        return;
+    }
+    attend<F32, CACHE, DIM, NT, 4>(a, w, lds, span, b, h, 0, span.units, chunk, chunk + 1, 0, wave, lane);
+}
+
+// The work is the list of all (sequence, key head, unit of tokens); every worker, a block's four waves (TEAM 4) or a wave (TEAM 1), takes an
+// equal stretch of it, found from the lengths on the device, whatever they are.  An item that lies in several stretches is left by each as a
+// part, and joined by attn_join_kernel in the order of the tokens.
+template <bool F32, int CACHE, int DIM, int NT, int TEAM>
+__global__ __launch_bounds__(256, waves_of(F32, DIM, NT == 2)) void attn_kernel(Attn a, int top_step) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    int* before = reinterpret_cast<int*>(lds + Lds<F32, CACHE, DIM, NT, TEAM>::kBytes);       // [B + 1] units of the sequences before
+    int* list = before + a.B + 1;                                     // their lengths, where there is room
+    const bool listed = a.B <= kListed;
+    __shared__ int wave_total[4];
+    const int tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
+    Wave<F32, CACHE, DIM, NT> w;
+    {
+        const int per = (a.B + 255) / 256, b0 = tid * per, b1 = min(b0 + per, a.B);
         int own = 0;
-        for (int i = 0; i < per; ++i)
-            if (tid * per + i < a.B) own += span_of(a, tid * per + i).units;
+        for (int i = b0; i < b1; ++i) {
+            const int len = a.lens[i];
+            if (listed) list[i] = len;
+            own += span_of(a, len).units;
+        }
+        w.lay_out(a, lane);
         int incl = own;
+#pragma unroll
         for (int o = 1; o < 64; o *= 2) {
             const int up = __shfl_up(incl, o);
             if (lane >= o) incl += up;
@@ -371,210 +576,180 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(Attn a) {
         if (lane == 63) wave_total[wave] = incl;
         __syncthreads();
         int at = incl - own;
-        for (int w = 0; w < wave; ++w) at += wave_total[w];
-        for (int i = 0; i < per; ++i)
-            if (tid * per + i < a.B) {
-                before[tid * per + i] = at;
-                at += span_of(a, tid * per + i).units;
-            }
-        if (tid == 255) before[a.B] = at;                             // (all of the later threads' sums are empty)
+        for (int i = 0; i < wave; ++i) at += wave_total[i];
+        for (int i = b0; i < b1; ++i) {
+            before[i] = at;
+            at += span_of(a, listed ? list[i] : a.lens[i]).units;
+        }
+        if (tid == 255) before[a.B] = at;                             // (the later threads' sums are empty)
         __syncthreads();
     }
-    const int per_unit = a.heads * a.chunks;                          // items of a sequence
-    const int q_heads = a.heads * a.group;
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+        if (before[b + 1] == before[b]) store_nothing<F32>(a, b, 0, a.heads * a.group, tid);
 
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {               // sequences without tokens
-        if (before[b + 1] != before[b]) continue;
-        for (int i = tid; i < q_heads * a.dim; i += 256) store_out<F32>(a, static_cast<long>(b) * q_heads * a.dim + i, 0.f);
-        for (int i = tid; i < q_heads && a.lse != nullptr; i += 256) a.lse[static_cast<long>(b) * q_heads + i] = -INFINITY;
-    }
-
-    const long total = static_cast<long>(before[a.B]) * per_unit;
-    long at = cut_at(total, gridDim.x, blockIdx.x);
-    const long stop = cut_at(total, gridDim.x, blockIdx.x + 1);
-    if (at >= stop) return;
+    const int worker = TEAM == 1 ? 4 * blockIdx.x + wave : blockIdx.x, workers = gridDim.x * (4 / TEAM);
+    const Cuts cuts(static_cast<long>(uniform(before[a.B])) * a.heads, workers);
+    long at = cuts.at(worker);
+    const long stop = cuts.at(worker + 1);
     int b = 0;                                                        // the last sequence that starts at or before `at`
-    for (int step = 4096; step > 0; step /= 2)
-        if (b + step < a.B && static_cast<long>(before[b + step]) * per_unit <= at) b += step;
+#pragma unroll 1
+    for (int step = top_step; step > 0; step /= 2)
+        if (b + step < a.B && static_cast<long>(uniform(before[b + step])) * a.heads <= at) b += step;
+    Cut cut{-1, 0, 0, 0};
     bool first_item = true;
     while (at < stop) {
-        while (static_cast<long>(before[b + 1]) * per_unit <= at) ++b;
-        const Span span = span_of(a, b);
-        const long in_b = at - static_cast<long>(before[b]) * per_unit;
-        const int item = static_cast<int>(in_b / span.units), u0 = static_cast<int>(in_b - static_cast<long>(item) * span.units);
+        while (static_cast<long>(uniform(before[b + 1])) * a.heads <= at) ++b;
+        const Span span = span_of(a, uniform(listed ? list[b] : a.lens[b]));
+        const int in_b = static_cast<int>(at - static_cast<long>(uniform(before[b])) * a.heads);        // (below heads * units <= 2^27)
+        const int h = in_b / span.units, u0 = in_b - h * span.units;
         const int u1 = static_cast<int>(min(static_cast<long>(span.units), u0 + (stop - at)));
-        const int h = item / a.chunks, chunk = item - h * a.chunks;
-        const int head0 = h * a.group + chunk * kHeads, n_heads = min(kHeads, a.group - chunk * kHeads);
-
-        Wave<F32, CACHE, DIM, NT> w;
-        w.start(a, b, head0, n_heads, lane);
-        for (int u = u0; u < u1; ++u) {
-            const int t0 = span.base + u * kUnit + 32 * wave;
-            if (t0 < span.end) w.step(a, span, b, h, t0, lane);
-        }
-
-        // the four waves' sums of each head, by the largest of their maxima
-        const int n = lane % 16, g = lane / 16;
-        float factor[NT], top[NT], weight[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const float l = quarters_sum(w.l[t]);
-            if (g == 0) {
-                join.m[wave][16 * t + n] = w.m[t];
-                join.l[wave][16 * t + n] = l;
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            top[t] = fmaxf(fmaxf(join.m[0][16 * t + n], join.m[1][16 * t + n]), fmaxf(join.m[2][16 * t + n], join.m[3][16 * t + n]));
-            const float ref = top[t] == -INFINITY ? 0.f : top[t];
-            weight[t] = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) weight[t] = fmaf(join.l[i][16 * t + n], __builtin_amdgcn_exp2f(join.m[i][16 * t + n] - ref), weight[t]);
-            factor[t] = __builtin_amdgcn_exp2f(w.m[t] - ref);
-        }
-        const bool whole = u0 == 0 && u1 == span.units;
-        const long slot = (2L * blockIdx.x + (first_item ? 0 : 1)) * kHeads;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (whole) {
-                factor[t] /= weight[t];
-                if (wave == 0 && g == 0 && 16 * t + n < n_heads && a.lse != nullptr)
-                    a.lse[static_cast<long>(b) * q_heads + head0 + 16 * t + n] = (top[t] + __builtin_amdgcn_logf(weight[t])) * 0.6931471805599453f;
-            } else if (wave == 0 && g == 0) {
-                a.part_ml[(slot + 16 * t + n) * 2] = top[t];
-                a.part_ml[(slot + 16 * t + n) * 2 + 1] = weight[t];
-            }
-#pragma unroll
-            for (int hf = 0; hf < L::kHalves; ++hf) {
-                if (t + hf > 0) __syncthreads();
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int j = 0; j < L::kOwn; ++j) join.o[wave][n][L::kOwn * (4 * g + r) + j] = w.o[t][hf][j][r] * factor[t];
-                __syncthreads();
-                const int rows = min(16, n_heads - 16 * t), cols = min(J::kCols, a.dim - 128 * hf);
-                for (int i = tid; i < rows * J::kCols; i += 256) {
-                    const int row = i / J::kCols, col = i % J::kCols;
-                    if (col >= cols) continue;
-                    const float v = (join.o[0][row][col] + join.o[1][row][col]) + (join.o[2][row][col] + join.o[3][row][col]);
-                    if (whole) store_out<F32>(a, (static_cast<long>(b) * q_heads + head0 + 16 * t + row) * a.dim + 128 * hf + col, v);
-                    else a.part_o[(slot + 16 * t + row) * a.dim + 128 * hf + col] = v;
-                }
-            }
-        }
-        __syncthreads();
+        if (u0 > 0 && cuts.at(worker - 1) <= at - u0)                 // begun in the stretch before (only a worker's first item can have)
+            cut = Cut{(b * a.heads + h) * a.group, 2 * (worker - 1) + (cuts.at(worker - 1) == at - u0 ? 0 : 1), cuts.of(at - u0 + span.units - 1), 0};
+        attend<F32, CACHE, DIM, NT, TEAM>(a, w, lds, span, b, h, u0, u1, 0, a.chunks, 2L * worker + (first_item ? 0 : 1), wave, lane);
         at += u1 - u0;
         first_item = false;
     }
+    if (lane == 0 && (TEAM == 1 || wave == 0)) a.cuts[worker] = cut;
 }
 
-// Joins the parts of the items that lie in several blocks' stretches: one block for each sequence and query head.
-template <bool F32>
-__global__ __launch_bounds__(256) void attn_join_kernel(Attn a, int workers, int item_heads) {
-    __shared__ int sums[4];
-    __shared__ float parts[256];
-    const int tid = threadIdx.x;
-    const int q_heads = a.heads * a.group;
-    const int b = blockIdx.x / q_heads, head = blockIdx.x - b * q_heads;
-    const int h = head / a.group, chunk = (head - h * a.group) / item_heads, row = head - h * a.group - chunk * item_heads;
-    int mine = 0, all = 0;
-    for (int i = tid; i < a.B; i += 256) {
-        const int u = span_of(a, i).units;
-        all += u;
-        if (i < b) mine += u;
-    }
-    auto over_block = [&](int v) {
-        for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
-        __syncthreads();
-        if (tid % 64 == 0) sums[tid / 64] = v;
-        __syncthreads();
-        return sums[0] + sums[1] + sums[2] + sums[3];
-    };
-    const long per_unit = static_cast<long>(a.heads) * a.chunks;
-    const long start = over_block(mine) * per_unit, total = over_block(all) * per_unit;
-    const int units = span_of(a, b).units;
-    if (units == 0) return;
-    const long r0 = start + static_cast<long>(h * a.chunks + chunk) * units;
-    const int w0 = cut_of(total, workers, r0), w1 = cut_of(total, workers, r0 + units - 1);
-    if (w0 == w1) return;                                             // one block had it all
-    const int first_slot = cut_at(total, workers, w0) == r0 ? 0 : 1;
-    auto slot_of = [&](int w) { return (2L * w + (w == w0 ? first_slot : 0)) * item_heads + row; };
-
-    float top = -INFINITY;
-    for (int w = w0 + tid; w <= w1; w += 256) top = fmaxf(top, a.part_ml[slot_of(w) * 2]);
+// Joins an item's parts, row by row (query head): blocks (w, y) those of the item that is cut for the first time where worker w's stretch
+// begins.  With TEAM 4 a block's waves share a row, with TEAM 1 (few parts) each wave has one of its own.
+template <bool F32, int TEAM>
+__global__ __launch_bounds__(256) void attn_join_kernel(Attn a) {
+    __shared__ f32x4 sums[TEAM == 4 ? 256 : 1];
+    constexpr int kLanes = 64 * TEAM, kAhead = 8;
+    const int w = blockIdx.x, tid = threadIdx.x, lane = TEAM == 4 ? tid : tid % 64;
+    const int row = TEAM == 4 ? blockIdx.y : 4 * blockIdx.y + tid / 64;
+    const Cut cut = a.cuts[w];
+    if (cut.rows < 0 || row >= a.group) return;
+    const int parts = cut.last - w + 2;
+    auto slot_of = [&](int i) { return static_cast<long>(i == 0 ? cut.first : 2 * (w - 1 + i)) * a.group + row; };
+    float top = -INFINITY, weight = 0.f;
+    for (int i = tid % 64; i < parts; i += 64) top = fmaxf(top, a.part_ml[slot_of(i) * 2]);
     top = lanes_max<64>(top);
-    if (tid % 64 == 0) parts[tid / 64] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(parts[0], parts[1]), fmaxf(parts[2], parts[3]));
     const float ref = top == -INFINITY ? 0.f : top;
-    float weight = 0.f;
-    __syncthreads();
-    for (int w = w0 + tid; w <= w1; w += 256) weight = fmaf(a.part_ml[slot_of(w) * 2 + 1], __builtin_amdgcn_exp2f(a.part_ml[slot_of(w) * 2] - ref), weight);
+    for (int i = tid % 64; i < parts; i += 64)
+        weight = fmaf(a.part_ml[slot_of(i) * 2 + 1], __builtin_amdgcn_exp2f(a.part_ml[slot_of(i) * 2] - ref), weight);
     weight = lanes_sum<64>(weight);
-    if (tid % 64 == 0) parts[tid / 64] = weight;
-    __syncthreads();
-    weight = (parts[0] + parts[1]) + (parts[2] + parts[3]);
-    if (tid == 0 && a.lse != nullptr) a.lse[static_cast<long>(b) * q_heads + head] = (top + __builtin_amdgcn_logf(weight)) * 0.6931471805599453f;
-
-    // columns of 64, four rows of threads over the parts
-    for (int c0 = 0; c0 < a.dim; c0 += 64) {
-        const int col = c0 + tid % 64;
-        float v = 0.f;
-        if (col < a.dim)
-            for (int w = w0 + tid / 64; w <= w1; w += 4)
-                v = fmaf(a.part_o[slot_of(w) * a.dim + col], __builtin_amdgcn_exp2f(a.part_ml[slot_of(w) * 2] - ref), v);
-        __syncthreads();
-        parts[tid] = v;
-        __syncthreads();
-        if (tid < 64 && col < a.dim)
-            store_out<F32>(a, (static_cast<long>(b) * q_heads + head) * a.dim + col,
-                           ((parts[tid] + parts[tid + 64]) + (parts[tid + 128] + parts[tid + 192])) / weight);
+    const int quads = a.dim / 4, at_once = kLanes / quads;            // threads of a part, parts at once
+    const int mine = lane / quads, col = lane - mine * quads;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = mine; i0 < parts && mine < at_once; i0 += kAhead * at_once) {
+        f32x4 p[kAhead];
+        float m[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {                            // past the last: the last again, with no weight
+            const long slot = slot_of(min(i0 + j * at_once, parts - 1));
+            p[j] = *reinterpret_cast<const f32x4*>(a.part_o + slot * a.dim + 4 * col);
+            m[j] = a.part_ml[slot * 2];
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (i0 + j * at_once >= parts) break;
+            const float f = __builtin_amdgcn_exp2f(m[j] - ref);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = fmaf(p[j][c], f, v[c]);
+        }
     }
+    const long head = static_cast<long>(cut.rows) + row;
+    if (lane == 0 && a.lse != nullptr) a.lse[head] = natural_log_of_sum(top, weight);
+    if constexpr (TEAM == 4) {
+        sums[lane] = v;
+        __syncthreads();
+        if (mine == 0)
+            for (int i = 1; i < at_once; ++i) v += sums[lane + i * quads];
+    } else {
+        const f32x4 own = v;
+        for (int i = 1; i < at_once; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] += __shfl(own[c], (lane + i * quads) % 64);
+    }
+    if (mine == 0)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) store_out<F32>(a, head * a.dim + 4 * col + c, v[c] / weight);
 }
 
-constexpr int kMaxWorkers = 1024;
+// How a call is cut.  Sequences of at most kShortUnits units are not split: a block for each.  Else the list of units is cut into a stretch per
+// worker: waves by themselves where there are many items for groups of one column tile (no wave waits for another between items), else blocks.
+constexpr int kShortUnits = 4, kManyItems = 1024, kMaxUnits = 256;
+struct Plan {
+    bool is_short;
+    int team, blocks, workers;
+};
+Plan plan_of(const moe_kv_cfg& kv, const moe_attn_cfg& c, int compute_units) {
+    const long room = static_cast<long>(c.table_pages) * kv.page_size;
+    const long longest = c.window > 0 ? std::min(room, c.window + 15L) : room, units = (longest + kUnit - 1) / kUnit;
+    const long items = static_cast<long>(c.B) * kv.heads;
+    Plan p;
+    p.is_short = units <= kShortUnits;
+    p.team = c.q_heads / kv.heads <= 16 && items >= kManyItems ? 1 : 4;
+    const int resident = waves_of(kv.dtype == MOE_F32, kv.head_dim, kv.dtype == MOE_BF16 && c.q_heads / kv.heads > 16);
+    const int per_cu = p.team == 4 ? std::min(2, resident) : resident;
+    p.blocks = static_cast<int>(std::min(units * items, static_cast<long>(per_cu) * std::min(compute_units, kMaxUnits)));
+    p.workers = p.blocks * (4 / p.team);
+    return p;
+}
 
-int item_heads_of(const moe_kv_cfg& kv, const moe_attn_cfg& c) { return c.q_heads / kv.heads <= 16 ? 16 : 32; }
+// The workspace: the parts' sums, their maxima and weights, the cuts.
+struct Parts {
+    size_t ml, cuts, bytes;
+    Parts(const moe_kv_cfg& kv, const moe_attn_cfg& c) {
+        const Plan p = plan_of(kv, c, kMaxUnits);
+        const size_t rows = p.is_short ? 0 : 2 * static_cast<size_t>(p.workers) * (c.q_heads / kv.heads);
+        ml = align256(rows * kv.head_dim * 4);
+        cuts = ml + align256(rows * 8);
+        bytes = std::max(cuts + align256(p.is_short ? 0 : p.workers * sizeof(Cut)), size_t(256));
+    }
+};
 
 template <bool F32, int CACHE, int DIM, int NT>
-int launch(const moe_kv_cfg& kv, const Attn& a, hipStream_t s) {
+int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) {
     int dev = 0;
     const DeviceInfo* info = nullptr;
     if (int rc = device_info(&dev, &info)) return rc;
-    const long longest = a.window > 0 ? std::min(static_cast<long>(a.table_pages) << a.page_bits, a.window + 15L) : static_cast<long>(a.table_pages) << a.page_bits;
-    const long units = (longest + kUnit - 1) / kUnit;
-    const long all = units * a.B * a.heads * a.chunks;
-    const int workers = static_cast<int>(std::min(std::min(all, static_cast<long>(kMaxWorkers)), 4L * info->compute_units));
-    const size_t lds = sizeof(Join<DIM, NT>) + sizeof(int) * (a.B + 1);
-    hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT>), dim3(workers), dim3(256), lds, s, a);
-    MOE_LAUNCH_CHECK("attn_kernel");
-    if (units > 1) {
-        hipLaunchKernelGGL((attn_join_kernel<F32>), dim3(a.B * a.heads * a.group), dim3(256), 0, s, a, workers, 16 * NT);
-        MOE_LAUNCH_CHECK("attn_join_kernel");
+    const Plan p = plan_of(kv, c, info->compute_units);
+    a.chunks = (a.group + 16 * NT - 1) / (16 * NT);
+    if (p.is_short) {
+        hipLaunchKernelGGL((attn_short_kernel<F32, CACHE, DIM, NT>), dim3(a.B * a.heads * a.chunks), dim3(256), (Lds<F32, CACHE, DIM, NT, 4>::kBytes), s, a);
+        MOE_LAUNCH_CHECK("attn_short_kernel");
+        return MOE_OK;
     }
+    int top_step = 1;
+    while (2 * top_step < a.B) top_step *= 2;
+    const size_t list = sizeof(int) * ((a.B <= kListed ? 2 : 1) * a.B + 1);
+    if constexpr (NT == 1)
+        if (p.team == 1)
+            hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT, 1>), dim3(p.blocks), dim3(256), (Lds<F32, CACHE, DIM, NT, 1>::kBytes) + list, s, a, top_step);
+    if (p.team == 4)
+        hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT, 4>), dim3(p.blocks), dim3(256), (Lds<F32, CACHE, DIM, NT, 4>::kBytes) + list, s, a, top_step);
+    MOE_LAUNCH_CHECK("attn_kernel");
+    if (p.team == 1) hipLaunchKernelGGL((attn_join_kernel<F32, 1>), dim3(p.workers, (a.group + 3) / 4), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_join_kernel<F32, 4>), dim3(p.workers, a.group), dim3(256), 0, s, a);
+    MOE_LAUNCH_CHECK("attn_join_kernel");
     return MOE_OK;
 }
 
+// fp32 products have no room for a second column tile in registers: larger groups read the cache again, 16 heads at a time.
 template <bool F32, int CACHE>
-int for_sizes(const moe_kv_cfg& kv, const Attn& a, hipStream_t s) {
-    const bool two = a.group > 16;
-    if (a.dim <= 64) return two ? launch<F32, CACHE, 64, 2>(kv, a, s) : launch<F32, CACHE, 64, 1>(kv, a, s);
-    if (a.dim <= 128) return two ? launch<F32, CACHE, 128, 2>(kv, a, s) : launch<F32, CACHE, 128, 1>(kv, a, s);
-    return two ? launch<F32, CACHE, 256, 2>(kv, a, s) : launch<F32, CACHE, 256, 1>(kv, a, s);
+int for_sizes(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) {
+    if constexpr (!F32)
+        if (a.group > 16) {
+            if (a.dim <= 64) return launch<F32, CACHE, 64, 2>(kv, c, a, s);
+            return a.dim <= 128 ? launch<F32, CACHE, 128, 2>(kv, c, a, s) : launch<F32, CACHE, 256, 2>(kv, c, a, s);
+        }
+    if (a.dim <= 64) return launch<F32, CACHE, 64, 1>(kv, c, a, s);
+    return a.dim <= 128 ? launch<F32, CACHE, 128, 1>(kv, c, a, s) : launch<F32, CACHE, 256, 1>(kv, c, a, s);
 }
 
 }  // namespace
 
-size_t attn_workspace_bytes(const moe_kv_cfg& kv, const moe_attn_cfg& c) {
-    const size_t rows = 2 * static_cast<size_t>(kMaxWorkers) * item_heads_of(kv, c);
-    return align256(rows * kv.head_dim * 4) + align256(rows * 8);
-}
+size_t attn_workspace_bytes(const moe_kv_cfg& kv, const moe_attn_cfg& c) { return Parts(kv, c).bytes; }
 
 int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* q, long q_stride, const void* k_pages, const void* v_pages,
                        const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens, void* out, float* lse,
                        void* ws, hipStream_t s) {
+    const Parts parts(kv, c);
+    char* base = static_cast<char*>(ws);
     Attn a;
     a.q = q;
     a.q_stride = q_stride;
@@ -586,22 +761,22 @@ int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* 
     a.lens = lens;
     a.out = out;
     a.lse = lse;
+    a.part_o = static_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float*>(base + parts.ml);
+    a.cuts = reinterpret_cast<Cut*>(base + parts.cuts);
     a.B = c.B;
     a.heads = kv.heads;
     a.group = c.q_heads / kv.heads;
-    const int item_heads = item_heads_of(kv, c);
-    a.part_o = static_cast<float*>(ws);
-    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(2 * static_cast<size_t>(kMaxWorkers) * item_heads * kv.head_dim * 4));
-    a.chunks = (a.group + item_heads - 1) / item_heads;
+    a.chunks = 0;                                                     // set where the column tiles are chosen
     a.dim = kv.head_dim;
     a.pages = kv.pages;
     a.page_bits = __builtin_ctz(kv.page_size);
     a.table_pages = c.table_pages;
     a.window = c.window;
     a.scale = (c.scale > 0.f ? c.scale : 1.f / sqrtf(static_cast<float>(kv.head_dim))) * 1.4426950408889634f;
-    if (kv.dtype == MOE_BF16) return kv.cache_dtype == MOE_BF16 ? for_sizes<false, MOE_BF16>(kv, a, s) : for_sizes<false, MOE_E4M3>(kv, a, s);
-    if (kv.cache_dtype == MOE_F32) return for_sizes<true, MOE_F32>(kv, a, s);
-    return kv.cache_dtype == MOE_BF16 ? for_sizes<true, MOE_BF16>(kv, a, s) : for_sizes<true, MOE_E4M3>(kv, a, s);
+    if (kv.dtype == MOE_BF16) return kv.cache_dtype == MOE_BF16 ? for_sizes<false, MOE_BF16>(kv, c, a, s) : for_sizes<false, MOE_E4M3>(kv, c, a, s);
+    if (kv.cache_dtype == MOE_F32) return for_sizes<true, MOE_F32>(kv, c, a, s);
+    return kv.cache_dtype == MOE_BF16 ? for_sizes<true, MOE_BF16>(kv, c, a, s) : for_sizes<true, MOE_E4M3>(kv, c, a, s);
 }
 
 }  // namespace moe

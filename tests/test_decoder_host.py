@@ -38,11 +38,14 @@ def test_oracle_attention_by_sums():
 KV = dict(pages=8, page_size=16, heads=2, head_dim=64)
 
 
-def test_workspace_covers_the_parts_of_every_block():
+def test_workspace_grows_with_what_is_split():
     kv = M.KvCfg.make(**KV)
-    for q_heads, item in ((2, 16), (32, 16), (34, 32), (256, 32)):
-        n = M.moe_attn_workspace_bytes(kv, M.AttnCfg.make(3, q_heads, 4))
-        assert n >= 2 * 1024 * item * (64 + 2) * 4 and n % 256 == 0
+    size = lambda **kw: M.moe_attn_workspace_bytes(kv, M.AttnCfg.make(**{**dict(B=3, q_heads=32, table_pages=1000), **kw}))
+    assert all(size(**kw) % 256 == 0 and size(**kw) >= 256 for kw in (dict(), dict(B=0), dict(B=4096, table_pages=1), dict(window=1)))
+    assert size(table_pages=1) <= size(table_pages=100) <= size()                 # short sequences are not split
+    assert size(q_heads=2) < size() < size(q_heads=1024)
+    parts = min(3 * 2 * 125, 512)                                                 # blocks that each may leave two parts of a head's group
+    assert size() >= 2 * parts * 16 * (64 + 2) * 4
 
 
 @pytest.mark.parametrize("kw,frag", [

@@ -225,11 +225,13 @@ def cache_of(seed, cfg, table, lens, k_std=1.0, window=0):
 def run_attention(cfg, arrays, q, table, lens, window=0, scale=0.0, want_lse=True):
     B, heads, dim = q.shape
     attn = M.AttnCfg.make(B, heads, table.shape[1], scale=scale, window=window)
-    ws = torch.full((M.moe_attn_workspace_bytes(cfg, attn),), 0xff, dtype=torch.uint8, device="cuda")
+    n = M.moe_attn_workspace_bytes(cfg, attn)
+    ws = torch.full((n + 4096,), 0xff, dtype=torch.uint8, device="cuda")
     out = torch.full((B, heads, dim), 7, dtype=q.dtype, device="cuda")
     lse = torch.full((B, heads), 7, dtype=torch.float32, device="cuda") if want_lse else None
     M.moe_attn_decode(cfg, attn, q, *arrays, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), out, lse, ws)
     torch.cuda.synchronize()
+    assert (ws[n:] == 0xff).all(), "written past the workspace"
     return out, lse
 
 
