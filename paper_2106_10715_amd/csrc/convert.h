@@ -37,6 +37,18 @@ __device__ inline void from_e4m3x4(uint32_t u, float (&v)[4]) {
 // The scale of values whose largest magnitude is `top`.
 __device__ inline float e4m3_scale(float top) { return fmaxf(top / kE4M3Max, kMinScale); }
 
+// Loads and stores that leave the caches to others, where STREAM says so.
+template <bool STREAM, typename T>
+__device__ inline T load_from(const T* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool STREAM, typename T>
+__device__ inline void store_to(T* p, T v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
 // Sum and maximum over each run of N neighbouring lanes (N a power of two up to 64), in all of its lanes.
 template <int N>
 __device__ inline float lanes_sum(float v) {

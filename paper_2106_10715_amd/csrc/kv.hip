@@ -56,8 +56,30 @@ struct Side {
     float* scales;      // [pages, heads, page], e4m3 only
 };
 
-// A row (token, head) is held by LANES lanes with eight elements each.
-template <int TYPE, int CACHE, int LANES, bool WRITE>
+template <bool STREAM, int TYPE>
+__device__ inline Eight<TYPE> load_eight(const Eight<TYPE>* p) {
+    Eight<TYPE> e;
+    if constexpr (TYPE == MOE_F32) {
+        e.lo = load_from<STREAM>(&p->lo);
+        e.hi = load_from<STREAM>(&p->hi);
+    } else {
+        e.u = load_from<STREAM>(&p->u);
+    }
+    return e;
+}
+template <bool STREAM, int TYPE>
+__device__ inline void store_eight(Eight<TYPE>* p, const Eight<TYPE>& e) {
+    if constexpr (TYPE == MOE_F32) {
+        store_to<STREAM>(&p->lo, e.lo);
+        store_to<STREAM>(&p->hi, e.hi);
+    } else {
+        store_to<STREAM>(&p->u, e.u);
+    }
+}
+
+// A row (token, head) is held by LANES lanes with eight elements each, its key and its value one after the other: both are requested
+// before either is used.  Bound by memory.  STREAM 1: non-temporal stores, 2: loads too.
+template <int TYPE, int CACHE, int LANES, bool WRITE, int STREAM>
 __global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* __restrict__ slots, int n, int heads, int eights,
                                                  int page_bits, int n_slots) {
     const int lane = threadIdx.x % LANES;
@@ -69,59 +91,88 @@ __global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* 
         if (WRITE && !there) continue;
         const long page = slot >> page_bits, in_page = slot & ((1 << page_bits) - 1);
         const long at = ((page * heads + head) << page_bits) + in_page;
+        const Side* sides[2] = {&k, &v};
+        Eight<TYPE>* plain[2];
+        Eight<CACHE>* cached[2];
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const Side& side = which == 0 ? k : v;
-            Eight<TYPE>* out = reinterpret_cast<Eight<TYPE>*>(side.rows) + (token * side.stride) / 8 + head * eights + lane;
-            Eight<CACHE>* in = reinterpret_cast<Eight<CACHE>*>(side.pages) + at * eights + lane;
-            float f[8] = {};
-            if (WRITE) {
-                float top = 0.f;
-                if (lane < eights) {
-                    out->get(f);
+        for (int i = 0; i < 2; ++i) {
+            plain[i] = reinterpret_cast<Eight<TYPE>*>(sides[i]->rows) + (token * sides[i]->stride) / 8 + head * eights + lane;
+            cached[i] = reinterpret_cast<Eight<CACHE>*>(sides[i]->pages) + at * eights + lane;
+        }
+        float f[2][8] = {}, scale[2];
+        if constexpr (WRITE) {
+            Eight<TYPE> e[2];
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(f[c]));
-                }
-                if (CACHE == MOE_E4M3) {
-                    const float scale = e4m3_scale(lanes_max<LANES>(top)), inv = 1.f / scale;
-                    if (lane == 0) side.scales[at] = scale;
+            for (int i = 0; i < 2; ++i)
+                if (lane < eights) e[i] = load_eight<STREAM == 2>(plain[i]);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) f[c] *= inv;
-                }
-                if (lane < eights) {
-                    Eight<CACHE> e;
-                    e.set(f);
-                    *in = e;
-                }
-            } else if (lane < eights) {
-                if (there) {
-                    in->get(f);
-                    if (CACHE == MOE_E4M3) {
-                        const float scale = side.scales[at];
+            for (int i = 0; i < 2; ++i) {
+                if (lane < eights) e[i].get(f[i]);
+                if constexpr (CACHE == MOE_E4M3) {
+                    float top = 0.f;
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) f[c] *= scale;
-                    }
+                    for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(f[i][c]));
+                    scale[i] = e4m3_scale(lanes_max<LANES>(top));
+                    if (lane == 0) sides[i]->scales[at] = scale[i];
+                    const float inv = 1.f / scale[i];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) f[i][c] *= inv;
                 }
-                Eight<TYPE> e;
-                e.set(f);
-                *out = e;
+                if (lane >= eights) continue;
+                Eight<CACHE> out;
+                out.set(f[i]);
+                store_eight<STREAM != 0>(cached[i], out);
+            }
+        } else if (lane < eights) {
+            Eight<CACHE> e[2];
+            if (there) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    e[i] = load_eight<STREAM == 2>(cached[i]);
+                    scale[i] = CACHE == MOE_E4M3 ? sides[i]->scales[at] : 1.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    e[i].get(f[i]);
+                    if constexpr (CACHE == MOE_E4M3)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) f[i][c] *= scale[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                Eight<TYPE> out;
+                out.set(f[i]);
+                store_eight<STREAM != 0>(plain[i], out);
             }
         }
     }
 }
 
-template <int TYPE, int CACHE, bool WRITE>
-int launch(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int32_t* slots, hipStream_t s) {
+template <int TYPE, int CACHE, bool WRITE, int STREAM>
+void launch(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int32_t* slots, hipStream_t s) {
     const int eights = c.head_dim / 8, bits = __builtin_ctz(c.page_size);
     const long rows = static_cast<long>(n) * c.heads;
     auto run = [&](auto kernel, int lanes) {
-        const long blocks = (rows + 256 / lanes - 1) / (256 / lanes);
-        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, k, v, slots, n, c.heads,
-                           eights, bits, c.pages << bits);
+        const long blocks = (rows + 256 / lanes - 1) / (256 / lanes), most = 1 << 20;     // one row per group of lanes, up to many millions of rows
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(256), 0, s, k, v, slots, n, c.heads, eights,
+                           bits, c.pages << bits);
     };
-    if (eights <= 8) run(kv_kernel<TYPE, CACHE, 8, WRITE>, 8);
-    else if (eights <= 16) run(kv_kernel<TYPE, CACHE, 16, WRITE>, 16);
-    else run(kv_kernel<TYPE, CACHE, 32, WRITE>, 32);
+    if (eights <= 8) run(kv_kernel<TYPE, CACHE, 8, WRITE, STREAM>, 8);
+    else if (eights <= 16) run(kv_kernel<TYPE, CACHE, 16, WRITE, STREAM>, 16);
+    else run(kv_kernel<TYPE, CACHE, 32, WRITE, STREAM>, 32);
+}
+
+// What is more than the caches hold does better without them.  us through the caches / non-temporal stores / loads too, 16 heads of 128, bf16:
+// writes of 4096 tokens (67 MB) 11.2 / 11.3 / 13.1, 8192 (134 MB) 26.3 / 20.3 / 23.4, 16384 (268 MB) 47.7 / 45.7 / 44.4; reads with a kernel
+// behind them that uses the rows: 8192 45.0 / 46.6 / 46.6, 16384 103.2 / 97.4 / 86.5.
+template <int TYPE, int CACHE, bool WRITE>
+int launch_for_size(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int32_t* slots, hipStream_t s) {
+    const size_t each = 2 * static_cast<size_t>(n) * c.heads * c.head_dim;
+    const size_t moved = each * ((TYPE == MOE_F32 ? 4 : 2) + (CACHE == MOE_F32 ? 4 : CACHE == MOE_BF16 ? 2 : 1));
+    if (moved > size_t(200) << 20) launch<TYPE, CACHE, WRITE, 2>(c, n, k, v, slots, s);
+    else if (WRITE && moved > size_t(80) << 20) launch<TYPE, CACHE, WRITE, WRITE ? 1 : 0>(c, n, k, v, slots, s);
+    else launch<TYPE, CACHE, WRITE, 0>(c, n, k, v, slots, s);
     MOE_LAUNCH_CHECK("kv_kernel");
     return MOE_OK;
 }
@@ -129,11 +180,11 @@ int launch(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int32
 template <bool WRITE>
 int for_types(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int32_t* slots, hipStream_t s) {
     if (c.dtype == MOE_BF16)
-        return c.cache_dtype == MOE_BF16 ? launch<MOE_BF16, MOE_BF16, WRITE>(c, n, k, v, slots, s)
-                                         : launch<MOE_BF16, MOE_E4M3, WRITE>(c, n, k, v, slots, s);
-    if (c.cache_dtype == MOE_F32) return launch<MOE_F32, MOE_F32, WRITE>(c, n, k, v, slots, s);
-    return c.cache_dtype == MOE_BF16 ? launch<MOE_F32, MOE_BF16, WRITE>(c, n, k, v, slots, s)
-                                     : launch<MOE_F32, MOE_E4M3, WRITE>(c, n, k, v, slots, s);
+        return c.cache_dtype == MOE_BF16 ? launch_for_size<MOE_BF16, MOE_BF16, WRITE>(c, n, k, v, slots, s)
+                                         : launch_for_size<MOE_BF16, MOE_E4M3, WRITE>(c, n, k, v, slots, s);
+    if (c.cache_dtype == MOE_F32) return launch_for_size<MOE_F32, MOE_F32, WRITE>(c, n, k, v, slots, s);
+    return c.cache_dtype == MOE_BF16 ? launch_for_size<MOE_F32, MOE_BF16, WRITE>(c, n, k, v, slots, s)
+                                     : launch_for_size<MOE_F32, MOE_E4M3, WRITE>(c, n, k, v, slots, s);
 }
 
 }  // namespace

@@ -6,8 +6,8 @@
 namespace moe {
 namespace {
 
-// ROW threads hold one row, V pieces of 16 bytes each; a block of at least 256 threads.
-template <bool BF16, int ROW, int V>
+// ROW threads hold one row, V pieces of 16 bytes each; a block of at least 256 threads.  STREAM 1: non-temporal stores, 2: loads too.
+template <bool BF16, int ROW, int V, int STREAM>
 __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void add_norm_kernel(const u32x4* x, const u32x4* residual,
                                                                         const u32x4* __restrict__ weight, u32x4* sum, u32x4* y,
                                                                         uint32_t* __restrict__ q, float* __restrict__ q_scale, int T,
@@ -53,8 +53,8 @@ __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void add_norm_kernel(const u
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int p = lane + i * ROW;
-        if (p < pieces) xr[i] = x[at + p];
-        if (p < pieces && residual != nullptr) rr[i] = residual[at + p];
+        if (p < pieces) xr[i] = load_from<STREAM == 2>(x + at + p);
+        if (p < pieces && residual != nullptr) rr[i] = load_from<STREAM == 2>(residual + at + p);
     }
     float v[V][E], squares = 0.f;
 #pragma unroll
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void add_norm_kernel(const u
 #pragma unroll
             for (int c = 0; c < E; ++c) v[i][c] += r[c];
         }
-        if (sum != nullptr) sum[at + p] = narrow(v[i]);
+        if (sum != nullptr) store_to<STREAM != 0>(sum + at + p, narrow(v[i]));
 #pragma unroll
         for (int c = 0; c < E; ++c) squares = fmaf(v[i][c], v[i][c], squares);
     }
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void add_norm_kernel(const u
             v[i][c] = v[i][c] * rms * w[c];
             top = fmaxf(top, fabsf(v[i][c]));
         }
-        if (y != nullptr) y[at + p] = narrow(v[i]);
+        if (y != nullptr) store_to<STREAM != 0>(y + at + p, narrow(v[i]));
     }
     if (q == nullptr) return;
     const int groups = group == 0 ? 1 : pieces * E / group;
@@ -112,14 +112,17 @@ __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void add_norm_kernel(const u
         if (p >= pieces) continue;
         const float inv = 1.f / scale;
 #pragma unroll
-        for (int c = 0; c < E; c += 4)
-            q[(at + p) * (E / 4) + c / 4] = to_e4m3x4(v[i][c] * inv, v[i][c + 1] * inv, v[i][c + 2] * inv, v[i][c + 3] * inv);
+        for (int c = 0; c < E; ++c) v[i][c] *= inv;
+        if constexpr (BF16)
+            store_to<STREAM != 0>(reinterpret_cast<u32x2*>(q) + at + p, u32x2{to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3]), to_e4m3x4(v[i][4], v[i][5], v[i][6], v[i][7])});
+        else
+            store_to<STREAM != 0>(q + at + p, to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3]));
     }
 }
 
-template <bool BF16>
-int launch(const moe_norm_cfg& c, const void* x, const void* residual, const void* weight, void* sum, void* y, void* q, float* q_scale,
-           hipStream_t s) {
+template <bool BF16, int STREAM>
+void launch(const moe_norm_cfg& c, const void* x, const void* residual, const void* weight, void* sum, void* y, void* q, float* q_scale,
+            hipStream_t s) {
     const int pieces = c.d / (BF16 ? 8 : 4);
     auto run = [&](auto kernel, int row) {
         const int rows = row < 256 ? 256 / row : 1;
@@ -127,24 +130,38 @@ int launch(const moe_norm_cfg& c, const void* x, const void* residual, const voi
                            static_cast<const u32x4*>(residual), static_cast<const u32x4*>(weight), static_cast<u32x4*>(sum),
                            static_cast<u32x4*>(y), static_cast<uint32_t*>(q), q_scale, c.T, pieces, c.q_group, c.eps, 1.f / c.d);
     };
-    if (pieces <= 64) run(add_norm_kernel<BF16, 64, 1>, 64);
-    else if (pieces <= 128) run(add_norm_kernel<BF16, 64, 2>, 64);
-    else if (pieces <= 256) run(add_norm_kernel<BF16, 256, 1>, 256);
-    else if (pieces <= 512) run(add_norm_kernel<BF16, 256, 2>, 256);
-    else if (pieces <= 1024) run(add_norm_kernel<BF16, 256, 4>, 256);
-    else if (pieces <= 2048) run(add_norm_kernel<BF16, 1024, 2>, 1024);
-    else if (pieces <= 4096) run(add_norm_kernel<BF16, 1024, 4>, 1024);
-    else if constexpr (!BF16) run(add_norm_kernel<BF16, 1024, 8>, 1024);
-    MOE_LAUNCH_CHECK("add_norm_kernel");
-    return MOE_OK;
+    // one piece per thread where a block can hold the row so (65536 x 4096: 363 us with 512 threads, 380 with 256 of two pieces)
+    if (pieces <= 64) run(add_norm_kernel<BF16, 64, 1, STREAM>, 64);
+    else if (pieces <= 128) run(add_norm_kernel<BF16, 64, 2, STREAM>, 64);
+    else if (pieces <= 256) run(add_norm_kernel<BF16, 256, 1, STREAM>, 256);
+    else if (pieces <= 512) run(add_norm_kernel<BF16, 512, 1, STREAM>, 512);
+    else if (pieces <= 1024) run(add_norm_kernel<BF16, 512, 2, STREAM>, 512);
+    else if (pieces <= 2048) run(add_norm_kernel<BF16, 1024, 2, STREAM>, 1024);
+    else if (pieces <= 4096) run(add_norm_kernel<BF16, 1024, 4, STREAM>, 1024);
+    else if constexpr (!BF16) run(add_norm_kernel<BF16, 1024, 8, STREAM>, 1024);
+}
+
+// What is more than the caches hold does better without them, even if the next kernel reads y: us alone (and with a kernel behind it that
+// reads y) through the caches / non-temporal stores / loads too, d 4096 in bf16:  2048 rows (67 MB) 10.8 (16.9) / 10.6 (18.3) / 12.8 (21.0),
+// 4096 rows (134 MB) 26.1 (40.2) / 20.4 (38.0) / 23.6 (36.3), 16384 rows (537 MB) 94.2 (140.9) / 88.9 (140.7) / 86.5 (132.6).
+template <bool BF16>
+void launch_for_size(const moe_norm_cfg& c, const void* x, const void* residual, const void* weight, void* sum, void* y, void* q, float* q_scale,
+                     hipStream_t s) {
+    const size_t es = BF16 ? 2 : 4, each = static_cast<size_t>(c.T) * c.d;
+    const size_t moved = each * (es * (1 + (residual != nullptr) + (sum != nullptr) + (y != nullptr)) + (q != nullptr));
+    if (moved <= size_t(100) << 20) launch<BF16, 0>(c, x, residual, weight, sum, y, q, q_scale, s);
+    else if (moved <= size_t(320) << 20) launch<BF16, 1>(c, x, residual, weight, sum, y, q, q_scale, s);
+    else launch<BF16, 2>(c, x, residual, weight, sum, y, q, q_scale, s);
 }
 
 }  // namespace
 
 int launch_add_norm(const moe_norm_cfg& c, const void* x, const void* residual, const void* weight, void* sum, void* y, void* q,
                     float* q_scale, hipStream_t s) {
-    return c.dtype == MOE_BF16 ? launch<true>(c, x, residual, weight, sum, y, q, q_scale, s)
-                               : launch<false>(c, x, residual, weight, sum, y, q, q_scale, s);
+    if (c.dtype == MOE_BF16) launch_for_size<true>(c, x, residual, weight, sum, y, q, q_scale, s);
+    else launch_for_size<false>(c, x, residual, weight, sum, y, q, q_scale, s);
+    MOE_LAUNCH_CHECK("add_norm_kernel");
+    return MOE_OK;
 }
 
 }  // namespace moe
