@@ -77,11 +77,14 @@ __device__ inline void store_eight(Eight<TYPE>* p, const Eight<TYPE>& e) {
     }
 }
 
-// A row (token, head) is held by LANES lanes with eight elements each, its key and its value one after the other: both are requested
-// before either is used.  Bound by memory.  STREAM 1: non-temporal stores, 2: loads too.
+// A row (token, head) is held by LANES lanes with eight elements each.  Bound by memory.  Where rows are quantised, the wait for a row's
+// maximum is made worth two rows: the same lanes take its key and its value, both requested before either is used (16384 tokens of 8 x 128:
+// 17.8 us, 19.8 with a block for each).  Else half of the blocks take the keys, half the values (32768 tokens of 64 x 64 read: 193 us, 204
+// with both in the same lanes).  STREAM 1: non-temporal stores, 2: loads too.
 template <int TYPE, int CACHE, int LANES, bool WRITE, int STREAM>
 __global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* __restrict__ slots, int n, int heads, int eights,
                                                  int page_bits, int n_slots) {
+    constexpr int kSides = WRITE && CACHE == MOE_E4M3 ? 2 : 1;
     const int lane = threadIdx.x % LANES;
     const long total = static_cast<long>(n) * heads, step = static_cast<long>(gridDim.x) * (256 / LANES);
     for (long row = static_cast<long>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES; row < total; row += step) {
@@ -91,22 +94,22 @@ __global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* 
         if (WRITE && !there) continue;
         const long page = slot >> page_bits, in_page = slot & ((1 << page_bits) - 1);
         const long at = ((page * heads + head) << page_bits) + in_page;
-        const Side* sides[2] = {&k, &v};
-        Eight<TYPE>* plain[2];
-        Eight<CACHE>* cached[2];
+        const Side* sides[2] = {kSides == 2 || blockIdx.y == 0 ? &k : &v, &v};
+        Eight<TYPE>* plain[kSides];
+        Eight<CACHE>* cached[kSides];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kSides; ++i) {
             plain[i] = reinterpret_cast<Eight<TYPE>*>(sides[i]->rows) + (token * sides[i]->stride) / 8 + head * eights + lane;
             cached[i] = reinterpret_cast<Eight<CACHE>*>(sides[i]->pages) + at * eights + lane;
         }
-        float f[2][8] = {}, scale[2];
+        float f[kSides][8] = {}, scale[kSides];
         if constexpr (WRITE) {
-            Eight<TYPE> e[2];
+            Eight<TYPE> e[kSides];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < kSides; ++i)
                 if (lane < eights) e[i] = load_eight<STREAM == 2>(plain[i]);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < kSides; ++i) {
                 if (lane < eights) e[i].get(f[i]);
                 if constexpr (CACHE == MOE_E4M3) {
                     float top = 0.f;
@@ -124,15 +127,15 @@ __global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* 
                 store_eight<STREAM != 0>(cached[i], out);
             }
         } else if (lane < eights) {
-            Eight<CACHE> e[2];
+            Eight<CACHE> e[kSides];
             if (there) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < kSides; ++i) {
                     e[i] = load_eight<STREAM == 2>(cached[i]);
                     scale[i] = CACHE == MOE_E4M3 ? sides[i]->scales[at] : 1.f;
                 }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < kSides; ++i) {
                     e[i].get(f[i]);
                     if constexpr (CACHE == MOE_E4M3)
 #pragma unroll
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* 
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < kSides; ++i) {
                 Eight<TYPE> out;
                 out.set(f[i]);
                 store_eight<STREAM != 0>(plain[i], out);
@@ -155,7 +158,7 @@ void launch(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int3
     const long rows = static_cast<long>(n) * c.heads;
     auto run = [&](auto kernel, int lanes) {
         const long blocks = (rows + 256 / lanes - 1) / (256 / lanes), most = 1 << 20;     // one row per group of lanes, up to many millions of rows
-        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(256), 0, s, k, v, slots, n, c.heads, eights,
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most), WRITE && CACHE == MOE_E4M3 ? 1 : 2), dim3(256), 0, s, k, v, slots, n, c.heads, eights,
                            bits, c.pages << bits);
     };
     if (eights <= 8) run(kv_kernel<TYPE, CACHE, 8, WRITE, STREAM>, 8);
