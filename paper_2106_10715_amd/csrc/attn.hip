@@ -22,8 +22,10 @@
 namespace moe {
 namespace {
 
-constexpr int kUnit = 128;          // tokens: the grain in which the work is shared out
-constexpr int kListed = 2048;       // up to so many sequences' lengths are kept in LDS (64 KB with what else is there)
+constexpr int kUnit = 128;          // tokens a block takes in one step, 32 for each of its four waves: the grain in which the work is shared out
+constexpr int kToll = 2;            // what the beginning and the end of an item cost, in units: short items take a block's time too
+constexpr int kAsk = 32;            // steps whose pages a wave looks up at once
+constexpr int kMaxB = 4096;         // sequences
 constexpr float kSlack = 8.f;       // the running maximum is raised only where a logit passes it by more than this (as a power of two)
 
 // An item of the work, a (sequence, key head), cut where a worker's stretch begins: written by that worker, for the join.
@@ -50,6 +52,7 @@ struct Attn {
 // The tokens [first, end) sequence b attends to, and `base`, `first` rounded down to a run of 16 (which lies in one page).
 struct Span {
     int first, end, base, units;
+    __device__ int places() const { return units == 0 ? 0 : units + kToll; }        // in the list of all work
 };
 __device__ inline Span span_of(const Attn& a, int len) {
     Span s;
@@ -74,13 +77,8 @@ struct Cuts {
     __device__ int of(long r) const { return static_cast<int>(r < rest * (q + 1) ? over(r, q + 1) : rest + over(r - rest * (q + 1), q)); }
 };
 
-// Waves a SIMD holds of the kernels for heads of up to `dim` and one or two column tiles: what their registers come to (512 / waves), and
-// how many blocks of four waves a compute unit is given.
-constexpr int waves_of(bool f32, int dim, bool two) {
-    if (dim <= 64) return two || f32 ? 3 : 4;
-    if (dim <= 128) return two || f32 ? 2 : 3;
-    return 1;
-}
+// Waves a SIMD has room for: with two, a wave has 256 registers.
+constexpr int waves_of(bool f32, int dim, int nt) { return nt == 1 && (dim <= 64 || (dim <= 128 && !f32)) ? 2 : 1; }
 
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -94,6 +92,7 @@ struct Layout {
     static constexpr int kOwn = DIM > 128 ? 8 : DIM / 16;      // of which each of 16 lanes holds this many
     static constexpr int kRun = 16 * DIM * kWidth;             // bytes of 16 rows of K
     static constexpr bool kStaged = kRun <= 8192;              // whether they pass through the LDS
+    static constexpr bool kAhead = DIM <= 128;                   // whether there are registers for a second tile
 };
 
 template <int BYTES>
@@ -195,9 +194,7 @@ struct Wave {
         for (int hf = 0; hf < L::kHalves; ++hf) v_at[hf] = 4 * g * row_bytes + min(128 * hf + L::kOwn * n, a.dim - L::kOwn) * L::kWidth;
     }
 
-    // the query heads [head0, head0 + n_heads) of sequence b
-    __device__ void start(const Attn& a, int b, int head0, int n_heads, int lane) {
-        const int n = lane % 16, g = lane / 16;
+    __device__ void reset() {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             m[t] = -INFINITY;
@@ -206,62 +203,76 @@ struct Wave {
             for (int h = 0; h < L::kHalves; ++h)
 #pragma unroll
                 for (int j = 0; j < L::kOwn; ++j) o[t][h][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const bool there = 16 * t + n < n_heads;
-            const long row = b * a.q_stride + static_cast<long>(head0 + 16 * t + n) * a.dim;
+        }
+    }
+
+    // Requests the query heads [head0, head0 + n_heads) of sequence b; zeros in the columns and past the row's end.
+    __device__ void load_q(const Attn& a, int b, int head0, int n_heads, int lane) {
+        constexpr int kBytes = F32 ? 4 : 2;
+        const int n = lane % 16, g = lane / 16;
+        const auto rows = stretch_of(static_cast<const char*>(a.q) + (b * a.q_stride + static_cast<long>(head0) * a.dim) * kBytes, n_heads * a.dim * kBytes);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < L::kPieces; ++i) {
                 const int d0 = (4 * i + g) * L::kPiece;
-                const bool in = there && d0 < a.dim;
+                const uint32_t at = d0 < a.dim ? ((16 * t + n) * a.dim + d0) * kBytes : 0x7fffff00;
                 if constexpr (F32) {
 #pragma unroll
                     for (int c = 0; c < L::kPiece; c += 4) {
-                        f32x4 u = {0.f, 0.f, 0.f, 0.f};
-                        if (in) u = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.q) + row + d0 + c);
+                        const f32x4 u = __builtin_bit_cast(f32x4, load_raw<16>(rows, at + 4 * c, 0));
 #pragma unroll
                         for (int e = 0; e < 4; ++e) q32[t][i][c + e] = u[e];
                     }
                 } else {
 #pragma unroll
-                    for (int s = 0; s < kSteps; ++s) {
-                        u32x4 u = {0, 0, 0, 0};
-                        if (in) u = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + row + d0 + 8 * s);
-                        q16[t][i][s] = __builtin_bit_cast(bf16x8, u);
-                    }
+                    for (int s = 0; s < kSteps; ++s) q16[t][i][s] = __builtin_bit_cast(bf16x8, load_raw<16>(rows, at + 16 * s, 0));
                 }
             }
-        }
     }
 
-    // The pages of the runs of up to 32 steps from token t0 on, `stride` tokens apart: lane 2 s + r holds that of run r of step s.
-    __device__ static int pages_of(const Attn& a, const Span& span, int b, int t0, int stride, int lane) {
-        const int t = min(t0 + (lane / 2) * stride + 16 * (lane % 2), (span.end - 1) & ~15);        // (past the end: a run that exists)
-        return min(max(a.table[static_cast<long>(b) * a.table_pages + (t >> a.page_bits)], 0), a.pages - 1);
+    // The pages of the runs of up to kAsk steps from token t0 on: lane 2 s + r holds that of run r of step s.
+    __device__ static int pages_of(const Attn& a, const Span& span, int b, int t0, int lane) {
+        const int t = min(t0 + (lane / 2) * kUnit + 16 * (lane % 2), (span.end - 1) & ~15);        // (past the end: a run that exists)
+        return a.table[static_cast<long>(b) * a.table_pages + (t >> a.page_bits)];
     }
 
-    // Tokens [t0, t0 + 32) of key head h, t0 a multiple of 16, step `at_step` of `ids`; those outside of the span weigh nothing.
-    // `mine`: a run of K in LDS that no other wave touches.
-    __device__ void step(char* mine, const Attn& a, const Span& span, int ids, int at_step, int h, int t0, int lane) {
-        const int g = lane / 16;
-        constexpr int kRowBytes = L::kOwn * L::kWidth;
+    // 32 tokens' rows of one key head as they come from the cache.
+    static constexpr int kRowBytes = L::kOwn * L::kWidth;
+    struct Tile {
         Raw<16> k[2][L::kPieces];
         Raw<kRowBytes> v[2][4][L::kHalves];
         f32x4 ks[2], vs[2];
+    };
+
+    // Requests tokens [t0, t0 + 32) of key head h, t0 a multiple of 16, step `s` of `ids`; reads nothing if not `wanted`.
+    __device__ void load(Tile& x, const Attn& a, const Span& span, int ids, int s, int h, int t0, bool wanted, int lane) const {
+        const int g = lane / 16, bytes = wanted ? 16 * row_bytes : 0;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int t = min(t0 + 16 * r, (span.end - 1) & ~15), page = __builtin_amdgcn_readlane(ids, 2 * at_step + r);
+            const int t = min(t0 + 16 * r, (span.end - 1) & ~15), page = min(max(__builtin_amdgcn_readlane(ids, (2 * s + r) & 63), 0), a.pages - 1);
             const long at = ((static_cast<long>(page) * a.heads + h) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
-            const auto kr = stretch_of(a.k_pages + at * row_bytes, 16 * row_bytes), vr = stretch_of(a.v_pages + at * row_bytes, 16 * row_bytes);
+            const auto kr = stretch_of(a.k_pages + at * row_bytes, bytes), vr = stretch_of(a.v_pages + at * row_bytes, bytes);
 #pragma unroll
-            for (int i = 0; i < L::kPieces; ++i) k[r][i] = load_raw<16>(kr, k_at[i], 0);
+            for (int i = 0; i < L::kPieces; ++i) x.k[r][i] = load_raw<16>(kr, k_at[i], 0);
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int hf = 0; hf < L::kHalves; ++hf) v[r][c][hf] = load_raw<kRowBytes>(vr, v_at[hf], c * row_bytes);
+                for (int hf = 0; hf < L::kHalves; ++hf) x.v[r][c][hf] = load_raw<kRowBytes>(vr, v_at[hf], c * row_bytes);
             if constexpr (CACHE == MOE_E4M3) {
-                ks[r] = __builtin_bit_cast(f32x4, load_raw<16>(stretch_of(a.k_scales + at, 64), 16 * g, 0));
-                vs[r] = __builtin_bit_cast(f32x4, load_raw<16>(stretch_of(a.v_scales + at, 64), 16 * g, 0));
+                x.ks[r] = __builtin_bit_cast(f32x4, load_raw<16>(stretch_of(a.k_scales + at, wanted ? 64 : 0), 16 * g, 0));
+                x.vs[r] = __builtin_bit_cast(f32x4, load_raw<16>(stretch_of(a.v_scales + at, wanted ? 64 : 0), 16 * g, 0));
             }
         }
+    }
+
+    // Attends to the tile of tokens [t0, t0 + 32); those outside of the span weigh nothing.
+    // `mine`: a run of K in LDS that no other wave touches.
+    __device__ void step(Tile& x, char* mine, const Attn& a, const Span& span, int t0, int lane) {
+        const int g = lane / 16;
+        auto &k = x.k;
+        auto &v = x.v;
+        auto &ks = x.ks, &vs = x.vs;
         if constexpr (L::kStaged) {
             // (A wave's LDS operations are done in their order: it needs no barrier between what it writes and reads.)
 #pragma unroll
@@ -392,19 +403,6 @@ struct Wave {
     }
 };
 
-// The LDS of a block: the waves' runs of K, then, where waves share an item, their sums.
-template <bool F32, int CACHE, int DIM, int NT, int TEAM>
-struct Lds {
-    static constexpr int kCols = DIM > 128 ? 128 : DIM;
-    struct Sums {
-        float o[4][16][kCols + 4];
-        float m[4][16 * NT], l[4][16 * NT];
-    };
-    using L = Layout<F32, CACHE, DIM>;
-    static constexpr size_t kRun = L::kStaged ? L::kRun : 0;                             // of one wave
-    static constexpr size_t kBytes = TEAM == 1 || 4 * kRun > sizeof(Sums) ? 4 * kRun : sizeof(Sums);
-};
-
 template <bool F32>
 __device__ inline void store_out(const Attn& a, long at, float v) {
     if constexpr (F32) static_cast<float*>(a.out)[at] = v;
@@ -412,150 +410,229 @@ __device__ inline void store_out(const Attn& a, long at, float v) {
 }
 __device__ inline float natural_log_of_sum(float m, float weight) { return (m + __builtin_amdgcn_logf(weight)) * 0.6931471805599453f; }
 
-// One sequence and key head, units [u0, u1): all query heads over them, 16 * NT at a time, by the TEAM waves of a worker.  Results go to out
-// and lse where the units are all there are, else to part `slot`.
-template <bool F32, int CACHE, int DIM, int NT, int TEAM>
-__device__ void attend(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* lds, const Span& span, int b, int h, int u0, int u1, int chunk0, int chunk1,
-                       long slot, int wave, int lane) {
-    using L = Layout<F32, CACHE, DIM>;
-    using S = Lds<F32, CACHE, DIM, NT, TEAM>;
-    constexpr int kHeads = 16 * NT, kStride = 32 * TEAM;
-    char* mine = lds + wave * S::kRun;
-    const int n = lane % 16, g = lane / 16, q_heads = a.heads * a.group;
-    const bool whole = u0 == 0 && u1 == span.units;
-    for (int chunk = chunk0; chunk < chunk1; ++chunk) {
-        const int in_group = chunk * kHeads, head0 = h * a.group + in_group, n_heads = min(kHeads, a.group - in_group);
-        int t0 = span.base + u0 * kUnit + (TEAM > 1 ? 32 * wave : 0);
-        const int t_end = min(span.end, span.base + u1 * kUnit);
-        int ids = t0 < t_end ? w.pages_of(a, span, b, t0, kStride, lane) : 0;
-        w.start(a, b, head0, n_heads, lane);
-        while (t0 < t_end) {
-            const int steps = min(32, (t_end - t0 + kStride - 1) / kStride);
-            for (int s = 0; s < steps; ++s) w.step(mine, a, span, ids, s, h, t0 + s * kStride, lane);
-            t0 += steps * kStride;
-            if (t0 < t_end) ids = w.pages_of(a, span, b, t0, kStride, lane);
-        }
+// One sequence and key head, units [u0, u1), and 16 * NT of its query heads.  slot -1: the units are all there are, else the part's place.
+struct Item {
+    int b, h, chunk, u0, u1;
+    long slot;
+    Span span;
+};
 
-        float l[NT], top[NT], weight[NT], factor[NT];
+// The waves' sums of up to 16 heads over up to 128 columns.
+template <int DIM, int NT>
+struct Sums {
+    static constexpr int kCols = DIM > 128 ? 128 : DIM;
+    float o[4][16][kCols + 4];
+    float m[4][16 * NT], l[4][16 * NT];
+};
+
+// A barrier for what lies in LDS: loads from memory stay on their way across it.
+__device__ inline void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Joins the four waves' sums of an item and stores its results, or its part's.  The block's last barrier before the next call comes after
+// every use of `sums`.
+template <bool F32, int CACHE, int DIM, int NT>
+__device__ void finish(const Attn& a, const Wave<F32, CACHE, DIM, NT>& w, Sums<DIM, NT>& sums, const Item& it, int wave, int lane) {
+    using L = Layout<F32, CACHE, DIM>;
+    constexpr int kCols = Sums<DIM, NT>::kCols;
+    const int n = lane % 16, g = lane / 16, tid = 64 * wave + lane;
+    const int in_group = 16 * NT * it.chunk, n_heads = min(16 * NT, a.group - in_group);
+    const long head0 = (static_cast<long>(it.b) * a.heads + it.h) * a.group + in_group, part0 = it.slot * a.group + in_group;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            l[t] = quarters_sum(w.l[t]);
-            top[t] = w.m[t];
-            weight[t] = l[t];
-            factor[t] = 1.f;
+    for (int t = 0; t < NT; ++t) {
+        const float l = quarters_sum(w.l[t]);
+        if (g == 0) {
+            sums.m[wave][16 * t + n] = w.m[t];
+            sums.l[wave][16 * t + n] = l;
         }
-        if constexpr (TEAM > 1) {                              // the waves' sums of each head, by the largest of their maxima
-            auto& sums = *reinterpret_cast<typename S::Sums*>(lds);
-            __syncthreads();                                   // all waves are done with their runs of K
+    }
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (g == 0) {
-                    sums.m[wave][16 * t + n] = w.m[t];
-                    sums.l[wave][16 * t + n] = l[t];
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int hf = 0; hf < L::kHalves; ++hf) {
+            if (16 * t + n < n_heads)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int j = 0; j < L::kOwn; j += 4)
+                        *reinterpret_cast<f32x4*>(&sums.o[wave][n][L::kOwn * (4 * g + r) + j]) =
+                            f32x4{w.o[t][hf][j][r], w.o[t][hf][j + 1][r], w.o[t][hf][j + 2][r], w.o[t][hf][j + 3][r]};
+            lds_barrier();
+            const int rows = min(16, n_heads - 16 * t), quads = min(kCols, a.dim - 128 * hf) / 4;
+            for (int i = tid; i < rows * (kCols / 4); i += 256) {
+                const int row = i / (kCols / 4), col = i % (kCols / 4), c = 16 * t + row;
+                if (col >= quads) continue;
+                const float top = fmaxf(fmaxf(sums.m[0][c], sums.m[1][c]), fmaxf(sums.m[2][c], sums.m[3][c])), ref = top == -INFINITY ? 0.f : top;
+                float weight = 0.f;
+                f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    const float f = __builtin_amdgcn_exp2f(sums.m[i4][c] - ref);
+                    const f32x4 o = *reinterpret_cast<const f32x4*>(&sums.o[i4][row][4 * col]);
+                    weight = fmaf(sums.l[i4][c], f, weight);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = fmaf(o[e], f, v[e]);
                 }
-            __syncthreads();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int c = 16 * t + n;
-                top[t] = fmaxf(fmaxf(sums.m[0][c], sums.m[1][c]), fmaxf(sums.m[2][c], sums.m[3][c]));
-                const float ref = top[t] == -INFINITY ? 0.f : top[t];
-                weight[t] = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) weight[t] = fmaf(sums.l[i][c], __builtin_amdgcn_exp2f(sums.m[i][c] - ref), weight[t]);
-                factor[t] = __builtin_amdgcn_exp2f(w.m[t] - ref);
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int head = 16 * t + n;                       // of the chunk
-            if (whole) factor[t] /= weight[t];
-            if ((TEAM == 1 || wave == 0) && g == 0 && head < n_heads) {
-                if (!whole) {
-                    a.part_ml[(slot * a.group + in_group + head) * 2] = top[t];
-                    a.part_ml[(slot * a.group + in_group + head) * 2 + 1] = weight[t];
-                } else if (a.lse != nullptr) {
-                    a.lse[static_cast<long>(b) * q_heads + head0 + head] = natural_log_of_sum(top[t], weight[t]);
-                }
-            }
-#pragma unroll
-            for (int hf = 0; hf < L::kHalves; ++hf) {
-                const long to_out = (static_cast<long>(b) * q_heads + head0) * a.dim + 128 * hf;
-                const long to_part = (slot * a.group + in_group) * a.dim + 128 * hf;
-                if constexpr (TEAM == 1) {
-                    if (head < n_heads)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int col = L::kOwn * (4 * g + r);
-                            if (128 * hf + col >= a.dim) continue;
-#pragma unroll
-                            for (int j = 0; j < L::kOwn; j += 4) {
-                                const float v[4] = {w.o[t][hf][j][r] * factor[t], w.o[t][hf][j + 1][r] * factor[t], w.o[t][hf][j + 2][r] * factor[t],
-                                                    w.o[t][hf][j + 3][r] * factor[t]};
-                                const long at = static_cast<long>(head) * a.dim + col + j;
-                                if (!whole) *reinterpret_cast<f32x4*>(a.part_o + to_part + at) = f32x4{v[0], v[1], v[2], v[3]};
-                                else if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to_out + at) = f32x4{v[0], v[1], v[2], v[3]};
-                                else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to_out + at) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
-                            }
-                        }
-                } else {
-                    auto& sums = *reinterpret_cast<typename S::Sums*>(lds);
-                    if (t + hf > 0) __syncthreads();
-                    if (head < n_heads)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-#pragma unroll
-                            for (int j = 0; j < L::kOwn; ++j) sums.o[wave][n][L::kOwn * (4 * g + r) + j] = w.o[t][hf][j][r] * factor[t];
-                    __syncthreads();
-                    const int rows = min(16, n_heads - 16 * t), cols = min(S::kCols, a.dim - 128 * hf);
-                    for (int i = 64 * wave + lane; i < rows * S::kCols; i += 256) {
-                        const int row = i / S::kCols, col = i % S::kCols;
-                        if (col >= cols) continue;
-                        const float v = (sums.o[0][row][col] + sums.o[1][row][col]) + (sums.o[2][row][col] + sums.o[3][row][col]);
-                        const long at = static_cast<long>(16 * t + row) * a.dim + col;
-                        if (whole) store_out<F32>(a, to_out + at, v);
-                        else a.part_o[to_part + at] = v;
+                if (it.slot >= 0) {
+                    *reinterpret_cast<f32x4*>(a.part_o + (part0 + c) * a.dim + 128 * hf + 4 * col) = v;
+                    if (hf == 0 && col == 0) {
+                        a.part_ml[(part0 + c) * 2] = top;
+                        a.part_ml[(part0 + c) * 2 + 1] = weight;
                     }
+                    continue;
                 }
+                const long at = (head0 + c) * a.dim + 128 * hf + 4 * col;
+                const float inv = 1.f / weight;
+                if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = v * inv;
+                else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = u32x2{to_bf16x2(v[0] * inv, v[1] * inv), to_bf16x2(v[2] * inv, v[3] * inv)};
+                if (hf == 0 && col == 0 && a.lse != nullptr) a.lse[head0 + c] = natural_log_of_sum(top, weight);
+            }
+            lds_barrier();
+        }
+}
+
+// The items a block works on, one after the other: the chunks of query heads of each (sequence, key head) in its stretch.
+struct Feed {
+    const Attn& a;
+    const int *before, *list;       // places of the sequences before; lengths
+    int worker, top_step, b;
+    long at, stop;
+    bool first;
+
+    __device__ long before_of(int i) const { return static_cast<long>(uniform(before[i])) * a.heads; }
+    __device__ Span span(int i) const { return span_of(a, uniform(list[i])); }
+    __device__ int sequence_at(long place) const {                   // the last one that begins at or before
+        int i = 0;
+#pragma unroll 1
+        for (int step = top_step; step > 0; step /= 2)
+            if (i + step < a.B && before_of(i + step) <= place) i += step;
+        return i;
+    }
+    // A cut that would leave an item's beginning to one block and its tokens to the next is moved to before it.
+    __device__ long moved(long place) const {
+        if (place >= before_of(a.B)) return place;
+        const int i = sequence_at(place), in_b = static_cast<int>(place - before_of(i)), in_item = in_b % span(i).places();
+        return in_item <= kToll ? place - in_item : place;
+    }
+    __device__ Feed(const Attn& args, const int* before_, const int* list_, const Cuts& cuts, int worker_, int top_step_)
+        : a(args), before(before_), list(list_), worker(worker_), top_step(top_step_), first(true) {
+        at = moved(cuts.at(worker));
+        stop = moved(cuts.at(worker + 1));
+        b = sequence_at(at);
+    }
+    // The piece at `at`, which must be below `stop`.
+    __device__ Item piece() {
+        while (before_of(b + 1) <= at) ++b;
+        Item it;
+        it.b = b;
+        it.chunk = 0;
+        it.span = span(b);
+        const int in_b = static_cast<int>(at - before_of(b)), places = it.span.places();       // (below heads * places < 2^28)
+        it.h = in_b / places;
+        const int in_item = in_b - it.h * places;
+        it.u0 = max(0, in_item - kToll);
+        it.u1 = static_cast<int>(min(static_cast<long>(places), in_item + (stop - at))) - kToll;
+        it.slot = it.u0 == 0 && it.u1 == it.span.units ? -1 : 2L * worker + (first ? 0 : 1);
+        return it;
+    }
+    __device__ bool next(Item& it) {
+        if (it.chunk + 1 < a.chunks) {
+            ++it.chunk;
+            return true;
+        }
+        at += it.u1 - it.u0 + (it.u0 == 0 ? kToll : 0);
+        first = false;
+        if (at >= stop) return false;
+        it = piece();
+        return true;
+    }
+};
+
+// Works through items, `more` saying which comes next.  A wave has two tiles on the way while it attends to a third (kAhead), the next
+// item's first ones among them, so that what an item's end costs is its barriers and not the memory's answer.
+template <bool F32, int CACHE, int DIM, int NT, typename More>
+__device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, Sums<DIM, NT>& sums, Item it, More more, int wave, int lane) {
+    using L = Layout<F32, CACHE, DIM>;
+    typename Wave<F32, CACHE, DIM, NT>::Tile x, y;
+    auto begin = [&](const Item& i) { return i.span.base + i.u0 * kUnit + 32 * wave; };
+    auto limit = [&](const Item& i) { return min(i.span.end, i.span.base + i.u1 * kUnit); };
+    auto steps_from = [&](const Item& i, int t) { return max(0, min(kAsk, (limit(i) - t + kUnit - 1) / kUnit)); };
+    auto ask_q = [&](const Item& i) { w.load_q(a, i.b, i.h * a.group + 16 * NT * i.chunk, min(16 * NT, a.group - 16 * NT * i.chunk), lane); };
+    int t = begin(it), steps = steps_from(it, t), ids = w.pages_of(a, it.span, it.b, t, lane);
+    ask_q(it);
+    w.reset();
+    if constexpr (L::kAhead) w.load(x, a, it.span, ids, 0, it.h, t, steps > 0, lane);
+    while (true) {
+        Item then = it;
+        const bool last = t + kAsk * kUnit >= limit(it), any = !last || more(then);
+        const int then_t = last ? begin(then) : t + kAsk * kUnit, then_steps = any ? steps_from(then, then_t) : 0;
+        const int then_ids = w.pages_of(a, then.span, then.b, any ? then_t : t, lane);
+        if constexpr (L::kAhead) {
+            if (steps == 0) w.load(x, a, then.span, then_ids, 0, then.h, then_t, then_steps > 0, lane);
+            for (int s = 0; s < steps; s += 2) {
+                w.load(y, a, it.span, ids, s + 1, it.h, t + (s + 1) * kUnit, s + 1 < steps, lane);
+                w.step(x, mine, a, it.span, t + s * kUnit, lane);
+                const bool here = s + 2 < steps, over = s + 2 >= steps;
+                w.load(x, a, over ? then.span : it.span, over ? then_ids : ids, over ? 0 : s + 2, over ? then.h : it.h, over ? then_t : t + (s + 2) * kUnit,
+                       here || (over && then_steps > 0), lane);
+                if (s + 1 < steps) w.step(y, mine, a, it.span, t + (s + 1) * kUnit, lane);
+            }
+        } else {
+            for (int s = 0; s < steps; ++s) {
+                w.load(x, a, it.span, ids, s, it.h, t + s * kUnit, true, lane);
+                w.step(x, mine, a, it.span, t + s * kUnit, lane);
             }
         }
-        if constexpr (TEAM > 1) __syncthreads();               // the LDS is K's again
+        if (last) {
+            if (any) ask_q(then);
+            finish<F32, CACHE, DIM, NT>(a, w, sums, it, wave, lane);
+            w.reset();
+            if (!any) return;
+        }
+        it = then;
+        t = then_t;
+        steps = then_steps;
+        ids = then_ids;
     }
 }
 
-// A sequence without tokens: this thread's share of its outputs.
+// Outputs of query heads of a sequence without tokens.
 template <bool F32>
-__device__ inline void store_nothing(const Attn& a, int b, int head0, int n_heads, int tid) {
-    const long row = static_cast<long>(b) * a.heads * a.group + head0;
+__device__ inline void store_nothing(const Attn& a, long row, int n_heads, int tid) {
     for (int i = tid; i < n_heads * a.dim; i += 256) store_out<F32>(a, row * a.dim + i, 0.f);
     for (int i = tid; i < n_heads && a.lse != nullptr; i += 256) a.lse[row + i] = -INFINITY;
 }
 
 // Short sequences: a block for each sequence, key head and 16 * NT of its query heads; nothing is split.
 template <bool F32, int CACHE, int DIM, int NT>
-__global__ __launch_bounds__(256, waves_of(F32, DIM, NT == 2)) void attn_short_kernel(Attn a) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+__global__ __launch_bounds__(256, waves_of(F32, DIM, NT)) void attn_short_kernel(Attn a) {
+    __shared__ __attribute__((aligned(16))) char runs[4][Layout<F32, CACHE, DIM>::kStaged ? Layout<F32, CACHE, DIM>::kRun : 16];
+    __shared__ Sums<DIM, NT> sums;
     const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
-    const int item = blockIdx.x / a.chunks, chunk = blockIdx.x - item * a.chunks, b = item / a.heads, h = item - b * a.heads;
+    const int pair = blockIdx.x / a.chunks;
+    Item it{pair / a.heads, pair % a.heads, static_cast<int>(blockIdx.x % a.chunks), 0, 0, -1, {}};
     Wave<F32, CACHE, DIM, NT> w;
     w.lay_out(a, lane);
-    const Span span = span_of(a, a.lens[b]);
-    if (span.units == 0) {
-        store_nothing<F32>(a, b, h * a.group + chunk * 16 * NT, min(16 * NT, a.group - chunk * 16 * NT), threadIdx.x);
+    it.span = span_of(a, a.lens[it.b]);
+    it.u1 = it.span.units;
+    if (it.u1 == 0) {
+        store_nothing<F32>(a, static_cast<long>(pair) * a.group + 16 * NT * it.chunk, min(16 * NT, a.group - 16 * NT * it.chunk), threadIdx.x);
         return;
     }
-    attend<F32, CACHE, DIM, NT, 4>(a, w, lds, span, b, h, 0, span.units, chunk, chunk + 1, 0, wave, lane);
+    work<F32, CACHE, DIM, NT>(a, w, runs[wave], sums, it, [](Item&) { return false; }, wave, lane);
 }
 
-// The work is the list of all (sequence, key head, unit of tokens); every worker, a block's four waves (TEAM 4) or a wave (TEAM 1), takes an
-// equal stretch of it, found from the lengths on the device, whatever they are.  An item that lies in several stretches is left by each as a
-// part, and joined by attn_join_kernel in the order of the tokens.
-template <bool F32, int CACHE, int DIM, int NT, int TEAM>
-__global__ __launch_bounds__(256, waves_of(F32, DIM, NT == 2)) void attn_kernel(Attn a, int top_step) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    int* before = reinterpret_cast<int*>(lds + Lds<F32, CACHE, DIM, NT, TEAM>::kBytes);       // [B + 1] units of the sequences before
-    int* list = before + a.B + 1;                                     // their lengths, where there is room
-    const bool listed = a.B <= kListed;
-    __shared__ int wave_total[4];
+// The work is the list of all (sequence, key head, unit of tokens); every block takes an equal stretch of it, found from the lengths on the
+// device, whatever they are.  An item that lies in several stretches is left by each as a part, and joined by attn_join_kernel in the order of
+// the tokens.
+template <bool F32, int CACHE, int DIM, int NT>
+__global__ __launch_bounds__(256, waves_of(F32, DIM, NT)) void attn_kernel(Attn a, int top_step) {
+    __shared__ __attribute__((aligned(16))) char runs[4][Layout<F32, CACHE, DIM>::kStaged ? Layout<F32, CACHE, DIM>::kRun : 16];
+    __shared__ Sums<DIM, NT> sums;
+    __shared__ int before[kMaxB + 1], list[kMaxB], wave_total[4];       // places of the sequences before; lengths
     const int tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
     Wave<F32, CACHE, DIM, NT> w;
     {
@@ -563,8 +640,8 @@ __global__ __launch_bounds__(256, waves_of(F32, DIM, NT == 2)) void attn_kernel(
         int own = 0;
         for (int i = b0; i < b1; ++i) {
             const int len = a.lens[i];
-            if (listed) list[i] = len;
-            own += span_of(a, len).units;
+            list[i] = len;
+            own += span_of(a, len).places();
         }
         w.lay_out(a, lane);
         int incl = own;
@@ -579,41 +656,32 @@ __global__ __launch_bounds__(256, waves_of(F32, DIM, NT == 2)) void attn_kernel(
         for (int i = 0; i < wave; ++i) at += wave_total[i];
         for (int i = b0; i < b1; ++i) {
             before[i] = at;
-            at += span_of(a, listed ? list[i] : a.lens[i]).units;
+            at += span_of(a, list[i]).places();
         }
         if (tid == 255) before[a.B] = at;                             // (the later threads' sums are empty)
         __syncthreads();
     }
     for (int b = blockIdx.x; b < a.B; b += gridDim.x)
-        if (before[b + 1] == before[b]) store_nothing<F32>(a, b, 0, a.heads * a.group, tid);
+        if (before[b + 1] == before[b]) store_nothing<F32>(a, static_cast<long>(b) * a.heads * a.group, a.heads * a.group, tid);
 
-    const int worker = TEAM == 1 ? 4 * blockIdx.x + wave : blockIdx.x, workers = gridDim.x * (4 / TEAM);
-    const Cuts cuts(static_cast<long>(uniform(before[a.B])) * a.heads, workers);
-    long at = cuts.at(worker);
-    const long stop = cuts.at(worker + 1);
-    int b = 0;                                                        // the last sequence that starts at or before `at`
-#pragma unroll 1
-    for (int step = top_step; step > 0; step /= 2)
-        if (b + step < a.B && static_cast<long>(uniform(before[b + step])) * a.heads <= at) b += step;
+    const int worker = blockIdx.x;
+    const Cuts cuts(static_cast<long>(uniform(before[a.B])) * a.heads, gridDim.x);
+    Feed feed(a, before, list, cuts, worker, top_step);
     Cut cut{-1, 0, 0, 0};
-    bool first_item = true;
-    while (at < stop) {
-        while (static_cast<long>(uniform(before[b + 1])) * a.heads <= at) ++b;
-        const Span span = span_of(a, uniform(listed ? list[b] : a.lens[b]));
-        const int in_b = static_cast<int>(at - static_cast<long>(uniform(before[b])) * a.heads);        // (below heads * units <= 2^27)
-        const int h = in_b / span.units, u0 = in_b - h * span.units;
-        const int u1 = static_cast<int>(min(static_cast<long>(span.units), u0 + (stop - at)));
-        if (u0 > 0 && cuts.at(worker - 1) <= at - u0)                 // begun in the stretch before (only a worker's first item can have)
-            cut = Cut{(b * a.heads + h) * a.group, 2 * (worker - 1) + (cuts.at(worker - 1) == at - u0 ? 0 : 1), cuts.of(at - u0 + span.units - 1), 0};
-        attend<F32, CACHE, DIM, NT, TEAM>(a, w, lds, span, b, h, u0, u1, 0, a.chunks, 2L * worker + (first_item ? 0 : 1), wave, lane);
-        at += u1 - u0;
-        first_item = false;
+    if (feed.at < feed.stop) {
+        const Item it = feed.piece();
+        const long start = feed.at - it.u0 - kToll, left = cuts.at(worker - 1);
+        if (it.u0 > 0 && left <= start + kToll)                       // begun in the stretch before
+            cut = Cut{(it.b * a.heads + it.h) * a.group, 2 * (worker - 1) + (left >= start ? 0 : 1), cuts.of(start + it.span.units + kToll - 1), 0};
+        if (tid == 0) a.cuts[worker] = cut;
+        work<F32, CACHE, DIM, NT>(a, w, runs[wave], sums, it, [&](Item& i) { return feed.next(i); }, wave, lane);
+    } else if (tid == 0) {
+        a.cuts[worker] = cut;
     }
-    if (lane == 0 && (TEAM == 1 || wave == 0)) a.cuts[worker] = cut;
 }
 
 // Joins an item's parts, row by row (query head): blocks (w, y) those of the item that is cut for the first time where worker w's stretch
-// begins.  With TEAM 4 a block's waves share a row, with TEAM 1 (few parts) each wave has one of its own.
+// begins.  With few parts each wave has a row of its own (TEAM 1), else a block's waves share one (TEAM 4).
 template <bool F32, int TEAM>
 __global__ __launch_bounds__(256) void attn_join_kernel(Attn a) {
     __shared__ f32x4 sums[TEAM == 4 ? 256 : 1];
@@ -669,12 +737,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a) {
         for (int c = 0; c < 4; ++c) store_out<F32>(a, head * a.dim + 4 * col + c, v[c] / weight);
 }
 
-// How a call is cut.  Sequences of at most kShortUnits units are not split: a block for each.  Else the list of units is cut into a stretch per
-// worker: waves by themselves where there are many items for groups of one column tile (no wave waits for another between items), else blocks.
-constexpr int kShortUnits = 4, kManyItems = 1024, kMaxUnits = 256;
+// How a call is cut.  Sequences of at most kShortUnits units are not split: a block for each item.  Else the list of units is cut into a
+// stretch per block.
+constexpr int kShortUnits = 4, kMaxUnits = 256;
 struct Plan {
     bool is_short;
-    int team, blocks, workers;
+    int workers;
 };
 Plan plan_of(const moe_kv_cfg& kv, const moe_attn_cfg& c, int compute_units) {
     const long room = static_cast<long>(c.table_pages) * kv.page_size;
@@ -682,11 +750,10 @@ Plan plan_of(const moe_kv_cfg& kv, const moe_attn_cfg& c, int compute_units) {
     const long items = static_cast<long>(c.B) * kv.heads;
     Plan p;
     p.is_short = units <= kShortUnits;
-    p.team = c.q_heads / kv.heads <= 16 && items >= kManyItems ? 1 : 4;
-    const int resident = waves_of(kv.dtype == MOE_F32, kv.head_dim, kv.dtype == MOE_BF16 && c.q_heads / kv.heads > 16);
-    const int per_cu = p.team == 4 ? std::min(2, resident) : resident;
-    p.blocks = static_cast<int>(std::min(units * items, static_cast<long>(per_cu) * std::min(compute_units, kMaxUnits)));
-    p.workers = p.blocks * (4 / p.team);
+    // One block per compute unit reads as fast as two and leaves fewer parts; only where heads are narrow and items many does a second one
+    // fill the gaps between items (us with one / two: 40 x 1024 tokens, 64 heads of 64: 123 / 104; 1 x 131072, 8 heads of 128: 85 / 88).
+    const int per_unit = kv.head_dim <= 64 && items >= 4 * kMaxUnits ? 2 : 1;
+    p.workers = static_cast<int>(std::min(units * items, static_cast<long>(per_unit) * std::min(compute_units, kMaxUnits)));
     return p;
 }
 
@@ -710,33 +777,25 @@ int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) 
     const Plan p = plan_of(kv, c, info->compute_units);
     a.chunks = (a.group + 16 * NT - 1) / (16 * NT);
     if (p.is_short) {
-        hipLaunchKernelGGL((attn_short_kernel<F32, CACHE, DIM, NT>), dim3(a.B * a.heads * a.chunks), dim3(256), (Lds<F32, CACHE, DIM, NT, 4>::kBytes), s, a);
+        hipLaunchKernelGGL((attn_short_kernel<F32, CACHE, DIM, NT>), dim3(a.B * a.heads * a.chunks), dim3(256), 0, s, a);
         MOE_LAUNCH_CHECK("attn_short_kernel");
         return MOE_OK;
     }
     int top_step = 1;
     while (2 * top_step < a.B) top_step *= 2;
-    const size_t list = sizeof(int) * ((a.B <= kListed ? 2 : 1) * a.B + 1);
-    if constexpr (NT == 1)
-        if (p.team == 1)
-            hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT, 1>), dim3(p.blocks), dim3(256), (Lds<F32, CACHE, DIM, NT, 1>::kBytes) + list, s, a, top_step);
-    if (p.team == 4)
-        hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT, 4>), dim3(p.blocks), dim3(256), (Lds<F32, CACHE, DIM, NT, 4>::kBytes) + list, s, a, top_step);
+    hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT>), dim3(p.workers), dim3(256), 0, s, a, top_step);
     MOE_LAUNCH_CHECK("attn_kernel");
-    if (p.team == 1) hipLaunchKernelGGL((attn_join_kernel<F32, 1>), dim3(p.workers, (a.group + 3) / 4), dim3(256), 0, s, a);
+    if (a.B * a.heads >= p.workers) hipLaunchKernelGGL((attn_join_kernel<F32, 1>), dim3(p.workers, (a.group + 3) / 4), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_join_kernel<F32, 4>), dim3(p.workers, a.group), dim3(256), 0, s, a);
     MOE_LAUNCH_CHECK("attn_join_kernel");
     return MOE_OK;
 }
 
-// fp32 products have no room for a second column tile in registers: larger groups read the cache again, 16 heads at a time.
+// fp32 products and heads of over 128 have no room for a second column tile in registers: larger groups read the cache again, 16 heads at a time.
 template <bool F32, int CACHE>
 int for_sizes(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) {
     if constexpr (!F32)
-        if (a.group > 16) {
-            if (a.dim <= 64) return launch<F32, CACHE, 64, 2>(kv, c, a, s);
-            return a.dim <= 128 ? launch<F32, CACHE, 128, 2>(kv, c, a, s) : launch<F32, CACHE, 256, 2>(kv, c, a, s);
-        }
+        if (a.group > 16 && a.dim <= 128) return a.dim <= 64 ? launch<F32, CACHE, 64, 2>(kv, c, a, s) : launch<F32, CACHE, 128, 2>(kv, c, a, s);
     if (a.dim <= 64) return launch<F32, CACHE, 64, 1>(kv, c, a, s);
     return a.dim <= 128 ? launch<F32, CACHE, 128, 1>(kv, c, a, s) : launch<F32, CACHE, 256, 1>(kv, c, a, s);
 }
