@@ -72,13 +72,16 @@ struct Cuts {
         if (r * d > n) --r;
         return r;
     }
-    __device__ Cuts(long n, int w) : q(over(n, w)), rest(n - q * w) {}
+    __device__ Cuts(long n, int w, double one_over_w) : q(static_cast<long>(static_cast<double>(n) * one_over_w)) {
+        q += q * w > n ? -1 : (q + 1) * w <= n ? 1 : 0;
+        rest = n - q * w;
+    }
     __device__ long at(int i) const { return i * q + min(static_cast<long>(i), rest); }
     __device__ int of(long r) const { return static_cast<int>(r < rest * (q + 1) ? over(r, q + 1) : rest + over(r - rest * (q + 1), q)); }
 };
 
 // Waves a SIMD has room for: with two, a wave has 256 registers.
-constexpr int waves_of(bool f32, int dim, int nt) { return nt == 1 && (dim <= 64 || (dim <= 128 && !f32)) ? 2 : 1; }
+constexpr int waves_of(bool f32, int cache, int dim, int nt) { return nt == 1 && (dim <= 64 || (dim <= 128 && !f32 && cache == MOE_E4M3)) ? 2 : 1; }
 
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -161,13 +164,28 @@ __device__ inline float quarters_sum(float v) {
     return v + __shfl_xor(v, 32);
 }
 
+// Two values as bf16, and what that leaves of them.
+__device__ inline uint32_t take_bf16x2(float& lo, float& hi) {
+    const uint32_t u = to_bf16x2(lo, hi);
+    lo -= bf16_lo(u);
+    hi -= bf16_hi(u);
+    return u;
+}
+
 // One wave's attention of 16 * NT query heads over some of an item's tokens.
+//
+// An fp32 cache takes the fp32 matrix instruction.  The other caches' values are bf16 values: the bf16 instruction multiplies them exactly, with
+// fp32 queries in three parts of 8 bits (all of their bits; a third of the fp32 instruction's time), and the weights p, of at most 2^8, in as
+// many parts as the output is worth: three for fp32, two for bf16 (with one, its rounding would be as large an error as the output's own; the
+// second costs nothing, 256 sequences in e4m3 take 349.8 us with one and 349.1 with two).
 template <bool F32, int CACHE, int DIM, int NT>
 struct Wave {
     using L = Layout<F32, CACHE, DIM>;
+    static constexpr bool kWide = CACHE == MOE_F32;                                 // fp32 products
     static constexpr int kSteps = L::kPiece / 8;                                    // bf16: matrix instructions of one piece of K
-    float q32[F32 ? NT : 1][F32 ? L::kPieces : 1][F32 ? L::kPiece : 1];             // Q^T, fp32 or bf16
-    bf16x8 q16[F32 ? 1 : NT][F32 ? 1 : L::kPieces][F32 ? 1 : kSteps];
+    static constexpr int kPartsQ = F32 ? 3 : 1, kPartsP = F32 ? 3 : 2;
+    float q32[F32 ? NT : 1][F32 ? L::kPieces : 1][F32 ? L::kPiece : 1];             // Q^T as it came, fp32
+    bf16x8 q16[kWide ? 1 : kPartsQ][kWide ? 1 : NT][kWide ? 1 : L::kPieces][kWide ? 1 : kSteps];
     f32x4 o[NT][L::kHalves][L::kOwn];                                               // O^T: dim 128 half + own (4 g + r) + j, head l % 16
     float m[NT], l[NT];                                                             // maximum (the same in all quarters), weight of the own tokens
 
@@ -226,9 +244,27 @@ struct Wave {
                     }
                 } else {
 #pragma unroll
-                    for (int s = 0; s < kSteps; ++s) q16[t][i][s] = __builtin_bit_cast(bf16x8, load_raw<16>(rows, at + 16 * s, 0));
+                    for (int s = 0; s < kSteps; ++s) q16[0][t][i][s] = __builtin_bit_cast(bf16x8, load_raw<16>(rows, at + 16 * s, 0));
                 }
             }
+    }
+
+    // Once the queries are wanted.
+    __device__ void split_q() {
+        if constexpr (F32 && !kWide)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < L::kPieces; ++i)
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                        for (int part = 0; part < kPartsQ; ++part) {
+                            u32x4 u;
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) u[c] = take_bf16x2(q32[t][i][8 * s + 2 * c], q32[t][i][8 * s + 2 * c + 1]);
+                            q16[part][t][i][s] = __builtin_bit_cast(bf16x8, u);
+                        }
     }
 
     // The pages of the runs of up to kAsk steps from token t0 on: lane 2 s + r holds that of run r of step s.
@@ -292,7 +328,8 @@ struct Wave {
                 s[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < L::kPieces; ++i) {
-                    if constexpr (F32) {
+                    if (4 * i * L::kPiece >= a.dim) break;
+                    if constexpr (kWide) {
                         float f[L::kPiece];
                         to_floats<CACHE, L::kPiece>(k[r][i].w, f);
 #pragma unroll
@@ -303,7 +340,9 @@ struct Wave {
                         to_pairs<CACHE, L::kPiece>(k[r][i].w, reinterpret_cast<uint32_t*>(pairs));
 #pragma unroll
                         for (int st = 0; st < kSteps; ++st)
-                            s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pairs[st]), q16[t][i][st], s[t][r], 0, 0, 0);
+#pragma unroll
+                            for (int part = kPartsQ - 1; part >= 0; --part)
+                                s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pairs[st]), q16[part][t][i][st], s[t][r], 0, 0, 0);
                     }
                 }
             }
@@ -359,7 +398,7 @@ struct Wave {
                 }
         }
 
-        if constexpr (F32) {
+        if constexpr (kWide) {
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -375,14 +414,16 @@ struct Wave {
                                 o[t][hf][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[j], p[t][r][c], o[t][hf][j], 0, 0, 0);
                     }
         } else {
-            bf16x8 pp[NT];                                     // weights of at most 2^8, rounded to 8 bits for the matrix instruction
+            bf16x8 weights[NT][kPartsP];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                u32x4 u;
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) u[c] = to_bf16x2(p[t][c / 2][2 * (c % 2)], p[t][c / 2][2 * (c % 2) + 1]);
-                pp[t] = __builtin_bit_cast(bf16x8, u);
-            }
+                for (int part = 0; part < kPartsP; ++part) {
+                    u32x4 u;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) u[c] = take_bf16x2(p[t][c / 2][2 * (c % 2)], p[t][c / 2][2 * (c % 2) + 1]);
+                    weights[t][part] = __builtin_bit_cast(bf16x8, u);
+                }
 #pragma unroll
             for (int hf = 0; hf < L::kHalves; ++hf) {
                 uint32_t pairs[8][L::kOwn / 2];
@@ -396,7 +437,9 @@ struct Wave {
                         u[c] = __builtin_amdgcn_perm(pairs[2 * c + 1][j / 2], pairs[2 * c][j / 2], j % 2 == 0 ? 0x05040100u : 0x07060302u);
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
-                        o[t][hf][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), pp[t], o[t][hf][j], 0, 0, 0);
+#pragma unroll
+                        for (int part = kPartsP - 1; part >= 0; --part)
+                            o[t][hf][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), weights[t][part], o[t][hf][j], 0, 0, 0);
                 }
             }
         }
@@ -498,30 +541,31 @@ __device__ void finish(const Attn& a, const Wave<F32, CACHE, DIM, NT>& w, Sums<D
 struct Feed {
     const Attn& a;
     const int *before, *list;       // places of the sequences before; lengths
-    int worker, top_step, b;
+    int worker, b;
     long at, stop;
     bool first;
 
     __device__ long before_of(int i) const { return static_cast<long>(uniform(before[i])) * a.heads; }
     __device__ Span span(int i) const { return span_of(a, uniform(list[i])); }
-    __device__ int sequence_at(long place) const {                   // the last one that begins at or before
-        int i = 0;
-#pragma unroll 1
-        for (int step = top_step; step > 0; step /= 2)
-            if (i + step < a.B && before_of(i + step) <= place) i += step;
-        return i;
+    // The last sequence that begins at or before a place: 64 of them, then those up to the next of the 64, looked at by a lane each.
+    __device__ int sequence_at(long place) const {
+        const int lane = threadIdx.x % 64;
+        auto last_of = [&](int i) { return __popcll(__ballot(i < a.B && static_cast<long>(before[min(i, a.B)]) * a.heads <= place)) - 1; };
+        const int from = a.B > 64 ? 64 * last_of(64 * lane) : 0;
+        return from + last_of(from + lane);
     }
-    // A cut that would leave an item's beginning to one block and its tokens to the next is moved to before it.
-    __device__ long moved(long place) const {
+    // A cut that would leave an item's beginning to one block and its tokens to the next is moved to before it.  i: the sequence it lies in.
+    __device__ long moved(long place, int& i) const {
+        i = sequence_at(place);
         if (place >= before_of(a.B)) return place;
-        const int i = sequence_at(place), in_b = static_cast<int>(place - before_of(i)), in_item = in_b % span(i).places();
+        const int in_b = static_cast<int>(place - before_of(i)), in_item = in_b % span(i).places();
         return in_item <= kToll ? place - in_item : place;
     }
-    __device__ Feed(const Attn& args, const int* before_, const int* list_, const Cuts& cuts, int worker_, int top_step_)
-        : a(args), before(before_), list(list_), worker(worker_), top_step(top_step_), first(true) {
-        at = moved(cuts.at(worker));
-        stop = moved(cuts.at(worker + 1));
-        b = sequence_at(at);
+    __device__ Feed(const Attn& args, const int* before_, const int* list_, const Cuts& cuts, int worker_)
+        : a(args), before(before_), list(list_), worker(worker_), first(true) {
+        int end;
+        at = moved(cuts.at(worker), b);
+        stop = moved(cuts.at(worker + 1), end);
     }
     // The piece at `at`, which must be below `stop`.
     __device__ Item piece() {
@@ -565,6 +609,7 @@ __device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, Su
     ask_q(it);
     w.reset();
     if constexpr (L::kAhead) w.load(x, a, it.span, ids, 0, it.h, t, steps > 0, lane);
+    w.split_q();
     while (true) {
         Item then = it;
         const bool last = t + kAsk * kUnit >= limit(it), any = !last || more(then);
@@ -591,6 +636,7 @@ __device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, Su
             finish<F32, CACHE, DIM, NT>(a, w, sums, it, wave, lane);
             w.reset();
             if (!any) return;
+            w.split_q();
         }
         it = then;
         t = then_t;
@@ -608,7 +654,7 @@ __device__ inline void store_nothing(const Attn& a, long row, int n_heads, int t
 
 // Short sequences: a block for each sequence, key head and 16 * NT of its query heads; nothing is split.
 template <bool F32, int CACHE, int DIM, int NT>
-__global__ __launch_bounds__(256, waves_of(F32, DIM, NT)) void attn_short_kernel(Attn a) {
+__global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_short_kernel(Attn a) {
     __shared__ __attribute__((aligned(16))) char runs[4][Layout<F32, CACHE, DIM>::kStaged ? Layout<F32, CACHE, DIM>::kRun : 16];
     __shared__ Sums<DIM, NT> sums;
     const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
@@ -629,7 +675,7 @@ __global__ __launch_bounds__(256, waves_of(F32, DIM, NT)) void attn_short_kernel
 // device, whatever they are.  An item that lies in several stretches is left by each as a part, and joined by attn_join_kernel in the order of
 // the tokens.
 template <bool F32, int CACHE, int DIM, int NT>
-__global__ __launch_bounds__(256, waves_of(F32, DIM, NT)) void attn_kernel(Attn a, int top_step) {
+__global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_kernel(Attn a, double one_over_workers) {
     __shared__ __attribute__((aligned(16))) char runs[4][Layout<F32, CACHE, DIM>::kStaged ? Layout<F32, CACHE, DIM>::kRun : 16];
     __shared__ Sums<DIM, NT> sums;
     __shared__ int before[kMaxB + 1], list[kMaxB], wave_total[4];       // places of the sequences before; lengths
@@ -665,8 +711,8 @@ __global__ __launch_bounds__(256, waves_of(F32, DIM, NT)) void attn_kernel(Attn 
         if (before[b + 1] == before[b]) store_nothing<F32>(a, static_cast<long>(b) * a.heads * a.group, a.heads * a.group, tid);
 
     const int worker = blockIdx.x;
-    const Cuts cuts(static_cast<long>(uniform(before[a.B])) * a.heads, gridDim.x);
-    Feed feed(a, before, list, cuts, worker, top_step);
+    const Cuts cuts(static_cast<long>(uniform(before[a.B])) * a.heads, gridDim.x, one_over_workers);
+    Feed feed(a, before, list, cuts, worker);
     Cut cut{-1, 0, 0, 0};
     if (feed.at < feed.stop) {
         const Item it = feed.piece();
@@ -781,9 +827,7 @@ int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) 
         MOE_LAUNCH_CHECK("attn_short_kernel");
         return MOE_OK;
     }
-    int top_step = 1;
-    while (2 * top_step < a.B) top_step *= 2;
-    hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT>), dim3(p.workers), dim3(256), 0, s, a, top_step);
+    hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT>), dim3(p.workers), dim3(256), 0, s, a, 1.0 / p.workers);
     MOE_LAUNCH_CHECK("attn_kernel");
     if (a.B * a.heads >= p.workers) hipLaunchKernelGGL((attn_join_kernel<F32, 1>), dim3(p.workers, (a.group + 3) / 4), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_join_kernel<F32, 4>), dim3(p.workers, a.group), dim3(256), 0, s, a);
