@@ -374,8 +374,8 @@ int moe_kv_read(const moe_kv_cfg* cfg, int32_t n, const void* k_pages, const voi
  * j / (q_heads / heads), to the last `window` (0: all) of the sequence's first lens[b] tokens:
  *     l_t = scale * q . k_t,   out = sum_t exp(l_t) v_t / sum_t exp(l_t),   lse = log sum_t exp(l_t).
  * The cache is read once, its length split over the whole device and the parts joined; what lies beyond lens[b] or before the window
- * is not looked at, whatever it is.  Sums and statistics are fp32; with dtype MOE_BF16 the weights exp(l_t) enter the sum rounded to
- * bf16.  lens[b] = 0: out 0 and lse -infinity.
+ * is not looked at, whatever it is.  Sums and statistics are fp32; with dtype MOE_BF16 the weights exp(l_t) enter the sum with 16
+ * bits.  lens[b] = 0, or all l_t of a head -infinity: out 0 and lse -infinity.
  *   q: device, dtype, sequence b's [q_heads, head_dim] at element b * q_stride.  out [B, q_heads, head_dim]: dtype, written.
  *   table [B, table_pages] int32: device, the sequences' pages (only those of attended tokens are read; a page outside of
  *   [0, pages) is taken as the nearest one that exists).  lens [B] int32: device, taken as within [0, table_pages * page_size].

@@ -86,9 +86,9 @@ int moe_add_norm(const moe_norm_cfg* cfg, const void* x, const void* residual, c
                  float* q_scale, void* stream) {
     if (int rc = check_norm(cfg)) return rc;
     REQUIRE(weight, "weight"); REQUIRE_ALIGNED(weight, "weight");
+    if (cfg->T == 0) return MOE_OK;                                   // arrays without rows have no address
     if (y == nullptr && q == nullptr) return fail(MOE_ERR_INVALID_ARG, "y and q are both NULL");
     if ((q == nullptr) != (q_scale == nullptr)) return fail(MOE_ERR_INVALID_ARG, "q and q_scale go together");
-    if (cfg->T == 0) return MOE_OK;
     REQUIRE(x, "x"); REQUIRE_ALIGNED(x, "x");
     REQUIRE_ALIGNED(residual, "residual"); REQUIRE_ALIGNED(sum, "sum"); REQUIRE_ALIGNED(y, "y"); REQUIRE_ALIGNED(q, "q"); REQUIRE_ALIGNED(q_scale, "q_scale");
     return launch_add_norm(*cfg, x, residual, weight, sum, y, q, q_scale, static_cast<hipStream_t>(stream));

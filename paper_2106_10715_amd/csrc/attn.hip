@@ -508,7 +508,7 @@ __device__ void finish(const Attn& a, const Wave<F32, CACHE, DIM, NT>& w, Sums<D
                     continue;
                 }
                 const long at = (head0 + c) * a.dim + 128 * hf + 4 * col;
-                const float inv = 1.f / weight;
+                const float inv = weight == 0.f ? 0.f : 1.f / weight;         // logits of -infinity alone: as if there were no tokens
                 if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = v * inv;
                 else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = u32x2{to_bf16x2(v[0] * inv, v[1] * inv), to_bf16x2(v[2] * inv, v[3] * inv)};
                 if (hf == 0 && col == 0 && a.lse != nullptr) a.lse[head0 + c] = natural_log_of_sum(top, weight);
@@ -760,7 +760,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a) {
     }
     if (mine == 0)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) store_out<F32>(a, head * a.dim + 4 * col + c, v[c] / weight);
+        for (int c = 0; c < 4; ++c) store_out<F32>(a, head * a.dim + 4 * col + c, weight == 0.f ? 0.f : v[c] / weight);
 }
 
 // How a call is cut.  Sequences of at most kShortUnits units are not split: a block for each item.  Else the list of units is cut into a

@@ -44,7 +44,7 @@ def test_workspace_grows_with_what_is_split():
     assert all(size(**kw) % 256 == 0 and size(**kw) >= 256 for kw in (dict(), dict(B=0), dict(B=4096, table_pages=1), dict(window=1)))
     assert size(table_pages=1) <= size(table_pages=100) <= size()                 # short sequences are not split
     assert size(q_heads=2) < size() < size(q_heads=1024)
-    parts = min(3 * 2 * 125, 512)                                                 # blocks that each may leave two parts of a head's group
+    parts = min(3 * 2 * 125, 256)                                                 # blocks that each may leave two parts of a head's group
     assert size() >= 2 * parts * 16 * (64 + 2) * 4
 
 
@@ -171,3 +171,13 @@ def test_binding_refuses_tensors_of_another_size_type_or_layout():
         M.moe_attn_decode(kv, attn, b(2, 4, 32), k, v, None, None, slots, slots, None, None, None)
     with pytest.raises(M.MoeError, match="ws is smaller"):
         M.moe_attn_decode(kv, attn, None, k, v, None, None, slots, slots, None, None, b(16))
+
+
+def test_no_rows_no_tokens_no_sequences_is_no_error():
+    """Tensors without elements have no address: that is no missing argument."""
+    L = M.lib()
+    buf = C.create_string_buffer(64 * 2 + 16)
+    weight = (C.addressof(buf) + 15) & ~15
+    none = torch.empty((0, 64), dtype=torch.bfloat16).data_ptr()
+    assert L.moe_add_norm(C.addressof(M.NormCfg.make(0, 64)), none, none, weight, none, none, None, None, None) == 0
+    assert L.moe_add_norm(C.addressof(M.NormCfg.make(0, 64)), none, none, weight, none, None, none, none, None) == 0

@@ -362,6 +362,39 @@ def test_attention_scale_no_lse_and_not_finite_values_that_count():
     assert torch.isfinite(shorter).all()
 
 
+@pytest.mark.parametrize("n", [20, 5000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_to_logits_of_minus_infinity(n, dtype):
+    """Tokens whose logit is -infinity weigh nothing; a head with no other tokens is as one without tokens (one launch, and split)."""
+    cfg = M.KvCfg.make(-(-n // 16), 16, 2, 64, dtype)
+    table = tables(6, 1, cfg.pages, cfg.pages)
+    arrays = cache_of(64, cfg, table, [n])
+    q = normal(66, (1, 4, 64), dtype).abs()
+    at = torch.arange(n)
+    place = (table[0][at // 16].long(), at % 16)
+    arrays[0][place[0], 0, place[1], 0] = -math.inf                             # key head 0: all tokens
+    arrays[0][place[0][7:], 1, place[1][7:], 63] = -math.inf                    # key head 1: all from the eighth on
+    out, lse = run_attention(cfg, arrays, q, table.cuda(), [n])
+    assert (out[0, :2] == 0).all() and (lse[0, :2] == -math.inf).all()
+    want, want_lse = run_attention(cfg, arrays, q, table.cuda(), [7])
+    tol = 2 * HALF[dtype] if dtype == "bf16" else 2.0 ** -18                    # the same seven weights in sums of another order
+    within(f64(out[0, 2:]), f64(want[0, 2:]), tol * (f64(want[0, 2:]).__abs__() + 4), "seven tokens")
+    assert torch.allclose(lse[0, 2:], want_lse[0, 2:], atol=2.0 ** -20)
+
+
+def test_empty_calls_through_the_binding():
+    x = torch.empty((0, 64), dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    M.moe_add_norm(M.NormCfg.make(0, 64), x, x, w, x, x)
+    cfg = M.KvCfg.make(2, 16, 1, 64)
+    arrays, rows, slots = cfg.empty(), x.view(0, 1, 64), torch.empty(0, dtype=torch.int32, device="cuda")
+    M.moe_kv_write(cfg, rows, rows, slots, *arrays)
+    M.moe_kv_read(cfg, *arrays, slots, rows, rows)
+    attn = M.AttnCfg.make(0, 2, 2)
+    ws = torch.empty(M.moe_attn_workspace_bytes(cfg, attn), dtype=torch.uint8, device="cuda")
+    M.moe_attn_decode(cfg, attn, rows.expand(0, 2, 64), *arrays, slots.view(0, 2), slots, rows.expand(0, 2, 64), None, ws)
+
+
 # ------------------------------------------------------------------------------------------- together
 
 def test_calls_on_another_stream_and_in_a_graph():
