@@ -12,6 +12,8 @@ _TORCH = {MOE_F32: torch.float32, MOE_BF16: torch.bfloat16, MOE_E4M3: torch.floa
 _CODE = {"f32": MOE_F32, "bf16": MOE_BF16, "e4m3": MOE_E4M3}
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB: Optional[C.CDLL] = None
+_ARGS = None
+_FN = {}            # addresses of the library's functions for _args, the marshalling in C++ of the calls that are over in microseconds
 
 
 class MoeError(RuntimeError):
@@ -132,6 +134,7 @@ def lib() -> C.CDLL:
             fn = getattr(L, name)
             fn.restype = C.c_int
             fn.argtypes = args
+            _FN[name] = C.cast(fn, p).value
         _LIB = L
     return _LIB
 
@@ -155,6 +158,23 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda de
 
 def _stream(stream: Optional[torch.cuda.Stream]):
     return stream.cuda_stream if stream is not None else _raw_stream(torch.cuda.current_device())
+
+
+def _native(name: str, *args, stream=None) -> bool:
+    """The call through _args.  False where an argument is not as it has to be, which the caller's own checks then explain."""
+    global _ARGS
+    if _LIB is None or _ARGS is None:
+        lib()
+        try:
+            from . import _args
+        except ImportError as e:
+            raise MoeError(f"_args is not built: run python -m paper_2106_10715_amd.build ({e})")
+        _ARGS = _args
+    rc = getattr(_ARGS, name)(_FN["moe_" + name], _FN["moe_attn_workspace_bytes"], *args, None if stream is None else stream.cuda_stream)
+    if rc is None:
+        return False
+    _check(rc)
+    return True
 
 
 def moe_workspace_bytes(cfg: MoeCfg) -> int:
@@ -372,6 +392,8 @@ def _head_rows(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int,
 
 
 def moe_add_norm(cfg: NormCfg, x, residual, weight, sum, y, q=None, q_scale=None, stream=None) -> None:
+    if _native("add_norm", cfg, x, residual, weight, sum, y, q, q_scale, stream=stream):
+        return
     dt, n = _TORCH.get(cfg.dtype), cfg.T * cfg.d
     groups = cfg.T * (cfg.d // cfg.q_group if cfg.q_group > 0 else 1)
     _check(lib().moe_add_norm(C.addressof(cfg), _array(x, "x", dt, n), _array(residual, "residual", dt, n),
@@ -387,6 +409,8 @@ def _cache(cfg: KvCfg, k_pages, v_pages, k_scales, v_scales):
 
 
 def moe_kv_write(cfg: KvCfg, k, v, slots, k_pages, v_pages, k_scales=None, v_scales=None, stream=None) -> None:
+    if _native("kv_write", cfg, k, v, slots, k_pages, v_pages, k_scales, v_scales, stream=stream):
+        return
     n, dt = slots.numel(), _TORCH.get(cfg.dtype)
     kp, ks = _head_rows(k, "k", dt, n, cfg.heads, cfg.head_dim)
     vp, vs = _head_rows(v, "v", dt, n, cfg.heads, cfg.head_dim)
@@ -395,6 +419,8 @@ def moe_kv_write(cfg: KvCfg, k, v, slots, k_pages, v_pages, k_scales=None, v_sca
 
 
 def moe_kv_read(cfg: KvCfg, k_pages, v_pages, k_scales, v_scales, slots, k, v, stream=None) -> None:
+    if _native("kv_read", cfg, k_pages, v_pages, k_scales, v_scales, slots, k, v, stream=stream):
+        return
     n, dt = slots.numel(), _TORCH.get(cfg.dtype)
     kp, ks = _head_rows(k, "k", dt, n, cfg.heads, cfg.head_dim)
     vp, vs = _head_rows(v, "v", dt, n, cfg.heads, cfg.head_dim)
@@ -409,6 +435,9 @@ def moe_attn_workspace_bytes(cfg: KvCfg, attn: AttnCfg) -> int:
 
 
 def moe_attn_decode(cfg: KvCfg, attn: AttnCfg, q, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws, stream=None) -> None:
+    if _native("attn_decode", cfg, attn, q, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws,
+               stream=stream):
+        return
     B, heads, dt = attn.B, attn.q_heads, _TORCH.get(cfg.dtype)
     qp, qs = _head_rows(q, "q", dt, B, heads, cfg.head_dim)
     if ws is not None and ws.nbytes < moe_attn_workspace_bytes(cfg, attn):

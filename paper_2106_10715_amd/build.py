@@ -1,16 +1,18 @@
-"""Builds libmoe355.so (all HIP sources, gfx950) next to this file with hipcc."""
+"""Builds libmoe355.so (all HIP sources, gfx950) next to this file with hipcc, and _args.so, the binding's marshalling, with g++."""
 from __future__ import annotations
 
 import os
 import re
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe355.so")
+ARGS = os.path.join(HERE, "_args.so")
 SOURCES = ["api.hip", "route.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "combine.hip", "schedule.hip",
            "api_decoder.hip", "norm.hip", "kv.hip", "attn.hip"]
 # ffn.hip is compiled in parts, side by side: each of its large kernels is an object of its own.
@@ -321,10 +323,26 @@ def _compile(src: str, part: int) -> str:
     return obj
 
 
+def _compile_args() -> None:
+    """The binding's marshalling, host code against torch's headers."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+           "-isystem", os.path.join(at, "include"), "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+           "-isystem", "/opt/rocm/include",
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "args.cpp"), "-o", ARGS,
+           "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed on args.cpp:\n" + r.stderr)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
     with ThreadPoolExecutor(max_workers=8) as pool:
         checks = [pool.submit(_check, src, part) for src, part in UNITS if src in NO_SPILL]
+        checks.append(pool.submit(_compile_args))
         objs = list(pool.map(lambda u: _compile(*u), UNITS))
         for c in checks:
             c.result()
