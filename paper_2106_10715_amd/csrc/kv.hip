@@ -80,15 +80,20 @@ __device__ inline void store_eight(Eight<TYPE>* p, const Eight<TYPE>& e) {
 // A row (token, head) is held by LANES lanes with eight elements each.  Bound by memory.  Where rows are quantised, the wait for a row's
 // maximum is made worth two rows: the same lanes take its key and its value, both requested before either is used (16384 tokens of 8 x 128:
 // 17.8 us, 19.8 with a block for each).  Else half of the blocks take the keys, half the values (32768 tokens of 64 x 64 read: 193 us, 204
-// with both in the same lanes).  STREAM 1: non-temporal stores, 2: loads too.
+// with both in the same lanes).  Rows go by runs of four tokens, in a run by head: a token's rows lie together in the plain array, the rows
+// of tokens that follow one another in the pages (32768 tokens of 64 x 64 read: 184 us, 190 token by token; 16384 written: 90, 92.5; runs of
+// 2 to 16 are within 4 % of this, of 32 up to 10 % slower).  STREAM 1: non-temporal stores, 2: loads too.
+constexpr int kRun = 4;
 template <int TYPE, int CACHE, int LANES, bool WRITE, int STREAM>
 __global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* __restrict__ slots, int n, int heads, int eights,
                                                  int page_bits, int n_slots) {
     constexpr int kSides = WRITE && CACHE == MOE_E4M3 ? 2 : 1;
     const int lane = threadIdx.x % LANES;
-    const long total = static_cast<long>(n) * heads, step = static_cast<long>(gridDim.x) * (256 / LANES);
+    const long total = (static_cast<long>(n) + kRun - 1) / kRun * kRun * heads, step = static_cast<long>(gridDim.x) * (256 / LANES);
     for (long row = static_cast<long>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES; row < total; row += step) {
-        const int token = static_cast<int>(row / heads), head = static_cast<int>(row - static_cast<long>(token) * heads);
+        const long pair = row / kRun, run = pair / heads, token = run * kRun + row % kRun;
+        const int head = static_cast<int>(pair - run * heads);
+        if (token >= n) continue;
         const int slot = slots[token];
         const bool there = slot >= 0 && slot < n_slots;          // others are nowhere: not written, read as zeros
         if (WRITE && !there) continue;
@@ -155,7 +160,7 @@ __global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* 
 template <int TYPE, int CACHE, bool WRITE, int STREAM>
 void launch(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int32_t* slots, hipStream_t s) {
     const int eights = c.head_dim / 8, bits = __builtin_ctz(c.page_size);
-    const long rows = static_cast<long>(n) * c.heads;
+    const long rows = (static_cast<long>(n) + kRun - 1) / kRun * kRun * c.heads;
     auto run = [&](auto kernel, int lanes) {
         const long blocks = (rows + 256 / lanes - 1) / (256 / lanes), most = 1 << 20;     // one row per group of lanes, up to many millions of rows
         hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most), WRITE && CACHE == MOE_E4M3 ? 1 : 2), dim3(256), 0, s, k, v, slots, n, c.heads, eights,
@@ -166,16 +171,21 @@ void launch(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int3
     else run(kv_kernel<TYPE, CACHE, 32, WRITE, STREAM>, 32);
 }
 
-// What is more than the caches hold does better without them.  us through the caches / non-temporal stores / loads too, 16 heads of 128, bf16:
-// writes of 4096 tokens (67 MB) 11.2 / 11.3 / 13.1, 8192 (134 MB) 26.3 / 20.3 / 23.4, 16384 (268 MB) 47.7 / 45.7 / 44.4; reads with a kernel
-// behind them that uses the rows: 8192 45.0 / 46.6 / 46.6, 16384 103.2 / 97.4 / 86.5.
+// What is more than the caches hold does better without them.  us through the caches / non-temporal stores / loads too (in brackets with a
+// kernel behind them that adds k and v), heads of 128, bf16:
+//   writes to bf16, 16 heads:   4096 tokens (67 MB) 11.2 / 11.3 / 13.1, 8192 (134 MB) 26.3 / 20.3 / 23.4, 16384 (268 MB) 47.7 / 45.7 / 44.4
+//   reads from bf16, 16 heads:  4096 12.0 (20.4) / 11.7 (22.0) / 13.5 (24.0), 8192 26.3 (43.0) / 20.7 (44.5) / 24.3 (42.8),
+//                               32768 (537 MB) 93.5 (159.9) / 89.7 (157.2) / 87.6 (157.5); fp32 as large: 95.2 / 95.0 / 101.6
+//   reads from e4m3, 8 heads:   4096 (25 MB) 7.2 (12.3) / 5.7 (12.2) / 7.5 (14.3), 16384 (102 MB) 26.5 (41.9) / 17.7 (43.4) / 24.2 (42.5),
+//                               100000 (621 MB) 149.8 (257.9) / 138.0 (240.3) / 136.6 (239.9)
 template <int TYPE, int CACHE, bool WRITE>
 int launch_for_size(const moe_kv_cfg& c, int n, const Side& k, const Side& v, const int32_t* slots, hipStream_t s) {
     const size_t each = 2 * static_cast<size_t>(n) * c.heads * c.head_dim;
     const size_t moved = each * ((TYPE == MOE_F32 ? 4 : 2) + (CACHE == MOE_F32 ? 4 : CACHE == MOE_BF16 ? 2 : 1));
-    if (moved > size_t(200) << 20) launch<TYPE, CACHE, WRITE, 2>(c, n, k, v, slots, s);
-    else if (WRITE && moved > size_t(80) << 20) launch<TYPE, CACHE, WRITE, WRITE ? 1 : 0>(c, n, k, v, slots, s);
-    else launch<TYPE, CACHE, WRITE, 0>(c, n, k, v, slots, s);
+    constexpr bool kLoadsToo = WRITE || TYPE == MOE_BF16, kAlways = !WRITE && CACHE == MOE_E4M3;
+    if (kLoadsToo && moved > size_t(WRITE ? 200 : 320) << 20) launch<TYPE, CACHE, WRITE, kLoadsToo ? 2 : 1>(c, n, k, v, slots, s);
+    else if (kAlways || moved > size_t(80) << 20) launch<TYPE, CACHE, WRITE, 1>(c, n, k, v, slots, s);
+    else launch<TYPE, CACHE, WRITE, kAlways ? 1 : 0>(c, n, k, v, slots, s);
     MOE_LAUNCH_CHECK("kv_kernel");
     return MOE_OK;
 }
