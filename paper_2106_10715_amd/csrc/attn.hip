@@ -28,11 +28,12 @@ constexpr int kAsk = 32;            // steps whose pages a wave looks up at once
 constexpr int kMaxB = 4096;         // sequences
 constexpr float kSlack = 8.f;       // the running maximum is raised only where a logit passes it by more than this (as a power of two)
 
-// An item of the work, a (sequence, key head), cut where a worker's stretch begins: written by that worker, for the join.
+// An item of the work, a (sequence, key head, 16 * NT of its query heads), cut where a worker's stretch begins: written by that worker, for
+// the join.
 struct Cut {
-    int rows;                       // its first query head's row of out and lse; -1: nothing is cut here, or not for the first time
+    int rows;                       // its key head's first row of out and lse; -1: nothing is cut here, or not for the first time
     int first, last;                // slot of its first part, worker of its last (in between: the slots 2 w)
-    int pad;
+    int in_group;                   // its first query head in the key head's group
 };
 
 struct Attn {
@@ -45,7 +46,7 @@ struct Attn {
     float* lse;
     float *part_o, *part_ml;        // [workers][2][group][dim], [workers][2][group][2]: unscaled sums; their maximum and weight
     Cut* cuts;                      // [workers]
-    int B, heads, group, chunks, dim, pages, page_bits, table_pages, window;
+    int B, heads, group, chunks, items, item_rows, dim, pages, page_bits, table_pages, window;
     float scale;                    // times log2 e
 };
 
@@ -517,7 +518,7 @@ __device__ void finish(const Attn& a, const Wave<F32, CACHE, DIM, NT>& w, Sums<D
         }
 }
 
-// The items a block works on, one after the other: the chunks of query heads of each (sequence, key head) in its stretch.
+// The items a block works on, one after the other.
 struct Feed {
     const Attn& a;
     const int *before, *list;       // places of the sequences before; lengths
@@ -525,12 +526,12 @@ struct Feed {
     long at, stop;
     bool first;
 
-    __device__ long before_of(int i) const { return static_cast<long>(uniform(before[i])) * a.heads; }
+    __device__ long before_of(int i) const { return static_cast<long>(uniform(before[i])) * a.items; }
     __device__ Span span(int i) const { return span_of(a, uniform(list[i])); }
     // The last sequence that begins at or before a place: 64 of them, then those up to the next of the 64, looked at by a lane each.
     __device__ int sequence_at(long place) const {
         const int lane = threadIdx.x % 64;
-        auto last_of = [&](int i) { return __popcll(__ballot(i < a.B && static_cast<long>(before[min(i, a.B)]) * a.heads <= place)) - 1; };
+        auto last_of = [&](int i) { return __popcll(__ballot(i < a.B && static_cast<long>(before[min(i, a.B)]) * a.items <= place)) - 1; };
         const int from = a.B > 64 ? 64 * last_of(64 * lane) : 0;
         return from + last_of(from + lane);
     }
@@ -552,21 +553,17 @@ struct Feed {
         while (before_of(b + 1) <= at) ++b;
         Item it;
         it.b = b;
-        it.chunk = 0;
         it.span = span(b);
-        const int in_b = static_cast<int>(at - before_of(b)), places = it.span.places();       // (below heads * places < 2^28)
-        it.h = in_b / places;
-        const int in_item = in_b - it.h * places;
+        const int in_b = static_cast<int>(at - before_of(b)), places = it.span.places();       // (below items * places < 2^28)
+        const int item = in_b / places, in_item = in_b - item * places;
+        it.h = item / a.chunks;
+        it.chunk = item - it.h * a.chunks;
         it.u0 = max(0, in_item - kToll);
         it.u1 = static_cast<int>(min(static_cast<long>(places), in_item + (stop - at))) - kToll;
         it.slot = it.u0 == 0 && it.u1 == it.span.units ? -1 : 2L * worker + (first ? 0 : 1);
         return it;
     }
     __device__ bool next(Item& it) {
-        if (it.chunk + 1 < a.chunks) {
-            ++it.chunk;
-            return true;
-        }
         at += it.u1 - it.u0 + (it.u0 == 0 ? kToll : 0);
         first = false;
         if (at >= stop) return false;
@@ -651,7 +648,7 @@ __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_short
     work<F32, CACHE, DIM, NT>(a, w, runs[wave], sums, it, [](Item&) { return false; }, wave, lane);
 }
 
-// The work is the list of all (sequence, key head, unit of tokens); every block takes an equal stretch of it, found from the lengths on the
+// The work is the list of all (sequence, key head, 16 * NT of its query heads, unit of tokens); every block takes an equal stretch of it, found from the lengths on the
 // device, whatever they are.  An item that lies in several stretches is left by each as a part, and joined by attn_join_kernel in the order of
 // the tokens.
 template <bool F32, int CACHE, int DIM, int NT>
@@ -691,14 +688,14 @@ __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_kerne
         if (before[b + 1] == before[b]) store_nothing<F32>(a, static_cast<long>(b) * a.heads * a.group, a.heads * a.group, tid);
 
     const int worker = blockIdx.x;
-    const Cuts cuts(static_cast<long>(uniform(before[a.B])) * a.heads, gridDim.x, one_over_workers);
+    const Cuts cuts(static_cast<long>(uniform(before[a.B])) * a.items, gridDim.x, one_over_workers);
     Feed feed(a, before, list, cuts, worker);
     Cut cut{-1, 0, 0, 0};
     if (feed.at < feed.stop) {
         const Item it = feed.piece();
         const long start = feed.at - it.u0 - kToll, left = cuts.at(worker - 1);
         if (it.u0 > 0 && left <= start + kToll)                       // begun in the stretch before
-            cut = Cut{(it.b * a.heads + it.h) * a.group, 2 * (worker - 1) + (left >= start ? 0 : 1), cuts.of(start + it.span.units + kToll - 1), 0};
+            cut = Cut{(it.b * a.heads + it.h) * a.group, 2 * (worker - 1) + (left >= start ? 0 : 1), cuts.of(start + it.span.units + kToll - 1), 16 * NT * it.chunk};
         if (tid == 0) a.cuts[worker] = cut;
         work<F32, CACHE, DIM, NT>(a, w, runs[wave], sums, it, [&](Item& i) { return feed.next(i); }, wave, lane);
     } else if (tid == 0) {
@@ -713,9 +710,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a) {
     __shared__ f32x4 sums[TEAM == 4 ? 256 : 1];
     constexpr int kLanes = 64 * TEAM, kAhead = 8;
     const int w = blockIdx.x, tid = threadIdx.x, lane = TEAM == 4 ? tid : tid % 64;
-    const int row = TEAM == 4 ? blockIdx.y : 4 * blockIdx.y + tid / 64;
     const Cut cut = a.cuts[w];
-    if (cut.rows < 0 || row >= a.group) return;
+    const int in_item = TEAM == 4 ? blockIdx.y : 4 * blockIdx.y + tid / 64, row = cut.in_group + in_item;
+    if (cut.rows < 0 || in_item >= a.item_rows || row >= a.group) return;
     const int parts = cut.last - w + 2;
     auto slot_of = [&](int i) { return static_cast<long>(i == 0 ? cut.first : 2 * (w - 1 + i)) * a.group + row; };
     float top = -INFINITY, weight = 0.f;
@@ -770,10 +767,17 @@ struct Plan {
     bool is_short;
     int workers;
 };
+// Matrix columns, in sixteens, that take a key head's query heads.  fp32 products and heads of over 128 have no room for a second sixteen in
+// registers (256 wide in bf16: 185 spilled): larger groups read the cache again for each.
+int columns_of(const moe_kv_cfg& kv, int group) { return kv.dtype == MOE_BF16 && kv.head_dim <= 128 && group > 16 ? 2 : 1; }
+int chunks_of(const moe_kv_cfg& kv, const moe_attn_cfg& c) {
+    const int group = c.q_heads / kv.heads, rows = 16 * columns_of(kv, group);
+    return (group + rows - 1) / rows;
+}
 Plan plan_of(const moe_kv_cfg& kv, const moe_attn_cfg& c, int compute_units) {
     const long room = static_cast<long>(c.table_pages) * kv.page_size;
     const long longest = c.window > 0 ? std::min(room, c.window + 15L) : room, units = (longest + kUnit - 1) / kUnit;
-    const long items = static_cast<long>(c.B) * kv.heads;
+    const long items = static_cast<long>(c.B) * kv.heads * chunks_of(kv, c);
     Plan p;
     p.is_short = units <= kShortUnits;
     // One block per compute unit reads as fast as two and leaves fewer parts; only where heads are narrow and items many does a second one
@@ -801,7 +805,9 @@ int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) 
     const DeviceInfo* info = nullptr;
     if (int rc = device_info(&dev, &info)) return rc;
     const Plan p = plan_of(kv, c, info->compute_units);
-    a.chunks = (a.group + 16 * NT - 1) / (16 * NT);
+    a.chunks = chunks_of(kv, c);
+    a.items = a.heads * a.chunks;
+    a.item_rows = std::min(16 * NT, a.group);
     if (p.is_short) {
         hipLaunchKernelGGL((attn_short_kernel<F32, CACHE, DIM, NT>), dim3(a.B * a.heads * a.chunks), dim3(256), 0, s, a);
         MOE_LAUNCH_CHECK("attn_short_kernel");
@@ -809,17 +815,16 @@ int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) 
     }
     hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT>), dim3(p.workers), dim3(256), 0, s, a, 1.0 / p.workers);
     MOE_LAUNCH_CHECK("attn_kernel");
-    if (a.B * a.heads >= p.workers) hipLaunchKernelGGL((attn_join_kernel<F32, 1>), dim3(p.workers, (a.group + 3) / 4), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_join_kernel<F32, 4>), dim3(p.workers, a.group), dim3(256), 0, s, a);
+    if (a.B * a.items >= p.workers) hipLaunchKernelGGL((attn_join_kernel<F32, 1>), dim3(p.workers, (a.item_rows + 3) / 4), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_join_kernel<F32, 4>), dim3(p.workers, a.item_rows), dim3(256), 0, s, a);
     MOE_LAUNCH_CHECK("attn_join_kernel");
     return MOE_OK;
 }
 
-// fp32 products and heads of over 128 have no room for a second column tile in registers: larger groups read the cache again, 16 heads at a time.
 template <bool F32, int CACHE>
 int for_sizes(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) {
     if constexpr (!F32)
-        if (a.group > 16 && a.dim <= 128) return a.dim <= 64 ? launch<F32, CACHE, 64, 2>(kv, c, a, s) : launch<F32, CACHE, 128, 2>(kv, c, a, s);
+        if (columns_of(kv, a.group) == 2) return a.dim <= 64 ? launch<F32, CACHE, 64, 2>(kv, c, a, s) : launch<F32, CACHE, 128, 2>(kv, c, a, s);
     if (a.dim <= 64) return launch<F32, CACHE, 64, 1>(kv, c, a, s);
     return a.dim <= 128 ? launch<F32, CACHE, 128, 1>(kv, c, a, s) : launch<F32, CACHE, 256, 1>(kv, c, a, s);
 }
@@ -850,7 +855,7 @@ int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* 
     a.B = c.B;
     a.heads = kv.heads;
     a.group = c.q_heads / kv.heads;
-    a.chunks = 0;                                                     // set where the column tiles are chosen
+    a.chunks = a.items = a.item_rows = 0;                             // set where the column tiles are chosen
     a.dim = kv.head_dim;
     a.pages = kv.pages;
     a.page_bits = __builtin_ctz(kv.page_size);
