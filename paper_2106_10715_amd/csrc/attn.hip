@@ -629,7 +629,7 @@ __device__ inline void store_nothing(const Attn& a, long row, int n_heads, int t
     for (int i = tid; i < n_heads && a.lse != nullptr; i += 256) a.lse[row + i] = -INFINITY;
 }
 
-// Short sequences: a block for each sequence, key head and 16 * NT of its query heads; nothing is split.
+// A block for each sequence, key head and 16 * NT of its query heads; nothing is split.
 template <bool F32, int CACHE, int DIM, int NT>
 __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_short_kernel(Attn a) {
     __shared__ __attribute__((aligned(16))) char runs[4][Layout<CACHE, DIM>::kStaged ? Layout<CACHE, DIM>::kRun : 16];
@@ -760,9 +760,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a) {
         for (int c = 0; c < 4; ++c) store_out<F32>(a, head * a.dim + 4 * col + c, weight == 0.f ? 0.f : v[c] / weight);
 }
 
-// How a call is cut.  Sequences of at most kShortUnits units are not split: a block for each item.  Else the list of units is cut into a
-// stretch per block.
-constexpr int kShortUnits = 4, kMaxUnits = 256;
+// How a call is cut: a block for each item, or, where sequences can be longer than `whole_units`, a stretch of the list of units for each block.
+constexpr int kMaxUnits = 256;
 struct Plan {
     bool is_short;
     int workers;
@@ -774,12 +773,25 @@ int chunks_of(const moe_kv_cfg& kv, const moe_attn_cfg& c) {
     const int group = c.q_heads / kv.heads, rows = 16 * columns_of(kv, group);
     return (group + rows - 1) / rows;
 }
+// Units up to which an item is left whole.  A split costs a join and the search for the cuts, 5 to 6 us, and two units per item; a whole item the
+// time of one block alone, per unit 0.8 us (64 wide in bf16) to 1.1 (128 wide) where two tiles are in flight, else 2 to 2.5.  More items than
+// compute units hide each other's waits.  us split / whole, ragged lengths, bf16:
+//   64 heads of 64, bf16 cache:      1 x 1000 12.4 / 10.1, 4 x 2048 19.8 / 17.3, 40 x 2048 117.4 / 113.5, but 1 x 2048 14.6 / 16.1
+//   64 over 8 of 128, e4m3 cache:    16 x 1500 17.7 / 17.5, 64 x 2048 36.0 / 32.8, 200 x 1000 60.0 / 48.8, but 16 x 2048 19.1 / 21.7
+//   32 over 8 of 128, bf16 cache:    4 x 700 11.8 / 11.0, 16 x 1000 16.2 / 14.4, 200 x 1000 77.2 / 73.0, but 4 x 1000 12.3 / 13.3, 16 x 1500 18.3 / 19.2
+//   16 over 2 of 256, bf16 cache:    4 x 700 13.9 / 19.7;   12 over 4 of 80 in fp32: 4 x 700 14.5 / 21.9
+int whole_units(const moe_kv_cfg& kv, long items) {
+    if (kv.dtype == MOE_F32 || kv.head_dim > 128) return 4;
+    const int row_bytes = kv.head_dim * (kv.cache_dtype == MOE_E4M3 ? 1 : 2);
+    if (row_bytes > 128) return items >= 64 ? 8 : 6;
+    return items >= 256 ? 16 : items >= 128 ? 12 : items >= 64 ? 8 : 6;
+}
 Plan plan_of(const moe_kv_cfg& kv, const moe_attn_cfg& c, int compute_units) {
     const long room = static_cast<long>(c.table_pages) * kv.page_size;
     const long longest = c.window > 0 ? std::min(room, c.window + 15L) : room, units = (longest + kUnit - 1) / kUnit;
     const long items = static_cast<long>(c.B) * kv.heads * chunks_of(kv, c);
     Plan p;
-    p.is_short = units <= kShortUnits;
+    p.is_short = units <= whole_units(kv, items);
     // One block per compute unit reads as fast as two and leaves fewer parts; only where heads are narrow and items many does a second one
     // fill the gaps between items (us with one / two: 40 x 1024 tokens, 64 heads of 64: 123 / 104; 1 x 131072, 8 heads of 128: 85 / 88).
     const int per_unit = kv.head_dim <= 64 && items >= 4 * kMaxUnits ? 2 : 1;

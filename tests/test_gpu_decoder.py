@@ -255,7 +255,8 @@ def run_and_check(cfg, arrays, q, table, lens, window=0, scale=0.0, only=None):
             used = torch.unique(table[b, :-(-n // cfg.page_size)].long())
             small = np.zeros(cfg.pages, np.int64)
             small[used.cpu().numpy()] = np.arange(len(used))
-            k, v = (D.paged_rows(f64(t[used]), None, small[tab[b]], first, n) for t in arrays[:2])
+            k, v = (D.paged_rows(f64(t.view(torch.uint8)[used].view(t.dtype)), None if s is None else f64(s[used]), small[tab[b]], first, n)
+                    for t, s in zip(arrays[:2], arrays[2:]))
         else:
             k, v = (D.paged_rows(t, s, tab[b], first, n) for t, s in zip(pages, scales))
         for j in range(heads):
@@ -309,6 +310,26 @@ def test_attention_split_over_long_sequences(B, length, heads, group, dim, page,
     a = run_and_check(cfg, arrays, q, table.cuda(), lens, only=sorted({0, B // 2, B - 1}))
     b = run_attention(cfg, arrays, q, table.cuda(), lens)
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), "two runs differ"
+
+
+@pytest.mark.parametrize("B,heads,group,dim,cache,most", [
+    (1, 3, 2, 64, "bf16", 768), (2, 32, 1, 64, "bf16", 1024), (16, 8, 1, 64, "e4m3", 1536), (4, 64, 1, 64, "bf16", 2048), (32, 8, 8, 128, "e4m3", 2048),
+    (5, 2, 16, 128, "bf16", 768), (16, 4, 4, 128, "bf16", 1024), (3, 1, 40, 128, "bf16", 768), (64, 1, 40, 96, "e4m3", 1536), (2, 1, 20, 256, "bf16", 512)])
+def test_attention_where_sequences_begin_to_be_split(B, heads, group, dim, cache, most):
+    """Tables of the most tokens that a block takes whole, and of one page more: ragged, with a sequence that fills its table and an empty one."""
+    page = 32
+    for room in (most, most + page):
+        per = room // page
+        cfg = M.KvCfg.make(B * per, page, heads, dim, "bf16", cache)
+        attn = M.AttnCfg.make(B, heads * group, per)
+        assert (M.moe_attn_workspace_bytes(cfg, attn) == 256) == (room == most)
+        table = tables(7, B, per, cfg.pages)
+        lens = [room if b == 0 else (room * b * 7) // (B * 7 + 3) % room for b in range(B)]
+        if B > 2:
+            lens[1] = 0
+        arrays = cache_of(34, cfg, table, lens)
+        q = normal(36, (B, heads * group, dim), "bf16", 2.0)
+        run_and_check(cfg, arrays, q, table.cuda(), lens, only=sorted({0, 1 % B, B - 1}))
 
 
 def test_attention_of_as_many_sequences_as_there_may_be():
