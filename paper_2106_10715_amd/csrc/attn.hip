@@ -250,9 +250,9 @@ struct Wave {
                         }
     }
 
-    // The pages of the runs of up to kAsk steps from token t0 on: lane 2 s + r holds that of run r of step s.
-    __device__ static int pages_of(const Attn& a, const Span& span, int b, int t0, int lane) {
-        const int t = min(t0 + (lane / 2) * kUnit + 16 * (lane % 2), (span.end - 1) & ~15);        // (past the end: a run that exists)
+    // The pages of the runs of up to kAsk steps from token t0 on: lane 2 s + r holds that of run r of step s, `tokens` from step to step.
+    __device__ static int pages_of(const Attn& a, const Span& span, int b, int t0, int lane, int tokens) {
+        const int t = min(t0 + (lane / 2) * tokens + 16 * (lane % 2), (span.end - 1) & ~15);        // (past the end: a run that exists)
         return a.table[static_cast<long>(b) * a.table_pages + (t >> a.page_bits)];
     }
 
@@ -573,44 +573,46 @@ struct Feed {
 };
 
 // Works through items, `more` saying which comes next.  A wave has two tiles on the way while it attends to a third (kAhead), the next
-// item's first ones among them, so that what an item's end costs is its barriers and not the memory's answer.
-template <bool F32, int CACHE, int DIM, int NT, typename More>
-__device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, Sums<DIM, NT>& sums, Item it, More more, int wave, int lane) {
+// item's first ones among them, so that what an item's end costs is its barriers and not the memory's answer.  TEAM waves share an item's tokens, `wave` this one's number;
+// `end(item)` stores what they have found.
+template <int TEAM, bool F32, int CACHE, int DIM, int NT, typename More, typename End>
+__device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, Item it, More more, End end, int wave, int lane) {
     using L = Layout<CACHE, DIM>;
+    constexpr int kStep = 32 * TEAM;
     typename Wave<F32, CACHE, DIM, NT>::Tile x, y;
     auto begin = [&](const Item& i) { return i.span.base + i.u0 * kUnit + 32 * wave; };
     auto limit = [&](const Item& i) { return min(i.span.end, i.span.base + i.u1 * kUnit); };
-    auto steps_from = [&](const Item& i, int t) { return max(0, min(kAsk, (limit(i) - t + kUnit - 1) / kUnit)); };
+    auto steps_from = [&](const Item& i, int t) { return max(0, min(kAsk, (limit(i) - t + kStep - 1) / kStep)); };
     auto ask_q = [&](const Item& i) { w.load_q(a, i.b, i.h * a.group + 16 * NT * i.chunk, min(16 * NT, a.group - 16 * NT * i.chunk), lane); };
-    int t = begin(it), steps = steps_from(it, t), ids = w.pages_of(a, it.span, it.b, t, lane);
+    int t = begin(it), steps = steps_from(it, t), ids = w.pages_of(a, it.span, it.b, t, lane, kStep);
     ask_q(it);
     w.reset();
     if constexpr (L::kAhead) w.load(x, a, it.span, ids, 0, it.h, t, steps > 0, lane);
     w.split_q();
     while (true) {
         Item then = it;
-        const bool last = t + kAsk * kUnit >= limit(it), any = !last || more(then);
-        const int then_t = last ? begin(then) : t + kAsk * kUnit, then_steps = any ? steps_from(then, then_t) : 0;
-        const int then_ids = w.pages_of(a, then.span, then.b, any ? then_t : t, lane);
+        const bool last = t + kAsk * kStep >= limit(it), any = !last || more(then);
+        const int then_t = last ? begin(then) : t + kAsk * kStep, then_steps = any ? steps_from(then, then_t) : 0;
+        const int then_ids = w.pages_of(a, then.span, then.b, any ? then_t : t, lane, kStep);
         if constexpr (L::kAhead) {
             if (steps == 0) w.load(x, a, then.span, then_ids, 0, then.h, then_t, then_steps > 0, lane);
             for (int s = 0; s < steps; s += 2) {
-                w.load(y, a, it.span, ids, s + 1, it.h, t + (s + 1) * kUnit, s + 1 < steps, lane);
-                w.step(x, mine, a, it.span, t + s * kUnit, lane);
+                w.load(y, a, it.span, ids, s + 1, it.h, t + (s + 1) * kStep, s + 1 < steps, lane);
+                w.step(x, mine, a, it.span, t + s * kStep, lane);
                 const bool here = s + 2 < steps, over = s + 2 >= steps;
-                w.load(x, a, over ? then.span : it.span, over ? then_ids : ids, over ? 0 : s + 2, over ? then.h : it.h, over ? then_t : t + (s + 2) * kUnit,
+                w.load(x, a, over ? then.span : it.span, over ? then_ids : ids, over ? 0 : s + 2, over ? then.h : it.h, over ? then_t : t + (s + 2) * kStep,
                        here || (over && then_steps > 0), lane);
-                if (s + 1 < steps) w.step(y, mine, a, it.span, t + (s + 1) * kUnit, lane);
+                if (s + 1 < steps) w.step(y, mine, a, it.span, t + (s + 1) * kStep, lane);
             }
         } else {
             for (int s = 0; s < steps; ++s) {
-                w.load(x, a, it.span, ids, s, it.h, t + s * kUnit, true, lane);
-                w.step(x, mine, a, it.span, t + s * kUnit, lane);
+                w.load(x, a, it.span, ids, s, it.h, t + s * kStep, true, lane);
+                w.step(x, mine, a, it.span, t + s * kStep, lane);
             }
         }
         if (last) {
             if (any) ask_q(then);
-            finish<F32, CACHE, DIM, NT>(a, w, sums, it, wave, lane);
+            end(it);
             w.reset();
             if (!any) return;
             w.split_q();
@@ -624,9 +626,9 @@ __device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, Su
 
 // Outputs of query heads of a sequence without tokens.
 template <bool F32>
-__device__ inline void store_nothing(const Attn& a, long row, int n_heads, int tid) {
-    for (int i = tid; i < n_heads * a.dim; i += 256) store_out<F32>(a, row * a.dim + i, 0.f);
-    for (int i = tid; i < n_heads && a.lse != nullptr; i += 256) a.lse[row + i] = -INFINITY;
+__device__ inline void store_nothing(const Attn& a, long row, int n_heads, int tid, int threads) {
+    for (int i = tid; i < n_heads * a.dim; i += threads) store_out<F32>(a, row * a.dim + i, 0.f);
+    for (int i = tid; i < n_heads && a.lse != nullptr; i += threads) a.lse[row + i] = -INFINITY;
 }
 
 // A block for each sequence, key head and 16 * NT of its query heads; nothing is split.
@@ -642,10 +644,58 @@ __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_short
     it.span = span_of(a, a.lens[it.b]);
     it.u1 = it.span.units;
     if (it.u1 == 0) {
-        store_nothing<F32>(a, static_cast<long>(pair) * a.group + 16 * NT * it.chunk, min(16 * NT, a.group - 16 * NT * it.chunk), threadIdx.x);
+        store_nothing<F32>(a, static_cast<long>(pair) * a.group + 16 * NT * it.chunk, min(16 * NT, a.group - 16 * NT * it.chunk), threadIdx.x, 256);
         return;
     }
-    work<F32, CACHE, DIM, NT>(a, w, runs[wave], sums, it, [](Item&) { return false; }, wave, lane);
+    work<4>(a, w, runs[wave], it, [](Item&) { return false; }, [&](const Item& i) { finish(a, w, sums, i, wave, lane); }, wave, lane);
+}
+
+// The results of a wave that has had an item to itself.
+template <bool F32, int CACHE, int DIM, int NT>
+__device__ void finish_alone(const Attn& a, const Wave<F32, CACHE, DIM, NT>& w, const Item& it, int lane) {
+    constexpr int kOwn = Layout<CACHE, DIM>::kOwn;
+    const int n = lane % 16, g = lane / 16, in_group = 16 * NT * it.chunk, n_heads = min(16 * NT, a.group - in_group);
+    const long head0 = (static_cast<long>(it.b) * a.heads + it.h) * a.group + in_group;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const float l = quarters_sum(w.l[t]), inv = l == 0.f ? 0.f : 1.f / l;
+        const int c = 16 * t + n;
+        if (c >= n_heads) continue;
+        if (g == 0 && a.lse != nullptr) a.lse[head0 + c] = natural_log_of_sum(w.m[t], l);
+#pragma unroll
+        for (int hf = 0; hf < Layout<CACHE, DIM>::kHalves; ++hf)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = 128 * hf + kOwn * (4 * g + r);
+                if (d >= a.dim) continue;                             // (a.dim is a multiple of kOwn)
+                const long at = (head0 + c) * a.dim + d;
+#pragma unroll
+                for (int j = 0; j < kOwn; j += 4) {
+                    const f32x4 v = f32x4{w.o[t][hf][j][r], w.o[t][hf][j + 1][r], w.o[t][hf][j + 2][r], w.o[t][hf][j + 3][r]} * inv;
+                    if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at + j) = v;
+                    else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at + j) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+                }
+            }
+    }
+}
+
+// Many short sequences: a wave for each item, and no wait for others.
+template <bool F32, int CACHE, int DIM, int NT>
+__global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_wave_kernel(Attn a) {
+    __shared__ __attribute__((aligned(16))) char runs[4][Layout<CACHE, DIM>::kStaged ? Layout<CACHE, DIM>::kRun : 16];
+    const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), index = 4 * blockIdx.x + wave;
+    if (index >= a.B * a.items) return;                               // (no barrier in this kernel)
+    const int pair = index / a.chunks;
+    Item it{pair / a.heads, pair % a.heads, index % a.chunks, 0, 0, -1, {}};
+    Wave<F32, CACHE, DIM, NT> w;
+    w.lay_out(a, lane);
+    it.span = span_of(a, uniform(a.lens[it.b]));
+    it.u1 = it.span.units;
+    if (it.u1 == 0) {
+        store_nothing<F32>(a, static_cast<long>(pair) * a.group + 16 * NT * it.chunk, min(16 * NT, a.group - 16 * NT * it.chunk), lane, 64);
+        return;
+    }
+    work<1>(a, w, runs[wave], it, [](Item&) { return false; }, [&](const Item& i) { finish_alone(a, w, i, lane); }, 0, lane);
 }
 
 // The work is the list of all (sequence, key head, 16 * NT of its query heads, unit of tokens); every block takes an equal stretch of it, found from the lengths on the
@@ -685,7 +735,7 @@ __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_kerne
         __syncthreads();
     }
     for (int b = blockIdx.x; b < a.B; b += gridDim.x)
-        if (before[b + 1] == before[b]) store_nothing<F32>(a, static_cast<long>(b) * a.heads * a.group, a.heads * a.group, tid);
+        if (before[b + 1] == before[b]) store_nothing<F32>(a, static_cast<long>(b) * a.heads * a.group, a.heads * a.group, tid, 256);
 
     const int worker = blockIdx.x;
     const Cuts cuts(static_cast<long>(uniform(before[a.B])) * a.items, gridDim.x, one_over_workers);
@@ -697,7 +747,7 @@ __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_kerne
         if (it.u0 > 0 && left <= start + kToll)                       // begun in the stretch before
             cut = Cut{(it.b * a.heads + it.h) * a.group, 2 * (worker - 1) + (left >= start ? 0 : 1), cuts.of(start + it.span.units + kToll - 1), 16 * NT * it.chunk};
         if (tid == 0) a.cuts[worker] = cut;
-        work<F32, CACHE, DIM, NT>(a, w, runs[wave], sums, it, [&](Item& i) { return feed.next(i); }, wave, lane);
+        work<4>(a, w, runs[wave], it, [&](Item& i) { return feed.next(i); }, [&](const Item& i) { finish(a, w, sums, i, wave, lane); }, wave, lane);
     } else if (tid == 0) {
         a.cuts[worker] = cut;
     }
@@ -760,10 +810,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a) {
         for (int c = 0; c < 4; ++c) store_out<F32>(a, head * a.dim + 4 * col + c, weight == 0.f ? 0.f : v[c] / weight);
 }
 
-// How a call is cut: a block for each item, or, where sequences can be longer than `whole_units`, a stretch of the list of units for each block.
+// How a call is cut: a wave or a block for each item, or, where sequences can be longer than `whole_units`, a stretch of the list of units for each block.
 constexpr int kMaxUnits = 256;
 struct Plan {
-    bool is_short;
+    bool alone, is_short;           // a wave for each item; a block for each item
     int workers;
 };
 // Matrix columns, in sixteens, that take a key head's query heads.  fp32 products and heads of over 128 have no room for a second sixteen in
@@ -786,12 +836,20 @@ int whole_units(const moe_kv_cfg& kv, long items) {
     if (row_bytes > 128) return items >= 64 ? 8 : 6;
     return items >= 256 ? 16 : items >= 128 ? 12 : items >= 64 ? 8 : 6;
 }
+// Items from which each gets a wave and not a block, by the most tokens an item can have.  A block's other waves have nothing to do in short
+// items but are waited for, and hold its place.  us with a block / a wave for each, ragged lengths:
+//   64 heads of 64, bf16, 2560 items:    32 tokens 13.8 / 8.1, 128 17.2 / 13.3, 256 21.3 / 20.6, 500 32.6 / 36.4; 10240 items: 500 115.4 / 111.7
+//   64 heads of 128, bf16, 10240 items:  32 146.4 / 50.4, 128 166.3 / 79.8, 256 198.8 / 125.0, 500 275.4 / 215.5
+//   32 over 8 of 128, bf16, 320 items:   32 9.6 / 6.3, 128 9.7 / 9.4, 256 10.7 / 13.7
+//   12 over 4 of 80, fp32, 640 items:    32 20.3 / 9.8, 128 22.3 / 18.6, 256 28.3 / 29.8
+long least_alone(long tokens) { return tokens <= 32 ? 320 : tokens <= kUnit ? 640 : tokens <= 2 * kUnit ? 1024 : tokens <= 4 * kUnit ? 4096 : 1L << 40; }
 Plan plan_of(const moe_kv_cfg& kv, const moe_attn_cfg& c, int compute_units) {
     const long room = static_cast<long>(c.table_pages) * kv.page_size;
     const long longest = c.window > 0 ? std::min(room, c.window + 15L) : room, units = (longest + kUnit - 1) / kUnit;
     const long items = static_cast<long>(c.B) * kv.heads * chunks_of(kv, c);
     Plan p;
-    p.is_short = units <= whole_units(kv, items);
+    p.alone = items >= least_alone(longest);
+    p.is_short = p.alone || units <= whole_units(kv, items);
     // One block per compute unit reads as fast as two and leaves fewer parts; only where heads are narrow and items many does a second one
     // fill the gaps between items (us with one / two: 40 x 1024 tokens, 64 heads of 64: 123 / 104; 1 x 131072, 8 heads of 128: 85 / 88).
     const int per_unit = kv.head_dim <= 64 && items >= 4 * kMaxUnits ? 2 : 1;
@@ -820,6 +878,11 @@ int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) 
     a.chunks = chunks_of(kv, c);
     a.items = a.heads * a.chunks;
     a.item_rows = std::min(16 * NT, a.group);
+    if (p.alone) {
+        hipLaunchKernelGGL((attn_wave_kernel<F32, CACHE, DIM, NT>), dim3((a.B * a.items + 3) / 4), dim3(256), 0, s, a);
+        MOE_LAUNCH_CHECK("attn_wave_kernel");
+        return MOE_OK;
+    }
     if (p.is_short) {
         hipLaunchKernelGGL((attn_short_kernel<F32, CACHE, DIM, NT>), dim3(a.B * a.heads * a.chunks), dim3(256), 0, s, a);
         MOE_LAUNCH_CHECK("attn_short_kernel");

@@ -332,6 +332,22 @@ def test_attention_where_sequences_begin_to_be_split(B, heads, group, dim, cache
         run_and_check(cfg, arrays, q, table.cuda(), lens, only=sorted({0, 1 % B, B - 1}))
 
 
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("B,room,heads,group,dim,window", [
+    (45, 32, 8, 1, 64, 0), (24, 128, 32, 3, 128, 0), (70, 256, 4, 33, 80, 0), (40, 512, 32, 2, 128, 100), (24, 128, 16, 17, 256, 0), (66, 512, 64, 1, 64, 0)])
+def test_attention_of_many_short_sequences(B, room, heads, group, dim, window, dtype, cache):
+    """A wave for each sequence and group of query heads: lengths of all kinds, a number of items that does not fill the last block."""
+    page = 16
+    per = room // page
+    cfg = M.KvCfg.make(B * per, page, heads, dim, dtype, cache)
+    table = tables(8, B, per, cfg.pages)
+    lens = [min(room, n) for n in [0, 1, 15, 17, 31, 32, 33, 64, 65, 127, 128, 129, 255, 300, room, room - 1]]
+    lens += [(37 * b) % (room + 1) for b in range(B - len(lens))]
+    arrays = cache_of(38, cfg, table, lens, window=window)
+    q = normal(40, (B, heads * group, dim), dtype, 2.0)
+    run_and_check(cfg, arrays, q, table.cuda(), lens, window, only=[*range(16), B - 1])
+
+
 def test_attention_of_as_many_sequences_as_there_may_be():
     """4096 sequences of 0 to 40 tokens, and 1000 of which one is long: the stretches of a block begin and end anywhere."""
     for B, lens, heads in ((4096, [(b * 29) % 41 for b in range(4096)], 1), (1000, [(b % 3) * 20 if b != 777 else 4000 for b in range(1000)], 2)):
