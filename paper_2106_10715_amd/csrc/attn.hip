@@ -47,6 +47,7 @@ struct Attn {
     float *part_o, *part_ml;        // [workers][2][group][dim], [workers][2][group][2]: unscaled sums; their maximum and weight
     Cut* cuts;                      // [workers]
     int B, heads, group, chunks, items, item_rows, dim, pages, page_bits, table_pages, window;
+    int over_row;                   // 2^16 over the pieces of a row, rounded up: a quotient of numbers below 2^10 is a product and a shift
     float scale;                    // times log2 e
 };
 
@@ -186,7 +187,7 @@ struct Wave {
                 k_at[i] = n * row_bytes + 16 * min(4 * i + g, per - 1);
                 continue;
             }
-            const int at = min(64 * i + lane, 16 * per - 1), token = at / per, piece = at - token * per;
+            const int at = min(64 * i + lane, 16 * per - 1), token = (at * a.over_row) >> 16, piece = at - token * per;
             k_at[i] = 16 * at;
             k_in[i] = 16 * (token * 4 * L::kPieces + ((piece ^ token) & (4 * L::kPieces - 1)));          // 16 tokens' pieces: in 16 different places of a row
             k_out[i] = 16 * (n * 4 * L::kPieces + ((min(4 * i + g, per - 1) ^ n) & (4 * L::kPieces - 1)));
@@ -877,6 +878,8 @@ int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) 
     const Plan p = plan_of(kv, c, info->compute_units);
     a.chunks = chunks_of(kv, c);
     a.items = a.heads * a.chunks;
+    const int per = a.dim / Layout<CACHE, DIM>::kPiece;
+    a.over_row = (65536 + per - 1) / per;
     a.item_rows = std::min(16 * NT, a.group);
     if (p.alone) {
         hipLaunchKernelGGL((attn_wave_kernel<F32, CACHE, DIM, NT>), dim3((a.B * a.items + 3) / 4), dim3(256), 0, s, a);
@@ -930,7 +933,7 @@ int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* 
     a.B = c.B;
     a.heads = kv.heads;
     a.group = c.q_heads / kv.heads;
-    a.chunks = a.items = a.item_rows = 0;                             // set where the column tiles are chosen
+    a.chunks = a.items = a.item_rows = a.over_row = 0;                        // set where the column tiles are chosen
     a.dim = kv.head_dim;
     a.pages = kv.pages;
     a.page_bits = __builtin_ctz(kv.page_size);
