@@ -122,9 +122,9 @@ __global__ __launch_bounds__(256) void kv_kernel(Side k, Side v, const int32_t* 
                     for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(f[i][c]));
                     scale[i] = e4m3_scale(lanes_max<LANES>(top));
                     if (lane == 0) sides[i]->scales[at] = scale[i];
-                    const float inv = 1.f / scale[i];
+                    const OverScale over(scale[i]);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) f[i][c] *= inv;
+                    for (int c = 0; c < 8; ++c) f[i][c] = over(f[i][c]);
                 }
                 if (lane >= eights) continue;
                 Eight<CACHE> out;

@@ -110,9 +110,9 @@ __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void add_norm_kernel(const u
             if (p < pieces && p % (group / E) == 0) q_scale[row * groups + p / (group / E)] = scale;
         }
         if (p >= pieces) continue;
-        const float inv = 1.f / scale;
+        const OverScale over(scale);
 #pragma unroll
-        for (int c = 0; c < E; ++c) v[i][c] *= inv;
+        for (int c = 0; c < E; ++c) v[i][c] = over(v[i][c]);
         if constexpr (BF16)
             store_to<STREAM != 0>(reinterpret_cast<u32x2*>(q) + at + p, u32x2{to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3]), to_e4m3x4(v[i][4], v[i][5], v[i][6], v[i][7])});
         else
