@@ -176,24 +176,33 @@ struct Wave {
     uint32_t k_at[L::kPieces], k_in[L::kPieces], k_out[L::kPieces], v_at[L::kHalves];    // of this lane: bytes from a run's first row, bytes in the LDS
     int row_bytes;
 
-    // What does not change from item to item.  Where rows are shorter than DIM, pieces past their end are taken from their last piece:
-    // Q has zeros there, and columns past the end are not stored.
+    // What does not change from item to item.  Where rows are shorter than DIM, K has zeros past their end as Q has (a zero of Q would make NaN of an
+    // infinity): past the end of a load, or as clear_past_end leaves them.  Columns of V past the end are taken from the last ones and not stored.
     __device__ void lay_out(const Attn& a, int lane) {
         const int n = lane % 16, g = lane / 16, per = a.dim / L::kPiece;
         row_bytes = a.dim * L::kWidth;
 #pragma unroll
         for (int i = 0; i < L::kPieces; ++i) {
             if constexpr (!L::kStaged) {
-                k_at[i] = n * row_bytes + 16 * min(4 * i + g, per - 1);
+                k_at[i] = 4 * i + g < per ? n * row_bytes + 16 * (4 * i + g) : 0x7fffff00;
                 continue;
             }
             const int at = min(64 * i + lane, 16 * per - 1), token = (at * a.over_row) >> 16, piece = at - token * per;
             k_at[i] = 16 * at;
             k_in[i] = 16 * (token * 4 * L::kPieces + ((piece ^ token) & (4 * L::kPieces - 1)));          // 16 tokens' pieces: in 16 different places of a row
-            k_out[i] = 16 * (n * 4 * L::kPieces + ((min(4 * i + g, per - 1) ^ n) & (4 * L::kPieces - 1)));
+            k_out[i] = 16 * (n * 4 * L::kPieces + (((4 * i + g) ^ n) & (4 * L::kPieces - 1)));
         }
 #pragma unroll
         for (int hf = 0; hf < L::kHalves; ++hf) v_at[hf] = 4 * g * row_bytes + min(128 * hf + L::kOwn * n, a.dim - L::kOwn) * L::kWidth;
+    }
+
+    // Zeros past the rows' ends in the wave's run of K in LDS.  Nothing is written over them, and each is read by its own lane alone.
+    __device__ void clear_past_end(const Attn& a, char* mine, int lane) const {
+        if constexpr (L::kStaged)
+            if (a.dim % (4 * L::kPiece) != 0)
+#pragma unroll
+                for (int i = 0; i < L::kPieces; ++i)
+                    if (4 * i + lane / 16 >= a.dim / L::kPiece) *reinterpret_cast<u32x4*>(mine + k_out[i]) = u32x4{0, 0, 0, 0};
     }
 
     __device__ void reset() {
@@ -589,6 +598,7 @@ __device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, It
     ask_q(it);
     w.reset();
     if constexpr (L::kAhead) w.load(x, a, it.span, ids, 0, it.h, t, steps > 0, lane);
+    w.clear_past_end(a, mine, lane);
     w.split_q();
     while (true) {
         Item then = it;
