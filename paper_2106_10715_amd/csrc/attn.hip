@@ -148,9 +148,12 @@ __device__ inline float quarters_sum(float v) {
     return v + __shfl_xor(v, 32);
 }
 
-// Two values as bf16, and what that leaves of them.
+constexpr float kMost = 0x1.fep127f;        // the largest bf16 value
+
+// Two values as bf16, and what that leaves of them.  CUT: their upper halves (rounded, the largest finite values would be infinite).
+template <bool CUT = false>
 __device__ inline uint32_t take_bf16x2(float& lo, float& hi) {
-    const uint32_t u = to_bf16x2(lo, hi);
+    const uint32_t u = CUT ? __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u) : to_bf16x2(lo, hi);
     lo -= bf16_lo(u);
     hi -= bf16_hi(u);
     return u;
@@ -255,7 +258,10 @@ struct Wave {
                         for (int part = 0; part < kPartsQ; ++part) {
                             u32x4 u;
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) u[c] = take_bf16x2(q32[t][i][8 * s + 2 * c], q32[t][i][8 * s + 2 * c + 1]);
+                            for (int c = 0; c < 4; ++c) {
+                                float &lo = q32[t][i][8 * s + 2 * c], &hi = q32[t][i][8 * s + 2 * c + 1];
+                                u[c] = part == 0 ? take_bf16x2<true>(lo, hi) : take_bf16x2(lo, hi);
+                            }
                             q16[part][t][i][s] = __builtin_bit_cast(bf16x8, u);
                         }
     }
@@ -316,12 +322,15 @@ struct Wave {
             }
         }
 
+        // The lesser parts of fp32 queries have a sum of their own: a part that is zero, or of the other sign, makes NaN of an infinite key, as what is
+        // left of an infinite query does, and then the leading part's sum, which is not finite either, is the logit.
         f32x4 s[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 s[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+                f32x4 rest = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < L::kPieces; ++i) {
                     if (4 * i * L::kPiece >= a.dim) break;
@@ -333,12 +342,17 @@ struct Wave {
                         u32x4 pairs[kSteps];
                         to_pairs<CACHE, L::kPiece>(k[r][i].w, reinterpret_cast<uint32_t*>(pairs));
 #pragma unroll
-                        for (int st = 0; st < kSteps; ++st)
+                        for (int st = 0; st < kSteps; ++st) {
+                            const auto at = __builtin_bit_cast(bf16x8, pairs[st]);
 #pragma unroll
-                            for (int part = kPartsQ - 1; part >= 0; --part)
-                                s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pairs[st]), q16[part][t][i][st], s[t][r], 0, 0, 0);
+                            for (int part = kPartsQ - 1; part > 0; --part) rest = __builtin_amdgcn_mfma_f32_16x16x32_bf16(at, q16[part][t][i][st], rest, 0, 0, 0);
+                            s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(at, q16[0][t][i][st], s[t][r], 0, 0, 0);
+                        }
                     }
                 }
+                if constexpr (F32 && !kWide)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) s[t][r][c] += __builtin_amdgcn_fmed3f(rest[c], -kMost, kMost);       // (the lower bound for NaN)
             }
 
         const bool edge = t0 < span.first || t0 + 32 > span.end;

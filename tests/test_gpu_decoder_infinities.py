@@ -60,3 +60,52 @@ def infinite_keys(dtype, cache, dim, n, column):
 @pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "f32")])
 def test_infinite_keys_in_the_last_column_of_odd_widths(dtype, cache, dim, n):
     infinite_keys(dtype, cache, dim, n, dim - 1)
+
+
+@pytest.mark.parametrize("n", [20, 5000])
+@pytest.mark.parametrize("dim,column", [(16, 0), (48, 47), (64, 33), (80, 79), (128, 5), (144, 143), (256, 200)])
+def test_infinite_keys_under_fp32_queries_in_parts(dim, column, n):
+    """The parts of 0.3 have two signs, those of 1.0 are zeros but for the first."""
+    infinite_keys("f32", "bf16", dim, n, column)
+
+
+@pytest.mark.parametrize("n", [20, 5000])
+@pytest.mark.parametrize("dim", [48, 64, 128, 144, 256])
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("bf16", "e4m3"), ("f32", "f32"), ("f32", "bf16"), ("f32", "e4m3")])
+def test_infinite_queries(dtype, cache, dim, n):
+    """-infinity against keys above zero: logits of -infinity alone; +infinity: no number; the other heads of the same keys as they were."""
+    page = 16
+    cfg = M.KvCfg.make(-(-n // page), page, 1, dim, dtype, cache)
+    table = tables(6, 1, cfg.pages, cfg.pages)
+    k, v = normal(70, (n, 1, dim), dtype), normal(71, (n, 1, dim), dtype)
+    k[:, :, dim - 1] = k[:, :, dim - 1].abs() + 0.5
+    arrays = cfg.empty()
+    index, at = place(table, n, page)
+    M.moe_kv_write(cfg, k, v, (index * page + at).int(), *arrays)
+    q = normal(72, (1, 4, dim), dtype)
+    want, want_lse = run_attention(cfg, arrays, q, table.cuda(), [n])
+    q[0, 1, dim - 1], q[0, 2, dim - 1] = -math.inf, math.inf
+    out, lse = run_attention(cfg, arrays, q, table.cuda(), [n])
+    assert (out[0, 1] == 0).all() and lse[0, 1] == -math.inf
+    assert torch.isnan(out[0, 2]).all()
+    assert torch.equal(out[0, ::3], want[0, ::3]) and torch.equal(lse[0, ::3], want_lse[0, ::3])
+
+
+@pytest.mark.parametrize("n", [20, 5000])
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+def test_the_largest_finite_query(cache, n):
+    """3.4e38 is past the largest value of 16 bits that is not infinite."""
+    page, dim = 16, 64
+    cfg = M.KvCfg.make(-(-n // page), page, 1, dim, "f32", cache)
+    table = tables(6, 1, cfg.pages, cfg.pages)
+    k, v = normal(73, (n, 1, dim), "f32"), normal(74, (n, 1, dim), "f32")
+    k[:, :, 3] *= 2.0 ** -124
+    arrays = cfg.empty()
+    index, at = place(table, n, page)
+    M.moe_kv_write(cfg, k, v, (index * page + at).int(), *arrays)
+    q = normal(75, (1, 2, dim), "f32")
+    q[0, 0, 3], q[0, 1, 3] = torch.finfo(torch.float32).max, -3.3962e38
+    out, lse = run_attention(cfg, arrays, q, table.cuda(), [n])
+    k, v = (t[index, 0, at].float().cpu().numpy().astype(np.float64) for t in arrays[:2])
+    for head in range(2):
+        check_head(out[0, head], lse[0, head], f64(q[0, head]), k, v, 1 / math.sqrt(dim), "f32", f"head {head}")
