@@ -161,7 +161,7 @@ def _stream(stream: Optional[torch.cuda.Stream]):
 
 
 def _native(name: str, *args, stream=None) -> bool:
-    """The call through _args.  False where an argument is not as it has to be, which the caller's own checks then explain."""
+    """The call through _args.  False where an argument is not as it has to be: the caller then says which and why, and calls nothing."""
     global _ARGS
     if _LIB is None or _ARGS is None:
         lib()
@@ -365,67 +365,92 @@ def moe_layer_forward_timed(cfg, x, W_g, gate_bias, W_packed, y, ws, timer: Time
                                          _ptr(ws), _stream(stream), timer.handle))
 
 
-def _array(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int) -> Optional[int]:
-    """Address of a contiguous device tensor of this type and size (None stays None: the library says whether it may be)."""
+def _tensor(t, name: str) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor):
+        raise MoeError(f"{name} must be a tensor (got {type(t).__name__})")
+    return t
+
+
+def _description(cfg, kind, name: str = "cfg"):
+    """The description, whose types have to be ones there are."""
+    if not isinstance(cfg, kind):
+        raise MoeError(f"{name} must be {'an' if kind is AttnCfg else 'a'} {kind.__name__} (got {type(cfg).__name__})")
+    for field in ("dtype", "cache_dtype"):
+        if getattr(cfg, field, MOE_F32) not in _TORCH:
+            raise MoeError(f"{field} must be MOE_F32, MOE_BF16 or MOE_E4M3 (got {getattr(cfg, field)})")
+    return cfg
+
+
+def _array(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int) -> None:
+    """Refuses what is not a contiguous device tensor of this type and size (None is for the library to refuse)."""
     if t is None:
-        return None
-    if t.dtype is dtype and t.numel() == numel and t.is_contiguous():
-        if t.is_cuda:
-            return t.data_ptr()
+        return
+    _tensor(t, name)
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
+        raise MoeError(f"{name} must be a contiguous {dtype} tensor of {numel} elements (got {t.dtype}, shape {tuple(t.shape)}, "
+                       f"strides {t.stride()})")
+    if not t.is_cuda:
         raise MoeError(f"{name} must be in device memory")
-    raise MoeError(f"{name} must be a contiguous {dtype} tensor of {numel} elements (got {t.dtype}, shape {tuple(t.shape)}, "
-                   f"strides {t.stride()})")
 
 
-def _head_rows(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int, heads: int, dim: int):
-    """Address and row stride of [n, heads, dim] whose rows may be part of wider ones, each row contiguous."""
+def _head_rows(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int, heads: int, dim: int) -> None:
+    """Refuses what is not [n, heads, dim] in device memory, whose rows may be part of wider ones, each row contiguous."""
     if t is None:
-        return None, heads * dim
-    if t.dtype is dtype and t.shape == (n, heads, dim):
-        row, head, one = t.stride()
-        if one == 1 and (head == dim or heads == 1) or n == 0:
-            if t.is_cuda:
-                return t.data_ptr(), row if n > 1 else heads * dim
-            raise MoeError(f"{name} must be in device memory")
-    raise MoeError(f"{name} must be a {dtype} tensor [{n}, {heads}, {dim}] with contiguous rows (got {t.dtype}, shape "
-                   f"{tuple(t.shape)}, strides {t.stride()})")
+        return
+    _tensor(t, name)
+    if t.dtype is not dtype or t.shape != (n, heads, dim) or n > 0 and (t.stride(2) != 1 or t.stride(1) != dim and heads != 1):
+        raise MoeError(f"{name} must be a {dtype} tensor [{n}, {heads}, {dim}] with contiguous rows (got {t.dtype}, shape "
+                       f"{tuple(t.shape)}, strides {t.stride()})")
+    if not t.is_cuda:
+        raise MoeError(f"{name} must be in device memory")
+
+
+def _cache(cfg: KvCfg, k_pages, v_pages, k_scales, v_scales) -> None:
+    dt, rows = _TORCH[cfg.cache_dtype], cfg.pages * cfg.heads * cfg.page_size
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        _array(t, name, dt, rows * cfg.head_dim)
+    for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+        _array(t, name, torch.float32, rows)
+
+
+def _tokens(slots) -> int:
+    if slots is None:
+        raise MoeError("slots is NULL")
+    return _tensor(slots, "slots").numel()
+
+
+def _refused(name: str):
+    raise MoeError(f"{name}: an argument is not as its description says")
 
 
 def moe_add_norm(cfg: NormCfg, x, residual, weight, sum, y, q=None, q_scale=None, stream=None) -> None:
     if _native("add_norm", cfg, x, residual, weight, sum, y, q, q_scale, stream=stream):
         return
-    dt, n = _TORCH.get(cfg.dtype), cfg.T * cfg.d
-    groups = cfg.T * (cfg.d // cfg.q_group if cfg.q_group > 0 else 1)
-    _check(lib().moe_add_norm(C.addressof(cfg), _array(x, "x", dt, n), _array(residual, "residual", dt, n),
-                              _array(weight, "weight", dt, cfg.d), _array(sum, "sum", dt, n), _array(y, "y", dt, n),
-                              _array(q, "q", torch.float8_e4m3fn, n), _array(q_scale, "q_scale", torch.float32, groups),
-                              _stream(stream)))
+    dt, n = _TORCH[_description(cfg, NormCfg).dtype], cfg.T * cfg.d
+    for t, name, numel in ((x, "x", n), (residual, "residual", n), (weight, "weight", cfg.d), (sum, "sum", n), (y, "y", n)):
+        _array(t, name, dt, numel)
+    _array(q, "q", torch.float8_e4m3fn, n)
+    _array(q_scale, "q_scale", torch.float32, cfg.T * (cfg.d // cfg.q_group if cfg.q_group > 0 else 1))
+    _refused("moe_add_norm")
 
 
-def _cache(cfg: KvCfg, k_pages, v_pages, k_scales, v_scales):
-    dt, rows = _TORCH.get(cfg.cache_dtype), cfg.pages * cfg.heads * cfg.page_size
-    return (_array(k_pages, "k_pages", dt, rows * cfg.head_dim), _array(v_pages, "v_pages", dt, rows * cfg.head_dim),
-            _array(k_scales, "k_scales", torch.float32, rows), _array(v_scales, "v_scales", torch.float32, rows))
+def _kv_refused(name: str, cfg: KvCfg, k, v, slots, cache) -> None:
+    dt, n = _TORCH[_description(cfg, KvCfg).dtype], _tokens(slots)
+    _head_rows(k, "k", dt, n, cfg.heads, cfg.head_dim)
+    _head_rows(v, "v", dt, n, cfg.heads, cfg.head_dim)
+    _cache(cfg, *cache)
+    _array(slots, "slots", torch.int32, n)
+    _refused(name)
 
 
 def moe_kv_write(cfg: KvCfg, k, v, slots, k_pages, v_pages, k_scales=None, v_scales=None, stream=None) -> None:
-    if _native("kv_write", cfg, k, v, slots, k_pages, v_pages, k_scales, v_scales, stream=stream):
-        return
-    n, dt = slots.numel(), _TORCH.get(cfg.dtype)
-    kp, ks = _head_rows(k, "k", dt, n, cfg.heads, cfg.head_dim)
-    vp, vs = _head_rows(v, "v", dt, n, cfg.heads, cfg.head_dim)
-    _check(lib().moe_kv_write(C.addressof(cfg), n, kp, ks, vp, vs, _array(slots, "slots", torch.int32, n),
-                              *_cache(cfg, k_pages, v_pages, k_scales, v_scales), _stream(stream)))
+    if not _native("kv_write", cfg, k, v, slots, k_pages, v_pages, k_scales, v_scales, stream=stream):
+        _kv_refused("moe_kv_write", cfg, k, v, slots, (k_pages, v_pages, k_scales, v_scales))
 
 
 def moe_kv_read(cfg: KvCfg, k_pages, v_pages, k_scales, v_scales, slots, k, v, stream=None) -> None:
-    if _native("kv_read", cfg, k_pages, v_pages, k_scales, v_scales, slots, k, v, stream=stream):
-        return
-    n, dt = slots.numel(), _TORCH.get(cfg.dtype)
-    kp, ks = _head_rows(k, "k", dt, n, cfg.heads, cfg.head_dim)
-    vp, vs = _head_rows(v, "v", dt, n, cfg.heads, cfg.head_dim)
-    _check(lib().moe_kv_read(C.addressof(cfg), n, *_cache(cfg, k_pages, v_pages, k_scales, v_scales),
-                             _array(slots, "slots", torch.int32, n), kp, ks, vp, vs, _stream(stream)))
+    if not _native("kv_read", cfg, k_pages, v_pages, k_scales, v_scales, slots, k, v, stream=stream):
+        _kv_refused("moe_kv_read", cfg, k, v, slots, (k_pages, v_pages, k_scales, v_scales))
 
 
 def moe_attn_workspace_bytes(cfg: KvCfg, attn: AttnCfg) -> int:
@@ -438,11 +463,19 @@ def moe_attn_decode(cfg: KvCfg, attn: AttnCfg, q, k_pages, v_pages, k_scales, v_
     if _native("attn_decode", cfg, attn, q, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws,
                stream=stream):
         return
-    B, heads, dt = attn.B, attn.q_heads, _TORCH.get(cfg.dtype)
-    qp, qs = _head_rows(q, "q", dt, B, heads, cfg.head_dim)
-    if ws is not None and ws.nbytes < moe_attn_workspace_bytes(cfg, attn):
-        raise MoeError("ws is smaller than moe_attn_workspace_bytes")
-    _check(lib().moe_attn_decode(C.addressof(cfg), C.addressof(attn), qp, qs, *_cache(cfg, k_pages, v_pages, k_scales, v_scales),
-                                 _array(table, "table", torch.int32, B * attn.table_pages), _array(lens, "lens", torch.int32, B),
-                                 _array(out, "out", dt, B * heads * cfg.head_dim), _array(lse, "lse", torch.float32, B * heads),
-                                 _ptr(ws), _stream(stream)))
+    dt = _TORCH[_description(cfg, KvCfg).dtype]
+    B, heads = _description(attn, AttnCfg, "attn").B, attn.q_heads
+    _head_rows(q, "q", dt, B, heads, cfg.head_dim)
+    if ws is not None:
+        if _tensor(ws, "ws").nbytes < moe_attn_workspace_bytes(cfg, attn):
+            raise MoeError("ws is smaller than moe_attn_workspace_bytes")
+        if not ws.is_contiguous():
+            raise MoeError("ws must be contiguous")
+        if not ws.is_cuda:
+            raise MoeError("ws must be in device memory")
+    _cache(cfg, k_pages, v_pages, k_scales, v_scales)
+    _array(table, "table", torch.int32, B * attn.table_pages)
+    _array(lens, "lens", torch.int32, B)
+    _array(out, "out", dt, B * heads * cfg.head_dim)
+    _array(lse, "lse", torch.float32, B * heads)
+    _refused("moe_attn_decode")
