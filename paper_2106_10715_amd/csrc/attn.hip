@@ -855,9 +855,10 @@ int chunks_of(const moe_kv_cfg& kv, const moe_attn_cfg& c) {
 //   64 over 8 of 128, e4m3 cache:    16 x 1500 17.7 / 17.5, 64 x 2048 36.0 / 32.8, 200 x 1000 60.0 / 48.8, but 16 x 2048 19.1 / 21.7
 //   32 over 8 of 128, bf16 cache:    4 x 700 11.8 / 11.0, 16 x 1000 16.2 / 14.4, 200 x 1000 77.2 / 73.0, but 4 x 1000 12.3 / 13.3, 16 x 1500 18.3 / 19.2
 //   16 over 2 of 256, bf16 cache:    4 x 700 13.9 / 19.7;   12 over 4 of 80 in fp32: 4 x 700 14.5 / 21.9
+int row_bytes_of(const moe_kv_cfg& kv) { return kv.head_dim * (kv.cache_dtype == MOE_F32 ? 4 : kv.cache_dtype == MOE_BF16 ? 2 : 1); }
 int whole_units(const moe_kv_cfg& kv, long items) {
     if (kv.dtype == MOE_F32 || kv.head_dim > 128) return 4;
-    const int row_bytes = kv.head_dim * (kv.cache_dtype == MOE_E4M3 ? 1 : 2);
+    const int row_bytes = row_bytes_of(kv);
     if (row_bytes > 128) return items >= 64 ? 8 : 6;
     return items >= 256 ? 16 : items >= 128 ? 12 : items >= 64 ? 8 : 6;
 }
@@ -875,9 +876,13 @@ Plan plan_of(const moe_kv_cfg& kv, const moe_attn_cfg& c, int compute_units) {
     Plan p;
     p.alone = items >= least_alone(longest);
     p.is_short = p.alone || units <= whole_units(kv, items);
-    // One block per compute unit reads as fast as two and leaves fewer parts; only where heads are narrow and items many does a second one
-    // fill the gaps between items (us with one / two: 40 x 1024 tokens, 64 heads of 64: 123 / 104; 1 x 131072, 8 heads of 128: 85 / 88).
-    const int per_unit = kv.head_dim <= 64 && items >= 4 * kMaxUnits ? 2 : 1;
+    // Blocks per compute unit: one leaves fewer parts, two fill the gaps between items where rows are short and items many.  us with one / two, full
+    // batches (ragged ones):
+    //   64 over 8 of 64, e4m3:       64 x 2080 41.3 / 33.8 (31.2 / 26.2), 256 x 4000 262 / 233 (148 / 116), but 32 x 4000 37.3 / 39.8 (28.1 / 27.2)
+    //   32 over 8 of 32, bf16:       64 x 4000 58.6 / 54.2 (40.5 / 36.2);   1 x 20000 14.8 / 15.8
+    //   32 over 8 of 64, bf16:       64 x 4000 124.9 / 87.4 (50.0 / 51.4), 256 x 4000 325 / 327 (173 / 175)
+    //   64 heads of 64, bf16:        40 x 4000 414 / 400 (202 / 205);   fp32 cache: 40 x 1024 212 / 213 (119 / 125)
+    const int per_unit = kv.head_dim <= 64 && row_bytes_of(kv) <= 128 && items >= 2 * kMaxUnits ? 2 : 1;
     p.workers = static_cast<int>(std::min(units * items, static_cast<long>(per_unit) * std::min(compute_units, kMaxUnits)));
     return p;
 }
