@@ -854,10 +854,22 @@ int chunks_of(const moe_kv_cfg& kv, const moe_attn_cfg& c) {
 //   64 heads of 64, bf16 cache:      1 x 1000 12.4 / 10.1, 4 x 2048 19.8 / 17.3, 40 x 2048 117.4 / 113.5, but 1 x 2048 14.6 / 16.1
 //   64 over 8 of 128, e4m3 cache:    16 x 1500 17.7 / 17.5, 64 x 2048 36.0 / 32.8, 200 x 1000 60.0 / 48.8, but 16 x 2048 19.1 / 21.7
 //   32 over 8 of 128, bf16 cache:    4 x 700 11.8 / 11.0, 16 x 1000 16.2 / 14.4, 200 x 1000 77.2 / 73.0, but 4 x 1000 12.3 / 13.3, 16 x 1500 18.3 / 19.2
-//   16 over 2 of 256, bf16 cache:    4 x 700 13.9 / 19.7;   12 over 4 of 80 in fp32: 4 x 700 14.5 / 21.9
+//   16 over 2 of 256, bf16 cache:    16 x 500 15.7 / 14.5, but 4 x 700 13.9 / 19.7, 16 x 700 14.0 / 18.2;  64 x 700 22.0 / 20.7, 200 x 1000 47.2 / 47.3
+//   40 heads of 160, bf16 cache:     2 x 1000 16.4 / 23.0, 40 x 1000 105.3 / 106.6 (all full: 175.5 / 192.1)
+//   64 heads of 160, e4m3 cache:     4 x 700 21.0 / 18.0, 40 x 1000 143.9 / 129.3, 40 x 1500 185.6 / 168.4, but 64 over 8 of 192: 8 x 1000 17.0 / 20.8
+//   32 over 8 of 128, fp32 over bf16: 16 x 700 15.4 / 12.2, 40 x 1000 24.0 / 18.4, 200 x 1000 78.8 / 74.7 (all full: 141.5 / 142.8);
+//                                    40 heads of 160: 2 x 1000 21.7 / 25.6, 16 x 1000 67.7 / 50.3
+//   12 over 4 of 80, fp32 cache:     16 x 500 17.0 / 15.9, 64 x 700 28.0 / 23.1, 64 x 1000 31.9 / 28.9, but 4 x 700 14.5 / 21.9, 16 x 700 17.2 / 20.7, 200 x 1000
+//                                    65.8 / 71.0;  40 heads of 80: 40 x 700 93.6 / 93.7 (all full: 142.6 / 159.4)
+//   16 over 4 of 256, fp32 cache:    2 x 128 17.7 / 13.1, 16 x 256 41.1 / 31.7, 64 x 500 77.3 / 72.0, but 2 x 500 19.4 / 43.1, 16 x 384 42.0 / 48.4,
+//                                    200 x 700 242 / 249 (all full: 357 / 419)
 int row_bytes_of(const moe_kv_cfg& kv) { return kv.head_dim * (kv.cache_dtype == MOE_F32 ? 4 : kv.cache_dtype == MOE_BF16 ? 2 : 1); }
 int whole_units(const moe_kv_cfg& kv, long items) {
-    if (kv.dtype == MOE_F32 || kv.head_dim > 128) return 4;
+    if (kv.cache_dtype == MOE_F32) return kv.head_dim > 128 && items < 256 ? 2 : 4;
+    if (kv.dtype == MOE_F32 || kv.head_dim > 128) {
+        const bool many = items >= (kv.head_dim > 128 ? 128 : 64);
+        return many && (kv.dtype == MOE_F32 || kv.cache_dtype == MOE_E4M3) ? 8 : 4;
+    }
     const int row_bytes = row_bytes_of(kv);
     if (row_bytes > 128) return items >= 64 ? 8 : 6;
     return items >= 256 ? 16 : items >= 128 ? 12 : items >= 64 ? 8 : 6;

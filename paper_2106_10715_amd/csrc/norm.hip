@@ -130,7 +130,8 @@ void launch(const moe_norm_cfg& c, const void* x, const void* residual, const vo
                            static_cast<const u32x4*>(residual), static_cast<const u32x4*>(weight), static_cast<u32x4*>(sum),
                            static_cast<u32x4*>(y), static_cast<uint32_t*>(q), q_scale, c.T, pieces, c.q_group, c.eps, 1.f / c.d);
     };
-    // one piece per thread where a block can hold the row so (65536 x 4096: 363 us with 512 threads, 380 with 256 of two pieces)
+    // one piece per thread where a block can hold the row so (65536 x 4096: 345 us with 512 threads, 370 with 256 of two pieces; threads without a
+    // piece cost nothing: as many bytes in rows of 4096, 5120, 8192, 12288 take 167, 167, 173, 170)
     if (pieces <= 64) run(add_norm_kernel<BF16, 64, 1, STREAM>, 64);
     else if (pieces <= 128) run(add_norm_kernel<BF16, 64, 2, STREAM>, 64);
     else if (pieces <= 256) run(add_norm_kernel<BF16, 256, 1, STREAM>, 256);
