@@ -603,6 +603,7 @@ template <int TEAM, bool F32, int CACHE, int DIM, int NT, typename More, typenam
 __device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, Item it, More more, End end, int wave, int lane) {
     using L = Layout<CACHE, DIM>;
     constexpr int kStep = 32 * TEAM;
+    constexpr bool kAskEarly = !(F32 && DIM > 128);              // (with the next queries beside its sums, a wave of these would spill up to 63 registers)
     typename Wave<F32, CACHE, DIM, NT>::Tile x, y;
     auto begin = [&](const Item& i) { return i.span.base + i.u0 * kUnit + 32 * wave; };
     auto limit = [&](const Item& i) { return min(i.span.end, i.span.base + i.u1 * kUnit); };
@@ -636,10 +637,12 @@ __device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, It
             }
         }
         if (last) {
-            if (any) ask_q(then);
+            if constexpr (kAskEarly)
+                if (any) ask_q(then);
             end(it);
             w.reset();
             if (!any) return;
+            if constexpr (!kAskEarly) ask_q(then);
             w.split_q();
         }
         it = then;
@@ -858,7 +861,7 @@ int chunks_of(const moe_kv_cfg& kv, const moe_attn_cfg& c) {
 //   40 heads of 160, bf16 cache:     2 x 1000 16.4 / 23.0, 40 x 1000 105.3 / 106.6 (all full: 175.5 / 192.1)
 //   64 heads of 160, e4m3 cache:     4 x 700 21.0 / 18.0, 40 x 1000 143.9 / 129.3, 40 x 1500 185.6 / 168.4, but 64 over 8 of 192: 8 x 1000 17.0 / 20.8
 //   32 over 8 of 128, fp32 over bf16: 16 x 700 15.4 / 12.2, 40 x 1000 24.0 / 18.4, 200 x 1000 78.8 / 74.7 (all full: 141.5 / 142.8);
-//                                    40 heads of 160: 2 x 1000 21.7 / 25.6, 16 x 1000 67.7 / 50.3
+//                                    40 heads of 160: 4 x 1000 23.8 / 26.8, 8 x 1000 34.2 / 27.9 (all full: 48.1 / 54.7), 40 x 1000 117 / 112 (181 / 197)
 //   12 over 4 of 80, fp32 cache:     16 x 500 17.0 / 15.9, 64 x 700 28.0 / 23.1, 64 x 1000 31.9 / 28.9, but 4 x 700 14.5 / 21.9, 16 x 700 17.2 / 20.7, 200 x 1000
 //                                    65.8 / 71.0;  40 heads of 80: 40 x 700 93.6 / 93.7 (all full: 142.6 / 159.4)
 //   16 over 4 of 256, fp32 cache:    2 x 128 17.7 / 13.1, 16 x 256 41.1 / 31.7, 64 x 500 77.3 / 72.0, but 2 x 500 19.4 / 43.1, 16 x 384 42.0 / 48.4,
@@ -866,10 +869,8 @@ int chunks_of(const moe_kv_cfg& kv, const moe_attn_cfg& c) {
 int row_bytes_of(const moe_kv_cfg& kv) { return kv.head_dim * (kv.cache_dtype == MOE_F32 ? 4 : kv.cache_dtype == MOE_BF16 ? 2 : 1); }
 int whole_units(const moe_kv_cfg& kv, long items) {
     if (kv.cache_dtype == MOE_F32) return kv.head_dim > 128 && items < 256 ? 2 : 4;
-    if (kv.dtype == MOE_F32 || kv.head_dim > 128) {
-        const bool many = items >= (kv.head_dim > 128 ? 128 : 64);
-        return many && (kv.dtype == MOE_F32 || kv.cache_dtype == MOE_E4M3) ? 8 : 4;
-    }
+    if (kv.head_dim > 128) return kv.cache_dtype == MOE_E4M3 && items >= 128 ? 8 : 4;
+    if (kv.dtype == MOE_F32) return items >= 64 ? 8 : 4;
     const int row_bytes = row_bytes_of(kv);
     if (row_bytes > 128) return items >= 64 ? 8 : 6;
     return items >= 256 ? 16 : items >= 128 ? 12 : items >= 64 ? 8 : 6;
