@@ -41,6 +41,9 @@ EXTRA = {"ffn.hip": ["-mllvm", "-enable-misched=false", "-mllvm", "-amdgpu-atomi
 # brackets those regions with "; pipeline begin" / "; pipeline end"; the build reads the assembly and
 # refuses any scratch access between the two or inside an inner loop of these kernels.
 NO_SPILL = {"ffn.hip": "ffn_mfma"}
+# The attention kernels fill a wave's registers; what they keep in scratch memory (bytes a lane) has to stay next to nothing: 256, written and read once
+# per item, went with a fifth of the time.
+MOST_SCRATCH = {"attn.hip": ("attn_", 16)}
 # The parts of ffn.hip with tiles of more than 16 blocks, whose last sums are in assembly.
 TALL = (1, 3, 4)
 
@@ -292,14 +295,36 @@ def _built(src: str, part: int, suffix: str) -> str:
     return os.path.join(HERE, "_build", src.replace(".hip", f"_{part}{suffix}" if src in PARTS else suffix))
 
 
-def _check(src: str, part: int) -> None:
-    """Compiles the unit to assembly and refuses what the checks above refuse (ffn.hip's part 0 holds no pipelined loop)."""
+def _assembly(src: str, part: int) -> str:
     asm = _built(src, part, ".s")
     ra = subprocess.run([_hipcc(), *_flags(src, part), "-S", "--cuda-device-only", os.path.join(CSRC, src), "-o", asm],
                         capture_output=True, text=True)
     if ra.returncode != 0:
         raise RuntimeError(f"hipcc -S failed on {src}:\n{ra.stderr}")
-    text = open(asm).read()
+    return open(asm).read()
+
+
+def check_scratch(asm: str, kernel_pattern: str, most: int, what: str = "assembly") -> int:
+    """Raises if a kernel whose name contains kernel_pattern has more than `most` bytes of scratch memory a lane; the number of kernels."""
+    kernels = 0
+    for name, body in re.findall(r"^\s*\.amdhsa_kernel (\S+)$(.*?)^\s*\.end_amdhsa_kernel", asm, re.M | re.S):
+        if kernel_pattern not in name:
+            continue
+        size = re.search(r"\.amdhsa_private_segment_fixed_size (\d+)", body)
+        if size is None or int(size.group(1)) > most:
+            raise RuntimeError(f"{what}: {name} keeps {size and size.group(1)} bytes a lane in scratch memory (at most {most})")
+        kernels += 1
+    return kernels
+
+
+def _check_scratch(src: str) -> None:
+    if check_scratch(_assembly(src, 0), *MOST_SCRATCH[src], src) == 0:
+        raise RuntimeError(f"{src}: no kernel found to verify (printed in another way?)")
+
+
+def _check(src: str, part: int) -> None:
+    """Compiles the unit to assembly and refuses what the checks above refuse (ffn.hip's part 0 holds no pipelined loop)."""
+    text = _assembly(src, part)
     check_no_spill(text, NO_SPILL[src], src)
     loops = check_loads_in_flight(text, NO_SPILL[src], src), check_prologue_in_flight(text, NO_SPILL[src], src)
     m0 = check_m0_free(text, NO_SPILL[src], src)
@@ -342,6 +367,7 @@ def build(verbose: bool = False) -> str:
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
     with ThreadPoolExecutor(max_workers=8) as pool:
         checks = [pool.submit(_check, src, part) for src, part in UNITS if src in NO_SPILL]
+        checks += [pool.submit(_check_scratch, src) for src in MOST_SCRATCH]
         checks.append(pool.submit(_compile_args))
         objs = list(pool.map(lambda u: _compile(*u), UNITS))
         for c in checks:
