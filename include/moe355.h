@@ -329,7 +329,8 @@ int moe_layer_forward_timed(const moe_cfg* cfg, const void* x, const void* W_g, 
  *   x, residual [T, d], weight [d]: device, dtype.  residual may be NULL (s = x).
  *   sum [T, d]: dtype, s rounded; may be NULL.     y [T, d]: dtype, n rounded; may be NULL if q is not.
  *   q [T, d]: e4m3 bytes, q_scale [T, d / q_group] (q_group 0: [T, 1]): fp32; both NULL or neither.
- *     q_scale = max(max |n| over the row's group / 448, 2^-126), q = n / q_scale, so that q * q_scale stands for n.
+ *     q_scale = max(max |n| over the row's group / 448, 2^-126), q = n / q_scale, so that q * q_scale stands for n.  Both quotients are those
+ *     of fp32, rounded to the nearest, q once more to e4m3.
  *   x, residual, sum and y may be the same arrays (not: overlap in part).  All 16-byte aligned.
  */
 typedef struct moe_norm_cfg {
@@ -358,7 +359,7 @@ typedef struct moe_kv_cfg {
 
 /*
  * Writes n tokens' keys and values into their slots, rounded to cache_dtype to the nearest; MOE_E4M3: a row of a head is divided by its
- * scale max(max |row| / 448, 2^-126) first.
+ * scale max(max |row| / 448, 2^-126) first (quotients as moe_add_norm's; a row with an infinity is read back as NaN, all of it).
  *   k, v: device, dtype, token i's [heads, head_dim] at element i * stride (stride >= heads * head_dim, a multiple of 8).
  *   slots [n] int32: device; a slot outside of [0, pages * page_size) is no place: that token is not written.  No slot twice.
  */
@@ -373,9 +374,10 @@ int moe_kv_read(const moe_kv_cfg* cfg, int32_t n, const void* k_pages, const voi
  * Attention of one new token per sequence over the cache: query head j of sequence b attends, with the keys and values of head
  * j / (q_heads / heads), to the last `window` (0: all) of the sequence's first lens[b] tokens:
  *     l_t = scale * q . k_t,   out = sum_t exp(l_t) v_t / sum_t exp(l_t),   lse = log sum_t exp(l_t).
- * The cache is read once, its length split over the whole device and the parts joined; what lies beyond lens[b] or before the window
- * is not looked at, whatever it is.  Sums and statistics are fp32; with dtype MOE_BF16 the weights exp(l_t) enter the sum with 16
- * bits.  lens[b] = 0, or all l_t of a head -infinity: out 0 and lse -infinity.
+ * A key head's tokens are read once for each 16 of its query heads (32 with dtype MOE_BF16 and head_dim up to 128), long sequences split over the
+ * whole device and the parts joined; what lies beyond lens[b] or before the window is not looked at, whatever it is.  Sums and statistics
+ * are fp32; with dtype MOE_BF16 the weights exp(l_t) enter the sum with 16 bits, all else with all of its bits.  A token whose l_t is
+ * -infinity weighs nothing.  lens[b] = 0, or all l_t of a head -infinity: out 0 and lse -infinity.
  *   q: device, dtype, sequence b's [q_heads, head_dim] at element b * q_stride.  out [B, q_heads, head_dim]: dtype, written.
  *   table [B, table_pages] int32: device, the sequences' pages (only those of attended tokens are read; a page outside of
  *   [0, pages) is taken as the nearest one that exists).  lens [B] int32: device, taken as within [0, table_pages * page_size].
