@@ -395,6 +395,93 @@ int moe_attn_decode(const moe_kv_cfg* cfg, const moe_attn_cfg* attn, const void*
                     const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens,
                     void* out, float* lse, void* ws, void* stream);
 
+/*
+ * Attention whose scores are capped or get a bias by distance.  A query at place p of its sequence (its first token is 0) scores the key at place t
+ *     x_t = scale * q . k_t,    l_t = cap * tanh(x_t / cap) - slopes[h] * |p - t| + bias[h][clamp(p - t, -ahead, back) + ahead]
+ * for query head h; cap 0, slopes NULL and bias NULL leave their part out.
+ *   slopes [q_heads], bias [q_heads, back + ahead + 1]: device, fp32, finite.
+ */
+typedef struct moe_scores_cfg {
+    float cap;            /* 2^-100 to 2^100; 0: scores are not capped */
+    int32_t back;         /* distances to earlier keys that have a bias of their own, 0 to 65535; those further back take the last one's */
+    int32_t ahead;        /* the same for later keys (of no use to moe_attn_decode_scored, whose query is the last token) */
+} moe_scores_cfg;
+
+/*
+ * moe_attn_decode with such scores (p = lens[b] - 1); all else as there, the workspace too.  scores may be NULL if bias is: no cap.
+ */
+int moe_attn_decode_scored(const moe_kv_cfg* cfg, const moe_attn_cfg* attn, const moe_scores_cfg* scores, const void* q, int64_t q_stride,
+                           const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table,
+                           const int32_t* lens, const float* slopes, const float* bias, void* out, float* lse, void* ws, void* stream);
+
+/*
+ * Attention of many new tokens per sequence over the cache, which holds them already (moe_kv_write first): prompts, further pieces of
+ * prompts, several tokens at a time.  Sequence b's new tokens are its last starts[b + 1] - starts[b] of lens[b], rows starts[b] on of q and
+ * out; row i of them, at place p, attends to the places t of
+ *     max(first[i], p - window + 1) <= t < end[i],        first NULL: 0, end NULL: p + 1, window 0: no bound,  0 <= t < lens[b],
+ * which is a causal mask as it stands, a prefix with end = max(p + 1, prefix), documents with first = where the token's document begins,
+ * and a mask that lets all tokens see each other with end = lens[b].
+ * Scores as moe_scores_cfg says (NULL: plain ones; slopes and bias may be NULL).  What a row's mask hides is of no effect, whatever it is, NaN
+ * among it.  A row that sees no key, or whose l_t are all -infinity: out 0 and lse -infinity.  Sums and statistics are fp32; with dtype MOE_BF16 the weights exp(l_t) enter
+ * the sum of values rounded to bf16, after they have entered that of the weights.
+ *   q: device, dtype, token i's [q_heads, head_dim] at element i * q_stride.  out [tokens, q_heads, head_dim]: dtype.  lse [tokens, q_heads]: fp32,
+ *   may be NULL.  Rows before starts[0] and from starts[B] on are left as they were.
+ *   table, lens: as moe_attn_decode's.  starts [B + 1] int32: device, ascending, taken as within [0, tokens].  first, end [tokens] int32: device.
+ *   ws: moe_attn_prompt_workspace_bytes(), 256-byte aligned; nothing in it is kept between calls.
+ */
+typedef struct moe_prompt_cfg {
+    int32_t tokens;       /* rows of q and out; 0 <= tokens < 2^22 */
+    int32_t B;            /* sequences, 0 to 4096 */
+    int32_t q_heads;      /* a multiple of heads, at most 1024 */
+    int32_t table_pages;  /* pages a row of table has room for; table_pages * page_size <= 2^24 */
+    int32_t window;       /* 0: no bound */
+    float scale;          /* 0: 1 / sqrt(head_dim) */
+} moe_prompt_cfg;
+int moe_attn_prompt_workspace_bytes(const moe_kv_cfg* cfg, const moe_prompt_cfg* prompt, size_t* bytes);
+int moe_attn_prompt(const moe_kv_cfg* cfg, const moe_prompt_cfg* prompt, const moe_scores_cfg* scores, const void* q, int64_t q_stride,
+                    const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table,
+                    const int32_t* lens, const int32_t* starts, const int32_t* first, const int32_t* end, const float* slopes,
+                    const float* bias, void* out, float* lse, void* ws, void* stream);
+
+/*
+ * Rotary positions: of each head's first rot_dim columns, pair i = 0 .. rot_dim / 2 - 1, columns (i, i + rot_dim / 2) or with MOE_PAIRS_NEIGHBOURS
+ * (2 i, 2 i + 1), is turned by the angle positions[token] * freqs[i]:
+ *     (a, b) -> amplitude * (a cos - b sin, a sin + b cos);    columns from rot_dim on stay as they are.
+ * Angles are fp64, their sines and cosines fp32, results rounded once.  Negative positions turn back.
+ */
+enum { MOE_PAIRS_HALF = 0, MOE_PAIRS_NEIGHBOURS = 1 };
+enum { MOE_ROPE_PLAIN = 0, MOE_ROPE_LINEAR = 1, MOE_ROPE_BASE = 2, MOE_ROPE_PARTS = 3 };
+typedef struct moe_rope_cfg {
+    int32_t q_heads;      /* 0 to 1024 */
+    int32_t k_heads;      /* 0 to 1024 */
+    int32_t head_dim;     /* a multiple of 16, 16 to 256 */
+    int32_t rot_dim;      /* even, 2 to head_dim */
+    int32_t dtype;        /* of q and k: MOE_F32 | MOE_BF16 */
+    int32_t pairs;        /* MOE_PAIRS_HALF | MOE_PAIRS_NEIGHBOURS */
+    int32_t scaling;      /* what moe_rope_frequencies makes of factor */
+    int32_t original;     /* MOE_ROPE_PARTS: tokens that the model was trained on */
+    float base;           /* > 0, usually 10000 */
+    float factor;         /* > 0; by how much the context is longer than the one trained on */
+    float slow, fast;     /* MOE_ROPE_PARTS: turns over `original` tokens, 0 <= slow < fast */
+    float amplitude;      /* finite; 0: 1 */
+} moe_rope_cfg;
+
+/*
+ * The frequencies, radians per position, freqs [rot_dim / 2]: host memory.  With f_i = base^(-2 i / rot_dim):
+ *   MOE_ROPE_PLAIN f_i;  MOE_ROPE_LINEAR f_i / factor;  MOE_ROPE_BASE those of the base  base * factor^(rot_dim / (rot_dim - 2));
+ *   MOE_ROPE_PARTS  keep f_i + (1 - keep) f_i / factor  with  keep = (original f_i / 2 pi - slow) / (fast - slow)  within [0, 1].
+ * Pure host function.  (moe_rope takes any frequencies; these are the usual ones.)
+ */
+int moe_rope_frequencies(const moe_rope_cfg* cfg, double* freqs);
+
+/*
+ *   positions [n] int32, freqs [rot_dim / 2] fp64: device.
+ *   q, q_out [n, q_heads, head_dim], k, k_out [n, k_heads, head_dim]: device, dtype, token i's at element i * stride (strides as moe_kv_write's).
+ *   q_out may be q itself (with the same stride), not overlap it otherwise; q and q_out may both be NULL (no queries); the same for k.
+ */
+int moe_rope(const moe_rope_cfg* cfg, int32_t n, const int32_t* positions, const double* freqs, const void* q, int64_t q_stride, void* q_out,
+             int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

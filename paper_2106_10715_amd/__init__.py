@@ -10,4 +10,5 @@ from .binding import (  # noqa: F401
     moe_route, moe_workspace_bytes, moe_gate_bytes, moe_pack_gate, moe_layer_forward_timed, Timer, STAGES, TIME_STAGES,
     TIME_UP_KERNEL, moe_schedule_order, moe_plan_slots, moe_stream_slots_that_fit, ORDER_ASCENDING, ORDER_GREEDY, GATE_TOPK, GATE_HASH,
     MOE_E4M3, NormCfg, KvCfg, AttnCfg, moe_add_norm, moe_kv_write, moe_kv_read, moe_attn_workspace_bytes, moe_attn_decode,
+    ScoresCfg, PromptCfg, RopeCfg, moe_attn_decode_scored, moe_attn_prompt_workspace_bytes, moe_attn_prompt, moe_rope_frequencies, moe_rope,
 )

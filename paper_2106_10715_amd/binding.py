@@ -77,6 +77,43 @@ class AttnCfg(C.Structure):
         return cls(B, q_heads, table_pages, window, scale)
 
 
+class ScoresCfg(C.Structure):
+    """moe_scores_cfg: scores capped by a tanh or biased by distance."""
+    _fields_ = [("cap", C.c_float), ("back", C.c_int32), ("ahead", C.c_int32)]
+
+    @classmethod
+    def make(cls, cap=0.0, back=0, ahead=0) -> "ScoresCfg":
+        return cls(cap, back, ahead)
+
+
+class PromptCfg(C.Structure):
+    """moe_prompt_cfg: the tokens, sequences and query heads of one moe_attn_prompt."""
+    _fields_ = [("tokens", C.c_int32), ("B", C.c_int32), ("q_heads", C.c_int32), ("table_pages", C.c_int32), ("window", C.c_int32),
+                ("scale", C.c_float)]
+
+    @classmethod
+    def make(cls, tokens, B, q_heads, table_pages, scale=0.0, window=0) -> "PromptCfg":
+        return cls(tokens, B, q_heads, table_pages, window, scale)
+
+
+_PAIRS = {"half": 0, "neighbours": 1}
+_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+class RopeCfg(C.Structure):
+    """moe_rope_cfg: heads, columns, pairs and frequencies of moe_rope."""
+    _fields_ = [("q_heads", C.c_int32), ("k_heads", C.c_int32), ("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("dtype", C.c_int32),
+                ("pairs", C.c_int32), ("scaling", C.c_int32), ("original", C.c_int32), ("base", C.c_float), ("factor", C.c_float),
+                ("slow", C.c_float), ("fast", C.c_float), ("amplitude", C.c_float)]
+
+    @classmethod
+    def make(cls, q_heads, k_heads, head_dim, rot_dim=None, dtype="bf16", pairs="half", base=10000.0, scaling="none", factor=1.0,
+             original=0, slow=1.0, fast=32.0, amplitude=1.0) -> "RopeCfg":
+        code = _CODE[dtype] if isinstance(dtype, str) else int(dtype)
+        return cls(q_heads, k_heads, head_dim, head_dim if rot_dim is None else rot_dim, code, _PAIRS[pairs] if isinstance(pairs, str) else int(pairs),
+                   _SCALING[scaling] if isinstance(scaling, str) else int(scaling), original, base, factor, slow, fast, amplitude)
+
+
 def lib_path() -> str:
     """The library next to this file, or the build named by the environment variable MOE355_LIB."""
     return os.environ.get("MOE355_LIB") or os.path.join(_HERE, "libmoe355.so")
@@ -129,6 +166,11 @@ def lib() -> C.CDLL:
             "moe_kv_read": [p, C.c_int32, p, p, p, p, p, p, C.c_int64, p, C.c_int64, p],
             "moe_attn_workspace_bytes": [p, p, C.POINTER(C.c_size_t)],
             "moe_attn_decode": [p, p, p, C.c_int64, p, p, p, p, p, p, p, p, p, p],
+            "moe_attn_decode_scored": [p, p, p, p, C.c_int64, *[p] * 12],
+            "moe_attn_prompt_workspace_bytes": [p, p, C.POINTER(C.c_size_t)],
+            "moe_attn_prompt": [p, p, p, p, C.c_int64, *[p] * 15],
+            "moe_rope_frequencies": [p, p],
+            "moe_rope": [p, C.c_int32, p, p, p, C.c_int64, p, C.c_int64, p, C.c_int64, p, C.c_int64, p],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -160,6 +202,9 @@ def _stream(stream: Optional[torch.cuda.Stream]):
     return stream.cuda_stream if stream is not None else _raw_stream(torch.cuda.current_device())
 
 
+_SIZES = {"attn_prompt": "moe_attn_prompt_workspace_bytes"}     # what says how large a call's workspace is; else moe_attn_workspace_bytes
+
+
 def _native(name: str, *args, stream=None) -> bool:
     """The call through _args.  False where an argument is not as it has to be: the caller then says which and why, and calls nothing."""
     global _ARGS
@@ -170,7 +215,7 @@ def _native(name: str, *args, stream=None) -> bool:
         except ImportError as e:
             raise MoeError(f"_args is not built: run python -m paper_2106_10715_amd.build ({e})")
         _ARGS = _args
-    rc = getattr(_ARGS, name)(_FN["moe_" + name], _FN["moe_attn_workspace_bytes"], *args, None if stream is None else stream.cuda_stream)
+    rc = getattr(_ARGS, name)(_FN["moe_" + name], _FN[_SIZES.get(name, "moe_attn_workspace_bytes")], *args, None if stream is None else stream.cuda_stream)
     if rc is None:
         return False
     _check(rc)
@@ -466,16 +511,103 @@ def moe_attn_decode(cfg: KvCfg, attn: AttnCfg, q, k_pages, v_pages, k_scales, v_
     dt = _TORCH[_description(cfg, KvCfg).dtype]
     B, heads = _description(attn, AttnCfg, "attn").B, attn.q_heads
     _head_rows(q, "q", dt, B, heads, cfg.head_dim)
-    if ws is not None:
-        if _tensor(ws, "ws").nbytes < moe_attn_workspace_bytes(cfg, attn):
-            raise MoeError("ws is smaller than moe_attn_workspace_bytes")
-        if not ws.is_contiguous():
-            raise MoeError("ws must be contiguous")
-        if not ws.is_cuda:
-            raise MoeError("ws must be in device memory")
+    _workspace(ws, lambda: moe_attn_workspace_bytes(cfg, attn), "moe_attn_workspace_bytes")
     _cache(cfg, k_pages, v_pages, k_scales, v_scales)
     _array(table, "table", torch.int32, B * attn.table_pages)
     _array(lens, "lens", torch.int32, B)
     _array(out, "out", dt, B * heads * cfg.head_dim)
     _array(lse, "lse", torch.float32, B * heads)
     _refused("moe_attn_decode")
+
+
+def _workspace(ws, need, what: str) -> None:
+    if ws is None:
+        return
+    if _tensor(ws, "ws").nbytes < need():
+        raise MoeError(f"ws is smaller than {what}")
+    if not ws.is_contiguous():
+        raise MoeError("ws must be contiguous")
+    if not ws.is_cuda:
+        raise MoeError("ws must be in device memory")
+
+
+def _scores(scores: Optional[ScoresCfg], heads: int, slopes, bias) -> None:
+    if scores is not None:
+        _description(scores, ScoresCfg, "scores")
+    distances = 1 if scores is None else scores.back + scores.ahead + 1
+    _array(slopes, "slopes", torch.float32, heads)
+    _array(bias, "bias", torch.float32, heads * distances)
+
+
+def _here(*tensors) -> None:
+    """Refuses tensors of another device than the current one, whose stream the call is put on."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise MoeError(f"a tensor is on {t.device}, the current device is {torch.cuda.current_device()}")
+
+
+def moe_attn_decode_scored(cfg: KvCfg, attn: AttnCfg, scores: Optional[ScoresCfg], q, k_pages, v_pages, k_scales, v_scales, table, lens, slopes,
+                           bias, out, lse, ws, stream=None) -> None:
+    if _native("attn_decode_scored", cfg, attn, scores, q, k_pages, v_pages, k_scales, v_scales, table, lens, slopes, bias, out, lse, ws,
+               stream=stream):
+        return
+    dt = _TORCH[_description(cfg, KvCfg).dtype]
+    B, heads = _description(attn, AttnCfg, "attn").B, attn.q_heads
+    _scores(scores, heads, slopes, bias)
+    _head_rows(q, "q", dt, B, heads, cfg.head_dim)
+    _workspace(ws, lambda: moe_attn_workspace_bytes(cfg, attn), "moe_attn_workspace_bytes")
+    _cache(cfg, k_pages, v_pages, k_scales, v_scales)
+    _array(table, "table", torch.int32, B * attn.table_pages)
+    _array(lens, "lens", torch.int32, B)
+    _array(out, "out", dt, B * heads * cfg.head_dim)
+    _array(lse, "lse", torch.float32, B * heads)
+    _here(q, k_pages, v_pages, k_scales, v_scales, table, lens, slopes, bias, out, lse, ws)
+    _refused("moe_attn_decode_scored")
+
+
+def moe_attn_prompt_workspace_bytes(cfg: KvCfg, prompt: PromptCfg) -> int:
+    n = C.c_size_t(0)
+    _check(lib().moe_attn_prompt_workspace_bytes(C.addressof(cfg), C.addressof(prompt), C.byref(n)))
+    return n.value
+
+
+def moe_attn_prompt(cfg: KvCfg, prompt: PromptCfg, scores: Optional[ScoresCfg], q, k_pages, v_pages, k_scales, v_scales, table, lens, starts,
+                    first, end, slopes, bias, out, lse, ws, stream=None) -> None:
+    if _native("attn_prompt", cfg, prompt, scores, q, k_pages, v_pages, k_scales, v_scales, table, lens, starts, first, end, slopes, bias, out, lse,
+               ws, stream=stream):
+        return
+    dt = _TORCH[_description(cfg, KvCfg).dtype]
+    n, heads = _description(prompt, PromptCfg, "prompt").tokens, prompt.q_heads
+    _scores(scores, heads, slopes, bias)
+    _head_rows(q, "q", dt, n, heads, cfg.head_dim)
+    _workspace(ws, lambda: moe_attn_prompt_workspace_bytes(cfg, prompt), "moe_attn_prompt_workspace_bytes")
+    _cache(cfg, k_pages, v_pages, k_scales, v_scales)
+    for t, name, numel in ((table, "table", prompt.B * prompt.table_pages), (lens, "lens", prompt.B), (starts, "starts", prompt.B + 1),
+                           (first, "first", n), (end, "end", n)):
+        _array(t, name, torch.int32, numel)
+    _array(out, "out", dt, n * heads * cfg.head_dim)
+    _array(lse, "lse", torch.float32, n * heads)
+    _here(q, k_pages, v_pages, k_scales, v_scales, table, lens, starts, first, end, slopes, bias, out, lse, ws)
+    _refused("moe_attn_prompt")
+
+
+def moe_rope_frequencies(cfg: RopeCfg) -> torch.Tensor:
+    """Radians per position of each pair, fp64, in host memory; moe_rope takes them from device memory."""
+    freqs = torch.empty(max(_description(cfg, RopeCfg).rot_dim, 0) // 2, dtype=torch.float64)
+    _check(lib().moe_rope_frequencies(C.addressof(cfg), freqs.data_ptr()))
+    return freqs
+
+
+def moe_rope(cfg: RopeCfg, positions, freqs, q, q_out, k=None, k_out=None, stream=None) -> None:
+    if _native("rope", cfg, positions, freqs, q, q_out, k, k_out, stream=stream):
+        return
+    dt = _TORCH[_description(cfg, RopeCfg).dtype]
+    if positions is None:
+        raise MoeError("positions is NULL")
+    n = _tensor(positions, "positions").numel()
+    for t, name, heads in ((q, "q", cfg.q_heads), (q_out, "q_out", cfg.q_heads), (k, "k", cfg.k_heads), (k_out, "k_out", cfg.k_heads)):
+        _head_rows(t, name, dt, n, heads, cfg.head_dim)
+    _array(freqs, "freqs", torch.float64, cfg.rot_dim // 2)
+    _array(positions, "positions", torch.int32, n)
+    _here(positions, freqs, q, q_out, k, k_out)
+    _refused("moe_rope")

@@ -14,9 +14,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe355.so")
 ARGS = os.path.join(HERE, "_args.so")
 SOURCES = ["api.hip", "route.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "combine.hip", "schedule.hip",
-           "api_decoder.hip", "norm.hip", "kv.hip", "attn.hip"]
-# ffn.hip is compiled in parts, side by side: each of its large kernels is an object of its own.
-PARTS = {"ffn.hip": 5}
+           "api_decoder.hip", "norm.hip", "kv.hip", "attn.hip", "rope.hip", "prompt.hip"]
+# ffn.hip is compiled in parts, side by side: each of its large kernels is an object of its own.  So are attn.hip's kernels with and without scores of their own.
+PARTS = {"ffn.hip": 5, "attn.hip": 2}
 UNITS = [(src, part) for src in SOURCES for part in range(PARTS.get(src, 1))]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -288,7 +288,7 @@ def check_prologue_in_flight(asm: str, kernel_pattern: str, what: str = "assembl
 
 
 def _flags(src: str, part: int) -> list:
-    return [*FLAGS, *EXTRA.get(src, []), *([f"-DFFN_PART={part}"] if src in PARTS else [])]
+    return [*FLAGS, *EXTRA.get(src, []), *([f"-D{src.split('.')[0].upper()}_PART={part}"] if src in PARTS else [])]
 
 
 def _built(src: str, part: int, suffix: str) -> str:
@@ -318,8 +318,9 @@ def check_scratch(asm: str, kernel_pattern: str, most: int, what: str = "assembl
 
 
 def _check_scratch(src: str) -> None:
-    if check_scratch(_assembly(src, 0), *MOST_SCRATCH[src], src) == 0:
-        raise RuntimeError(f"{src}: no kernel found to verify (printed in another way?)")
+    for part in range(PARTS.get(src, 1)):
+        if check_scratch(_assembly(src, part), *MOST_SCRATCH[src], src) == 0:
+            raise RuntimeError(f"{src}: no kernel found to verify (printed in another way?)")
 
 
 def _check(src: str, part: int) -> None:

@@ -73,6 +73,56 @@ int check_rows(const void* p, int64_t stride, int64_t width, const char* name) {
     return MOE_OK;
 }
 
+// What moe_scores_cfg and its arrays say; the arrays' addresses are the caller's.
+int scores_of(const moe_scores_cfg* c, const float* slopes, const float* bias, Scores* out) {
+    *out = Scores{0.f, 0, 0, slopes, bias};
+    if (c == nullptr) {
+        if (bias != nullptr) return fail(MOE_ERR_INVALID_ARG, "a bias needs scores, which say what distances it is for");
+        return MOE_OK;
+    }
+    if (c->cap != 0.f && !(c->cap >= 0x1p-100f && c->cap <= 0x1p100f)) return fail(MOE_ERR_INVALID_ARG, "cap must be 0 or in [2^-100, 2^100]");
+    if (c->back < 0 || c->back > 65535) return fail(MOE_ERR_INVALID_ARG, "back must be in [0, 65535] (got %d)", c->back);
+    if (c->ahead < 0 || c->ahead > 65535) return fail(MOE_ERR_INVALID_ARG, "ahead must be in [0, 65535] (got %d)", c->ahead);
+    out->cap = c->cap;
+    out->back = c->back;
+    out->ahead = c->ahead;
+    return MOE_OK;
+}
+
+int check_prompt(const moe_kv_cfg* kv, const moe_prompt_cfg* c) {
+    if (int rc = check_kv(kv)) return rc;
+    if (c == nullptr) return fail(MOE_ERR_INVALID_ARG, "prompt is NULL");
+    if (c->tokens < 0 || c->tokens >= 1 << 22) return fail(MOE_ERR_INVALID_ARG, "tokens must be in [0, 2^22) (got %d)", c->tokens);
+    const moe_attn_cfg as{c->B, c->q_heads, c->table_pages, c->window, c->scale};
+    return check_attn(kv, &as);
+}
+
+int check_rope(const moe_rope_cfg* c) {
+    if (c == nullptr) return fail(MOE_ERR_INVALID_ARG, "cfg is NULL");
+    if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "dtype must be MOE_F32 or MOE_BF16");
+    if (c->q_heads < 0 || c->q_heads > 1024) return fail(MOE_ERR_INVALID_ARG, "q_heads must be in [0, 1024] (got %d)", c->q_heads);
+    if (c->k_heads < 0 || c->k_heads > 1024) return fail(MOE_ERR_INVALID_ARG, "k_heads must be in [0, 1024] (got %d)", c->k_heads);
+    if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16 != 0)
+        return fail(MOE_ERR_INVALID_ARG, "head_dim must be a multiple of 16 in [16, 256] (got %d)", c->head_dim);
+    if (c->rot_dim < 2 || c->rot_dim > c->head_dim || c->rot_dim % 2 != 0)
+        return fail(MOE_ERR_INVALID_ARG, "rot_dim must be even and in [2, head_dim] (got %d)", c->rot_dim);
+    if (c->pairs != MOE_PAIRS_HALF && c->pairs != MOE_PAIRS_NEIGHBOURS)
+        return fail(MOE_ERR_INVALID_ARG, "pairs must be MOE_PAIRS_HALF or MOE_PAIRS_NEIGHBOURS (got %d)", c->pairs);
+    if (!isfinite(c->amplitude)) return fail(MOE_ERR_INVALID_ARG, "amplitude must be finite");
+    return MOE_OK;
+}
+
+// One side of moe_rope.
+int check_turned(const void* in, int64_t in_stride, const void* out, int64_t out_stride, int heads, int dim, const char* name, const char* out_name) {
+    if (in == nullptr && out == nullptr) return MOE_OK;
+    if (heads == 0) return fail(MOE_ERR_INVALID_ARG, "%s has no heads and must be NULL", name);
+    const int64_t width = static_cast<int64_t>(heads) * dim;
+    if (int rc = check_rows(in, in_stride, width, name)) return rc;
+    if (int rc = check_rows(out, out_stride, width, out_name)) return rc;
+    if (in == out && in_stride != out_stride) return fail(MOE_ERR_INVALID_ARG, "%s in its own place must keep its stride", name);
+    return MOE_OK;
+}
+
 int check_n(int32_t n) {
     if (n < 0) return fail(MOE_ERR_INVALID_ARG, "n must be >= 0 (got %d)", n);
     return MOE_OK;
@@ -139,6 +189,85 @@ int moe_attn_decode(const moe_kv_cfg* cfg, const moe_attn_cfg* attn, const void*
     if ((reinterpret_cast<uintptr_t>(ws) & 255) != 0) return fail(MOE_ERR_WORKSPACE, "ws must be 256-byte aligned");
     return launch_attn_decode(*cfg, *attn, q, q_stride, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws,
                               static_cast<hipStream_t>(stream));
+}
+
+int moe_attn_decode_scored(const moe_kv_cfg* cfg, const moe_attn_cfg* attn, const moe_scores_cfg* scores, const void* q, int64_t q_stride,
+                           const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table,
+                           const int32_t* lens, const float* slopes, const float* bias, void* out, float* lse, void* ws, void* stream) {
+    if (int rc = check_attn(cfg, attn)) return rc;
+    Scores sc;
+    if (int rc = scores_of(scores, slopes, bias, &sc)) return rc;
+    if (int rc = check_pages(*cfg, k_pages, v_pages, k_scales, v_scales)) return rc;
+    if (attn->B == 0) return MOE_OK;
+    if (int rc = check_rows(q, q_stride, static_cast<int64_t>(attn->q_heads) * cfg->head_dim, "q")) return rc;
+    REQUIRE(table, "table"); REQUIRE(lens, "lens"); REQUIRE(out, "out"); REQUIRE(ws, "ws");
+    REQUIRE_ALIGNED(out, "out");
+    if ((reinterpret_cast<uintptr_t>(ws) & 255) != 0) return fail(MOE_ERR_WORKSPACE, "ws must be 256-byte aligned");
+    const auto stream_ = static_cast<hipStream_t>(stream);
+    if (!sc.any()) return launch_attn_decode(*cfg, *attn, q, q_stride, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws, stream_);
+    return launch_attn_decode_scored(*cfg, *attn, sc, q, q_stride, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws, stream_);
+}
+
+int moe_attn_prompt_workspace_bytes(const moe_kv_cfg* cfg, const moe_prompt_cfg* prompt, size_t* bytes) {
+    if (int rc = check_prompt(cfg, prompt)) return rc;
+    REQUIRE(bytes, "bytes");
+    *bytes = attn_prompt_workspace_bytes(*cfg, *prompt);
+    return MOE_OK;
+}
+
+int moe_attn_prompt(const moe_kv_cfg* cfg, const moe_prompt_cfg* prompt, const moe_scores_cfg* scores, const void* q, int64_t q_stride,
+                    const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table,
+                    const int32_t* lens, const int32_t* starts, const int32_t* first, const int32_t* end, const float* slopes,
+                    const float* bias, void* out, float* lse, void* ws, void* stream) {
+    if (int rc = check_prompt(cfg, prompt)) return rc;
+    Scores sc;
+    if (int rc = scores_of(scores, slopes, bias, &sc)) return rc;
+    if (int rc = check_pages(*cfg, k_pages, v_pages, k_scales, v_scales)) return rc;
+    if (prompt->B == 0 || prompt->tokens == 0) return MOE_OK;
+    if (int rc = check_rows(q, q_stride, static_cast<int64_t>(prompt->q_heads) * cfg->head_dim, "q")) return rc;
+    REQUIRE(table, "table"); REQUIRE(lens, "lens"); REQUIRE(starts, "starts"); REQUIRE(out, "out"); REQUIRE(ws, "ws");
+    REQUIRE_ALIGNED(out, "out");
+    if ((reinterpret_cast<uintptr_t>(ws) & 255) != 0) return fail(MOE_ERR_WORKSPACE, "ws must be 256-byte aligned");
+    return launch_attn_prompt(*cfg, *prompt, sc, q, q_stride, k_pages, v_pages, k_scales, v_scales, table, lens, starts, first, end, out, lse, ws,
+                              static_cast<hipStream_t>(stream));
+}
+
+int moe_rope_frequencies(const moe_rope_cfg* cfg, double* freqs) {
+    if (int rc = check_rope(cfg)) return rc;
+    REQUIRE(freqs, "freqs");
+    if (!(cfg->base > 0.f) || !isfinite(cfg->base)) return fail(MOE_ERR_INVALID_ARG, "base must be positive and finite");
+    if (cfg->scaling < MOE_ROPE_PLAIN || cfg->scaling > MOE_ROPE_PARTS) return fail(MOE_ERR_INVALID_ARG, "scaling must be one of MOE_ROPE_* (got %d)", cfg->scaling);
+    if (cfg->scaling != MOE_ROPE_PLAIN && (!(cfg->factor > 0.f) || !isfinite(cfg->factor))) return fail(MOE_ERR_INVALID_ARG, "factor must be positive and finite");
+    if (cfg->scaling == MOE_ROPE_PARTS && (cfg->original < 1 || !(cfg->slow >= 0.f) || !(cfg->fast > cfg->slow) || !isfinite(cfg->fast)))
+        return fail(MOE_ERR_INVALID_ARG, "parts need original >= 1 and 0 <= slow < fast");
+    const double rot = cfg->rot_dim, factor = cfg->factor;
+    // (with one pair there is but one frequency, 1, and no base that changes it)
+    const double base = cfg->scaling == MOE_ROPE_BASE && cfg->rot_dim > 2 ? cfg->base * pow(factor, rot / (rot - 2)) : cfg->base;
+    for (int i = 0; i < cfg->rot_dim / 2; ++i) {
+        double f = pow(base, -2.0 * i / rot);
+        if (cfg->scaling == MOE_ROPE_LINEAR) f /= factor;
+        if (cfg->scaling == MOE_ROPE_PARTS) {
+            const double turns = cfg->original * f / (2.0 * M_PI);
+            const double keep = fmin(fmax((turns - cfg->slow) / (static_cast<double>(cfg->fast) - cfg->slow), 0.0), 1.0);
+            f = keep * f + (1.0 - keep) * f / factor;
+        }
+        freqs[i] = f;
+    }
+    return MOE_OK;
+}
+
+int moe_rope(const moe_rope_cfg* cfg, int32_t n, const int32_t* positions, const double* freqs, const void* q, int64_t q_stride, void* q_out,
+             int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, void* stream) {
+    if (int rc = check_rope(cfg)) return rc;
+    if (int rc = check_n(n)) return rc;
+    REQUIRE(freqs, "freqs");
+    if (n == 0) return MOE_OK;
+    if (int rc = check_turned(q, q_stride, q_out, q_out_stride, cfg->q_heads, cfg->head_dim, "q", "q_out")) return rc;
+    if (int rc = check_turned(k, k_stride, k_out, k_out_stride, cfg->k_heads, cfg->head_dim, "k", "k_out")) return rc;
+    REQUIRE(positions, "positions");
+    if (q == nullptr && k == nullptr) return MOE_OK;
+    return launch_rope(*cfg, n, positions, freqs, RopeSide{q, q_out, q_stride, q_out_stride, q == nullptr ? 0 : cfg->q_heads},
+                       RopeSide{k, k_out, k_stride, k_out_stride, k == nullptr ? 0 : cfg->k_heads}, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

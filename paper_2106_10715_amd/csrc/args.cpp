@@ -5,6 +5,7 @@
 #include <Python.h>
 #include <string.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -16,6 +17,7 @@ namespace {
 struct Args {
     PyObject* const* at;
     bool ok = true;
+    int device = -1;        // if not, the one that all tensors have to be on
 
     template <typename F>
     F* function(int i) { return reinterpret_cast<F*>(PyLong_AsVoidPtr(at[i])); }
@@ -35,6 +37,16 @@ struct Args {
         PyBuffer_Release(&b);
         return c;
     }
+    // All tensors from here on have to be on the current device, on whose stream the call is put (calls without any device: refused for their tensors).
+    void only_here() { device = c10::hip::device_count() > 0 ? c10::hip::current_device() : 0; }
+    // A description that may be None; whether it is there.
+    template <typename C>
+    bool optional(int i, C* c) {
+        *c = C{};
+        if (at[i] == Py_None) return false;
+        *c = description<C>(i);
+        return true;
+    }
     const at::Tensor* tensor(int i) {
         if (at[i] == Py_None) return nullptr;
         if (!THPVariable_Check(at[i])) {
@@ -42,7 +54,7 @@ struct Args {
             return nullptr;
         }
         const at::Tensor& t = THPVariable_Unpack(at[i]);
-        if (!t.is_cuda()) ok = false;
+        if (!t.is_cuda() || (device >= 0 && t.get_device() != device)) ok = false;
         return &t;
     }
     // A contiguous device tensor of this type and size; None stays a null pointer (the library says whether it may be).
@@ -178,6 +190,97 @@ PyObject* attn_decode(Args a) {
     return outcome(a, [&] { return f(&c, &t, q, qs, p.k, p.v, p.k_scales, p.v_scales, table, lens, out, static_cast<float*>(lse), ws, stream); });
 }
 
+// Scores, and the arrays that go with them: slopes, bias.
+struct ScoreArgs {
+    moe_scores_cfg c;
+    const moe_scores_cfg* cfg;
+    const float *slopes, *bias;
+    ScoreArgs(Args& a, int at_cfg, int at_slopes, int64_t q_heads) {
+        cfg = a.optional(at_cfg, &c) ? &c : nullptr;
+        slopes = static_cast<const float*>(a.array(at_slopes, at::kFloat, q_heads));
+        const int64_t distances = static_cast<int64_t>(c.back) + c.ahead + 1;
+        bias = static_cast<const float*>(a.array(at_slopes + 1, at::kFloat, q_heads * distances));
+    }
+};
+
+// The workspace: a contiguous tensor of at least `need` bytes; `known`: whether that is known.
+void* workspace(Args& a, int i, bool known, size_t need) {
+    const at::Tensor* w = a.tensor(i);
+    if (w == nullptr) return nullptr;
+    if (!a.ok || !w->is_contiguous() || !known || w->nbytes() < need) {
+        a.ok = false;
+        return nullptr;
+    }
+    return w->data_ptr();
+}
+
+// (function, moe_attn_workspace_bytes, cfg, attn, scores, q, k_pages, v_pages, k_scales, v_scales, table, lens, slopes, bias, out, lse, ws, stream)
+PyObject* attn_decode_scored(Args a) {
+    a.only_here();
+    const auto c = a.description<moe_kv_cfg>(2);
+    const auto t = a.description<moe_attn_cfg>(3);
+    const auto dt = a.type(c.dtype);
+    const int64_t heads = static_cast<int64_t>(t.B) * t.q_heads;
+    const ScoreArgs sc(a, 4, 12, t.q_heads);
+    int64_t qs;
+    void* q = a.rows(5, dt, t.B, t.q_heads, c.head_dim, &qs);
+    const Pages p(a, c, 6);
+    auto* table = static_cast<const int32_t*>(a.array(10, at::kInt, static_cast<int64_t>(t.B) * t.table_pages));
+    auto* lens = static_cast<const int32_t*>(a.array(11, at::kInt, t.B));
+    void *out = a.array(14, dt, heads * c.head_dim), *lse = a.array(15, at::kFloat, heads);
+    size_t need = 0;
+    const bool known = a.ok && a.function<decltype(moe_attn_workspace_bytes)>(1)(&c, &t, &need) == 0;
+    void* ws = workspace(a, 16, known, need);
+    void* stream = a.stream(17);
+    auto* f = a.function<decltype(moe_attn_decode_scored)>(0);
+    return outcome(a, [&] {
+        return f(&c, &t, sc.cfg, q, qs, p.k, p.v, p.k_scales, p.v_scales, table, lens, sc.slopes, sc.bias, out, static_cast<float*>(lse), ws, stream);
+    });
+}
+
+// (function, moe_attn_prompt_workspace_bytes, cfg, prompt, scores, q, k_pages, v_pages, k_scales, v_scales, table, lens, starts, first, end, slopes, bias,
+// out, lse, ws, stream)
+PyObject* attn_prompt(Args a) {
+    a.only_here();
+    const auto c = a.description<moe_kv_cfg>(2);
+    const auto t = a.description<moe_prompt_cfg>(3);
+    const auto dt = a.type(c.dtype);
+    const int64_t heads = static_cast<int64_t>(t.tokens) * t.q_heads;
+    const ScoreArgs sc(a, 4, 15, t.q_heads);
+    int64_t qs;
+    void* q = a.rows(5, dt, t.tokens, t.q_heads, c.head_dim, &qs);
+    const Pages p(a, c, 6);
+    auto ints = [&](int i, int64_t n) { return static_cast<const int32_t*>(a.array(i, at::kInt, n)); };
+    auto *table = ints(10, static_cast<int64_t>(t.B) * t.table_pages), *lens = ints(11, t.B), *starts = ints(12, static_cast<int64_t>(t.B) + 1);
+    auto *first = ints(13, t.tokens), *end = ints(14, t.tokens);
+    void *out = a.array(17, dt, heads * c.head_dim), *lse = a.array(18, at::kFloat, heads);
+    size_t need = 0;
+    const bool known = a.ok && a.function<decltype(moe_attn_prompt_workspace_bytes)>(1)(&c, &t, &need) == 0;
+    void* ws = workspace(a, 19, known, need);
+    void* stream = a.stream(20);
+    auto* f = a.function<decltype(moe_attn_prompt)>(0);
+    return outcome(a, [&] {
+        return f(&c, &t, sc.cfg, q, qs, p.k, p.v, p.k_scales, p.v_scales, table, lens, starts, first, end, sc.slopes, sc.bias, out,
+                 static_cast<float*>(lse), ws, stream);
+    });
+}
+
+// (function, -, cfg, positions, freqs, q, q_out, k, k_out, stream)
+PyObject* rope(Args a) {
+    a.only_here();
+    const auto c = a.description<moe_rope_cfg>(2);
+    const auto dt = a.type(c.dtype);
+    const int64_t n = length(a, 3);
+    auto* positions = static_cast<const int32_t*>(a.array(3, at::kInt, n));
+    auto* freqs = static_cast<const double*>(a.array(4, at::kDouble, c.rot_dim / 2));
+    int64_t qs, qos, ks, kos;
+    void *q = a.rows(5, dt, n, c.q_heads, c.head_dim, &qs), *qo = a.rows(6, dt, n, c.q_heads, c.head_dim, &qos);
+    void *k = a.rows(7, dt, n, c.k_heads, c.head_dim, &ks), *ko = a.rows(8, dt, n, c.k_heads, c.head_dim, &kos);
+    void* stream = a.stream(9);
+    auto* f = a.function<decltype(moe_rope)>(0);
+    return outcome(a, [&] { return f(&c, static_cast<int32_t>(n), positions, freqs, q, qs, qo, qos, k, ks, ko, kos, stream); });
+}
+
 template <PyObject* (*F)(Args), int N>
 PyObject* entry(PyObject* self, PyObject* const* at, Py_ssize_t n) { return guarded<F>(self, at, n, N); }
 
@@ -186,7 +289,8 @@ PyMethodDef method(const char* name) {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<F, N>)), METH_FASTCALL, nullptr};
 }
 PyMethodDef methods[] = {method<add_norm, 11>("add_norm"), method<kv_write, 11>("kv_write"), method<kv_read, 11>("kv_read"),
-                         method<attn_decode, 15>("attn_decode"), {nullptr, nullptr, 0, nullptr}};
+                         method<attn_decode, 15>("attn_decode"), method<attn_decode_scored, 18>("attn_decode_scored"),
+                         method<attn_prompt, 21>("attn_prompt"), method<rope, 10>("rope"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -18,6 +18,7 @@
 
 #include "common.h"
 #include "convert.h"
+#include "scores.h"
 
 namespace moe {
 namespace {
@@ -49,6 +50,7 @@ struct Attn {
     int B, heads, group, chunks, items, item_rows, dim, pages, page_bits, table_pages, window;
     int over_row;                   // 2^16 over the pieces of a row, rounded up: a quotient of numbers below 2^10 is a product and a shift
     float scale;                    // times log2 e
+    ScoreArgs scores;               // SCORED kernels only
 };
 
 // The tokens [first, end) sequence b attends to, and `base`, `first` rounded down to a run of 16 (which lies in one page).
@@ -165,7 +167,8 @@ __device__ inline uint32_t take_bf16x2(float& lo, float& hi) {
 // fp32 queries in three parts of 8 bits (all of their bits; a third of the fp32 instruction's time), and the weights p, of at most 2^8, in as
 // many parts as the output is worth: three for fp32, two for bf16 (with one, its rounding would be as large an error as the output's own; the
 // second costs nothing, 256 sequences in e4m3 take 349.8 us with one and 349.1 with two).
-template <bool F32, int CACHE, int DIM, int NT>
+// SCORED: logits may be capped or get a bias by distance.
+template <bool F32, int CACHE, int DIM, int NT, bool SCORED>
 struct Wave {
     using L = Layout<CACHE, DIM>;
     static constexpr bool kWide = CACHE == MOE_F32;                                 // fp32 products
@@ -175,6 +178,7 @@ struct Wave {
     bf16x8 q16[kWide ? 1 : kPartsQ][kWide ? 1 : NT][kWide ? 1 : L::kPieces][kWide ? 1 : kSteps];
     f32x4 o[NT][L::kHalves][L::kOwn];                                               // O^T: dim 128 half + own (4 g + r) + j, head l % 16
     float m[NT], l[NT];                                                             // maximum (the same in all quarters), weight of the own tokens
+    HeadScores<false> of_head[SCORED ? NT : 0];
 
     uint32_t k_at[L::kPieces], k_in[L::kPieces], k_out[L::kPieces], v_at[L::kHalves];    // of this lane: bytes from a run's first row, bytes in the LDS
     int row_bytes;
@@ -223,6 +227,7 @@ struct Wave {
     // Requests the query heads [head0, head0 + n_heads) of sequence b; zeros in the columns and past the row's end.
     __device__ void load_q(const Attn& a, int b, int head0, int n_heads, int lane) {
         constexpr int kBytes = F32 ? 4 : 2;
+        if constexpr (SCORED && F32 && DIM > 128) asm("" : "+v"(lane));       // (these addresses are computed anew for each item: held from item to item they are spilled)
         const int n = lane % 16, g = lane / 16;
         const auto rows = stretch_of(static_cast<const char*>(a.q) + (b * a.q_stride + static_cast<long>(head0) * a.dim) * kBytes, n_heads * a.dim * kBytes);
 #pragma unroll
@@ -243,6 +248,13 @@ struct Wave {
                     for (int s = 0; s < kSteps; ++s) q16[0][t][i][s] = __builtin_bit_cast(bf16x8, load_raw<16>(rows, at + 16 * s, 0));
                 }
             }
+    }
+
+    // Requests what the scores of the query heads from head0 on have of their own.
+    __device__ void load_scores(const Attn& a, int head0, int n_heads, int lane) {
+        if constexpr (SCORED)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) of_head[t].load(a.scores, head0 + min(16 * t + lane % 16, n_heads - 1));
     }
 
     // Once the queries are wanted.
@@ -297,6 +309,28 @@ struct Wave {
             if constexpr (CACHE == MOE_E4M3) {
                 x.ks[r] = __builtin_bit_cast(f32x4, load_raw<16>(stretch_of(a.k_scales + at, wanted ? 64 : 0), 16 * g, 0));
                 x.vs[r] = __builtin_bit_cast(f32x4, load_raw<16>(stretch_of(a.v_scales + at, wanted ? 64 : 0), 16 * g, 0));
+            }
+        }
+    }
+
+    // Sums of products of the t-th sixteen query heads to their logits; d: the distance of the first.
+    __device__ void score(f32x4 (&s)[2], const f32x4 (&ks)[2], const Attn& a, int t, int d, bool near) const {
+        const HeadScores<false>& own = of_head[t];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float x[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                x[c] = s[r][c] * a.scale;
+                if constexpr (CACHE == MOE_E4M3) x[c] *= ks[r][c];
+            }
+            if (a.scores.cap > 0.f) cap_scores(a.scores, x);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int at = d - 16 * r - c;
+                if (a.scores.slopes != nullptr) x[c] = fmaf(-own.slope, fabsf(static_cast<float>(at)), x[c]);
+                if (a.scores.bias != nullptr) x[c] += own.bias(a.scores, at, near);
+                s[r][c] = x[c];
             }
         }
     }
@@ -369,16 +403,21 @@ struct Wave {
                 }
         }
 
+        const bool near = SCORED && a.scores.near(span.end - t0 - 32, span.end - 1 - t0);
         float p[NT][2][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             float top = -INFINITY;
+            if constexpr (SCORED) score(s[t], ks, a, t, span.end - 1 - (t0 + 4 * g), near);
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    float x = s[t][r][c] * a.scale;
-                    if constexpr (CACHE == MOE_E4M3) x *= ks[r][c];
+                    float x = s[t][r][c];
+                    if constexpr (!SCORED) {
+                        x *= a.scale;
+                        if constexpr (CACHE == MOE_E4M3) x *= ks[r][c];
+                    }
                     const int tok = t0 + 16 * r + 4 * g + c;
                     if (edge && (tok < span.first || tok >= span.end)) x = -INFINITY;
                     p[t][r][c] = x;
@@ -482,8 +521,8 @@ __device__ inline void lds_barrier() {
 
 // Joins the four waves' sums of an item and stores its results, or its part's.  The block's last barrier before the next call comes after
 // every use of `sums`.
-template <bool F32, int CACHE, int DIM, int NT>
-__device__ void finish(const Attn& a, const Wave<F32, CACHE, DIM, NT>& w, Sums<DIM, NT>& sums, const Item& it, int wave, int lane) {
+template <bool F32, int CACHE, int DIM, int NT, bool SCORED>
+__device__ void finish(const Attn& a, const Wave<F32, CACHE, DIM, NT, SCORED>& w, Sums<DIM, NT>& sums, const Item& it, int wave, int lane) {
     using L = Layout<CACHE, DIM>;
     constexpr int kCols = Sums<DIM, NT>::kCols;
     const int n = lane % 16, g = lane / 16, tid = 64 * wave + lane;
@@ -599,16 +638,20 @@ struct Feed {
 // Works through items, `more` saying which comes next.  A wave has two tiles on the way while it attends to a third (kAhead), the next
 // item's first ones among them, so that what an item's end costs is its barriers and not the memory's answer.  TEAM waves share an item's tokens, `wave` this one's number;
 // `end(item)` stores what they have found.
-template <int TEAM, bool F32, int CACHE, int DIM, int NT, typename More, typename End>
-__device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT>& w, char* mine, Item it, More more, End end, int wave, int lane) {
+template <int TEAM, bool F32, int CACHE, int DIM, int NT, bool SCORED, typename More, typename End>
+__device__ void work(const Attn& a, Wave<F32, CACHE, DIM, NT, SCORED>& w, char* mine, Item it, More more, End end, int wave, int lane) {
     using L = Layout<CACHE, DIM>;
     constexpr int kStep = 32 * TEAM;
     constexpr bool kAskEarly = !(F32 && DIM > 128);              // (with the next queries beside its sums, a wave of these would spill up to 63 registers)
-    typename Wave<F32, CACHE, DIM, NT>::Tile x, y;
+    typename Wave<F32, CACHE, DIM, NT, SCORED>::Tile x, y;
     auto begin = [&](const Item& i) { return i.span.base + i.u0 * kUnit + 32 * wave; };
     auto limit = [&](const Item& i) { return min(i.span.end, i.span.base + i.u1 * kUnit); };
     auto steps_from = [&](const Item& i, int t) { return max(0, min(kAsk, (limit(i) - t + kStep - 1) / kStep)); };
-    auto ask_q = [&](const Item& i) { w.load_q(a, i.b, i.h * a.group + 16 * NT * i.chunk, min(16 * NT, a.group - 16 * NT * i.chunk), lane); };
+    auto ask_q = [&](const Item& i) {
+        const int head0 = i.h * a.group + 16 * NT * i.chunk, n_heads = min(16 * NT, a.group - 16 * NT * i.chunk);
+        w.load_q(a, i.b, head0, n_heads, lane);
+        w.load_scores(a, head0, n_heads, lane);
+    };
     int t = begin(it), steps = steps_from(it, t), ids = w.pages_of(a, it.span, it.b, t, lane, kStep);
     ask_q(it);
     w.reset();
@@ -660,14 +703,14 @@ __device__ inline void store_nothing(const Attn& a, long row, int n_heads, int t
 }
 
 // A block for each sequence, key head and 16 * NT of its query heads; nothing is split.
-template <bool F32, int CACHE, int DIM, int NT>
+template <bool F32, int CACHE, int DIM, int NT, bool SCORED>
 __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_short_kernel(Attn a) {
     __shared__ __attribute__((aligned(16))) char runs[4][Layout<CACHE, DIM>::kStaged ? Layout<CACHE, DIM>::kRun : 16];
     __shared__ Sums<DIM, NT> sums;
     const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
     const int pair = blockIdx.x / a.chunks;
     Item it{pair / a.heads, pair % a.heads, static_cast<int>(blockIdx.x % a.chunks), 0, 0, -1, {}};
-    Wave<F32, CACHE, DIM, NT> w;
+    Wave<F32, CACHE, DIM, NT, SCORED> w;
     w.lay_out(a, lane);
     it.span = span_of(a, a.lens[it.b]);
     it.u1 = it.span.units;
@@ -679,8 +722,8 @@ __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_short
 }
 
 // The results of a wave that has had an item to itself.
-template <bool F32, int CACHE, int DIM, int NT>
-__device__ void finish_alone(const Attn& a, const Wave<F32, CACHE, DIM, NT>& w, const Item& it, int lane) {
+template <bool F32, int CACHE, int DIM, int NT, bool SCORED>
+__device__ void finish_alone(const Attn& a, const Wave<F32, CACHE, DIM, NT, SCORED>& w, const Item& it, int lane) {
     constexpr int kOwn = Layout<CACHE, DIM>::kOwn;
     const int n = lane % 16, g = lane / 16, in_group = 16 * NT * it.chunk, n_heads = min(16 * NT, a.group - in_group);
     const long head0 = (static_cast<long>(it.b) * a.heads + it.h) * a.group + in_group;
@@ -708,14 +751,14 @@ __device__ void finish_alone(const Attn& a, const Wave<F32, CACHE, DIM, NT>& w, 
 }
 
 // Many short sequences: a wave for each item, and no wait for others.
-template <bool F32, int CACHE, int DIM, int NT>
+template <bool F32, int CACHE, int DIM, int NT, bool SCORED>
 __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_wave_kernel(Attn a) {
     __shared__ __attribute__((aligned(16))) char runs[4][Layout<CACHE, DIM>::kStaged ? Layout<CACHE, DIM>::kRun : 16];
     const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), index = 4 * blockIdx.x + wave;
     if (index >= a.B * a.items) return;                               // (no barrier in this kernel)
     const int pair = index / a.chunks;
     Item it{pair / a.heads, pair % a.heads, index % a.chunks, 0, 0, -1, {}};
-    Wave<F32, CACHE, DIM, NT> w;
+    Wave<F32, CACHE, DIM, NT, SCORED> w;
     w.lay_out(a, lane);
     it.span = span_of(a, uniform(a.lens[it.b]));
     it.u1 = it.span.units;
@@ -729,13 +772,13 @@ __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_wave_
 // The work is the list of all (sequence, key head, 16 * NT of its query heads, unit of tokens); every block takes an equal stretch of it, found from the lengths on the
 // device, whatever they are.  An item that lies in several stretches is left by each as a part, and joined by attn_join_kernel in the order of
 // the tokens.
-template <bool F32, int CACHE, int DIM, int NT>
+template <bool F32, int CACHE, int DIM, int NT, bool SCORED>
 __global__ __launch_bounds__(256, waves_of(F32, CACHE, DIM, NT)) void attn_kernel(Attn a, double one_over_workers) {
     __shared__ __attribute__((aligned(16))) char runs[4][Layout<CACHE, DIM>::kStaged ? Layout<CACHE, DIM>::kRun : 16];
     __shared__ Sums<DIM, NT> sums;
     __shared__ int before[kMaxB + 1], list[kMaxB], wave_total[4];       // places of the sequences before; lengths
     const int tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
-    Wave<F32, CACHE, DIM, NT> w;
+    Wave<F32, CACHE, DIM, NT, SCORED> w;
     {
         const int per = (a.B + 255) / 256, b0 = tid * per, b1 = min(b0 + per, a.B);
         int own = 0;
@@ -912,7 +955,7 @@ struct Parts {
     }
 };
 
-template <bool F32, int CACHE, int DIM, int NT>
+template <bool F32, int CACHE, int DIM, int NT, bool SCORED>
 int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) {
     int dev = 0;
     const DeviceInfo* info = nullptr;
@@ -924,16 +967,16 @@ int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) 
     a.over_row = (65536 + per - 1) / per;
     a.item_rows = std::min(16 * NT, a.group);
     if (p.alone) {
-        hipLaunchKernelGGL((attn_wave_kernel<F32, CACHE, DIM, NT>), dim3((a.B * a.items + 3) / 4), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((attn_wave_kernel<F32, CACHE, DIM, NT, SCORED>), dim3((a.B * a.items + 3) / 4), dim3(256), 0, s, a);
         MOE_LAUNCH_CHECK("attn_wave_kernel");
         return MOE_OK;
     }
     if (p.is_short) {
-        hipLaunchKernelGGL((attn_short_kernel<F32, CACHE, DIM, NT>), dim3(a.B * a.heads * a.chunks), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((attn_short_kernel<F32, CACHE, DIM, NT, SCORED>), dim3(a.B * a.heads * a.chunks), dim3(256), 0, s, a);
         MOE_LAUNCH_CHECK("attn_short_kernel");
         return MOE_OK;
     }
-    hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT>), dim3(p.workers), dim3(256), 0, s, a, 1.0 / p.workers);
+    hipLaunchKernelGGL((attn_kernel<F32, CACHE, DIM, NT, SCORED>), dim3(p.workers), dim3(256), 0, s, a, 1.0 / p.workers);
     MOE_LAUNCH_CHECK("attn_kernel");
     if (a.B * a.items >= p.workers) hipLaunchKernelGGL((attn_join_kernel<F32, 1>), dim3(p.workers, (a.item_rows + 3) / 4), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_join_kernel<F32, 4>), dim3(p.workers, a.item_rows), dim3(256), 0, s, a);
@@ -941,24 +984,23 @@ int launch(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) 
     return MOE_OK;
 }
 
-template <bool F32, int CACHE>
+template <bool F32, int CACHE, bool SCORED>
 int for_sizes(const moe_kv_cfg& kv, const moe_attn_cfg& c, Attn& a, hipStream_t s) {
     if constexpr (!F32)
-        if (columns_of(kv, a.group) == 2) return a.dim <= 64 ? launch<F32, CACHE, 64, 2>(kv, c, a, s) : launch<F32, CACHE, 128, 2>(kv, c, a, s);
-    if (a.dim <= 64) return launch<F32, CACHE, 64, 1>(kv, c, a, s);
-    return a.dim <= 128 ? launch<F32, CACHE, 128, 1>(kv, c, a, s) : launch<F32, CACHE, 256, 1>(kv, c, a, s);
+        if (columns_of(kv, a.group) == 2) return a.dim <= 64 ? launch<F32, CACHE, 64, 2, SCORED>(kv, c, a, s) : launch<F32, CACHE, 128, 2, SCORED>(kv, c, a, s);
+    if (a.dim <= 64) return launch<F32, CACHE, 64, 1, SCORED>(kv, c, a, s);
+    return a.dim <= 128 ? launch<F32, CACHE, 128, 1, SCORED>(kv, c, a, s) : launch<F32, CACHE, 256, 1, SCORED>(kv, c, a, s);
 }
 
-}  // namespace
-
-size_t attn_workspace_bytes(const moe_kv_cfg& kv, const moe_attn_cfg& c) { return Parts(kv, c).bytes; }
-
-int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* q, long q_stride, const void* k_pages, const void* v_pages,
-                       const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens, void* out, float* lse,
-                       void* ws, hipStream_t s) {
+// The call's arrays and sizes; the workspace's address is that of the parts' sums.
+template <bool SCORED>
+int for_types(const moe_kv_cfg& kv, const moe_attn_cfg& c, const ScoreArgs& scores, const void* q, long q_stride, const void* k_pages,
+              const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens, void* out, float* lse,
+              void* ws, hipStream_t s) {
     const Parts parts(kv, c);
     char* base = static_cast<char*>(ws);
     Attn a;
+    a.scores = scores;
     a.q = q;
     a.q_stride = q_stride;
     a.k_pages = static_cast<const char*>(k_pages);
@@ -982,9 +1024,28 @@ int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* 
     a.table_pages = c.table_pages;
     a.window = c.window;
     a.scale = (c.scale > 0.f ? c.scale : 1.f / sqrtf(static_cast<float>(kv.head_dim))) * 1.4426950408889634f;
-    if (kv.dtype == MOE_BF16) return kv.cache_dtype == MOE_BF16 ? for_sizes<false, MOE_BF16>(kv, c, a, s) : for_sizes<false, MOE_E4M3>(kv, c, a, s);
-    if (kv.cache_dtype == MOE_F32) return for_sizes<true, MOE_F32>(kv, c, a, s);
-    return kv.cache_dtype == MOE_BF16 ? for_sizes<true, MOE_BF16>(kv, c, a, s) : for_sizes<true, MOE_E4M3>(kv, c, a, s);
+    if (kv.dtype == MOE_BF16) return kv.cache_dtype == MOE_BF16 ? for_sizes<false, MOE_BF16, SCORED>(kv, c, a, s) : for_sizes<false, MOE_E4M3, SCORED>(kv, c, a, s);
+    if (kv.cache_dtype == MOE_F32) return for_sizes<true, MOE_F32, SCORED>(kv, c, a, s);
+    return kv.cache_dtype == MOE_BF16 ? for_sizes<true, MOE_BF16, SCORED>(kv, c, a, s) : for_sizes<true, MOE_E4M3, SCORED>(kv, c, a, s);
 }
+
+}  // namespace
+
+// The kernels with and without scores of their own are objects of their own, compiled side by side.
+#if ATTN_PART == 0
+size_t attn_workspace_bytes(const moe_kv_cfg& kv, const moe_attn_cfg& c) { return Parts(kv, c).bytes; }
+
+int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* q, long q_stride, const void* k_pages, const void* v_pages,
+                       const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens, void* out, float* lse,
+                       void* ws, hipStream_t s) {
+    return for_types<false>(kv, c, ScoreArgs{}, q, q_stride, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws, s);
+}
+#else
+int launch_attn_decode_scored(const moe_kv_cfg& kv, const moe_attn_cfg& c, const Scores& scores, const void* q, long q_stride, const void* k_pages,
+                              const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens,
+                              void* out, float* lse, void* ws, hipStream_t s) {
+    return for_types<true>(kv, c, ScoreArgs(scores), q, q_stride, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws, s);
+}
+#endif
 
 }  // namespace moe

@@ -136,6 +136,29 @@ int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* 
                        const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens, void* out, float* lse,
                        void* ws, hipStream_t s);
 
+// scores, slopes, bias: NULL where there is no such part (scores NULL: no cap, and no bias).
+struct Scores {
+    float cap;
+    int back, ahead;
+    const float *slopes, *bias;
+    bool any() const { return cap > 0.f || slopes != nullptr || bias != nullptr; }
+};
+int launch_attn_decode_scored(const moe_kv_cfg& kv, const moe_attn_cfg& c, const Scores& scores, const void* q, long q_stride, const void* k_pages,
+                              const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens,
+                              void* out, float* lse, void* ws, hipStream_t s);
+size_t attn_prompt_workspace_bytes(const moe_kv_cfg& kv, const moe_prompt_cfg& c);
+int launch_attn_prompt(const moe_kv_cfg& kv, const moe_prompt_cfg& c, const Scores& scores, const void* q, long q_stride, const void* k_pages,
+                       const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens,
+                       const int32_t* starts, const int32_t* first, const int32_t* end, void* out, float* lse, void* ws, hipStream_t s);
+// One of the two sides of moe_rope; `in` NULL: it is left out.
+struct RopeSide {
+    const void* in;
+    void* out;
+    long in_stride, out_stride;
+    int heads;
+};
+int launch_rope(const moe_rope_cfg& c, int n, const int32_t* positions, const double* freqs, const RopeSide& q, const RopeSide& k, hipStream_t s);
+
 // Batches of at most kDirectRows assignments, by one wave (all lanes; lane = assignment): the lanes that hold the same expert as this one
 // (0 where there is no assignment).  Values out of range are clamped, as in the batching kernels.
 __device__ inline unsigned long long direct_peers(const int32_t* __restrict__ idx, int A, int E, int lane, int& expert) {

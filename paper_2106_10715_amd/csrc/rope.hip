@@ -1,0 +1,161 @@
+// Rotary positions: pairs of a head's columns turned by angles that grow with the token's place.
+//
+// Bound by reading and writing the rows once.  All heads of a token turn by the same angles, so a block takes some tokens, computes each
+// (token, pair)'s sine and cosine once, into LDS, and turns all of their heads with them.  Angles are fp64 products, of which only the part
+// of a turn is kept: a place of a million times a frequency has, in fp32, no digit left that says where on the circle it is.
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "convert.h"
+
+namespace moe {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct Rope {
+    RopeSide q, k;
+    const int32_t* positions;
+    const double* freqs;
+    int n, dim, rot, tokens, heads, pieces, row_pieces;      // tokens of a block, heads of both sides; pieces of a row that are turned, and all of them
+    uint32_t over_heads;                                     // 2^32 / heads, rounded up (more than one head): a quotient of numbers below 2^20 is a product's upper half
+    float amplitude;
+};
+
+// V elements of a row, in registers and memory.
+template <bool BF16, int V>
+struct Piece {
+    static constexpr int kBytes = V * (BF16 ? 2 : 4);
+    uint32_t u[kBytes >= 4 ? kBytes / 4 : 1];
+    __device__ void load(const void* p) {
+        if constexpr (kBytes == 16) { const u32x4 r = *static_cast<const u32x4*>(p); for (int c = 0; c < 4; ++c) u[c] = r[c]; }
+        else if constexpr (kBytes == 8) { const u32x2 r = *static_cast<const u32x2*>(p); u[0] = r[0]; u[1] = r[1]; }
+        else if constexpr (kBytes == 4) u[0] = *static_cast<const uint32_t*>(p);
+        else u[0] = *static_cast<const uint16_t*>(p);
+    }
+    __device__ void store(void* p) const {
+        if constexpr (kBytes == 16) *static_cast<u32x4*>(p) = u32x4{u[0], u[1], u[2], u[3]};
+        else if constexpr (kBytes == 8) *static_cast<u32x2*>(p) = u32x2{u[0], u[1]};
+        else if constexpr (kBytes == 4) *static_cast<uint32_t*>(p) = u[0];
+        else *static_cast<uint16_t*>(p) = static_cast<uint16_t>(u[0]);
+    }
+    __device__ float get(int i) const {
+        if constexpr (!BF16) return __uint_as_float(u[i]);
+        else return i % 2 == 0 ? bf16_lo(u[i / 2]) : bf16_hi(u[i / 2]);
+    }
+    __device__ void set(const float (&v)[V]) {
+        if constexpr (!BF16) for (int c = 0; c < V; ++c) u[c] = __float_as_uint(v[c]);
+        else if constexpr (V == 1) u[0] = to_bf16x2(v[0], 0.f);
+        else for (int c = 0; c < V / 2; ++c) u[c] = to_bf16x2(v[2 * c], v[2 * c + 1]);
+    }
+};
+
+// HALF: an item is V pairs, a piece of either half; else V / 2 pairs in one piece.  Items past the turned columns copy one piece.
+template <bool BF16, bool HALF, int V>
+__global__ __launch_bounds__(kThreads) void rope_kernel(Rope a) {
+    __shared__ float sines[kThreads], cosines[kThreads];
+    const int tid = threadIdx.x, pairs = a.rot / 2, first = blockIdx.x * a.tokens, tokens = min(a.tokens, a.n - first);
+    if (tid < tokens * pairs) {
+        const int token = tid / pairs, pair = tid - token * pairs;
+        const double turns = static_cast<double>(a.positions[first + token]) * a.freqs[pair] * 0.15915494309189533577;
+        float s, c;
+        sincospif(2.f * static_cast<float>(turns - rint(turns)), &s, &c);
+        sines[tid] = s * a.amplitude;
+        cosines[tid] = c * a.amplitude;
+    }
+    __syncthreads();
+    constexpr int kBytes = BF16 ? 2 : 4;
+    const int rows = tokens * a.heads, per = kThreads / a.row_pieces;
+    const int piece = tid % a.row_pieces;
+    if (tid >= per * a.row_pieces) return;
+    for (int row = tid / a.row_pieces; row < rows; row += per) {
+        const int token = a.heads == 1 ? row : static_cast<int>(__umulhi(static_cast<uint32_t>(row), a.over_heads)), in_token = row - token * a.heads;
+        const RopeSide& side = in_token < a.q.heads ? a.q : a.k;
+        const int head = in_token < a.q.heads ? in_token : in_token - a.q.heads;
+        const char* in = static_cast<const char*>(side.in) + ((first + token) * side.in_stride + head * a.dim) * kBytes;
+        char* out = static_cast<char*>(side.out) + ((first + token) * side.out_stride + head * a.dim) * kBytes;
+        if (piece >= a.pieces) {
+            if (in == out) continue;
+            const long at = static_cast<long>(a.rot + (piece - a.pieces) * V) * kBytes;
+            Piece<BF16, V> x;
+            x.load(in + at);
+            x.store(out + at);
+            continue;
+        }
+        if constexpr (HALF) {
+            const int p0 = piece * V;
+            Piece<BF16, V> x, y;
+            x.load(in + p0 * kBytes);
+            y.load(in + (pairs + p0) * kBytes);
+            float u[V], v[V];
+#pragma unroll
+            for (int c = 0; c < V; ++c) {
+                const float s = sines[token * pairs + p0 + c], k = cosines[token * pairs + p0 + c], l = x.get(c), r = y.get(c);
+                u[c] = l * k - r * s;
+                v[c] = l * s + r * k;
+            }
+            x.set(u);
+            y.set(v);
+            x.store(out + p0 * kBytes);
+            y.store(out + (pairs + p0) * kBytes);
+        } else {
+            const int p0 = piece * (V / 2);
+            Piece<BF16, V> x;
+            x.load(in + 2 * p0 * kBytes);
+            float u[V];
+#pragma unroll
+            for (int c = 0; c < V / 2; ++c) {
+                const float s = sines[token * pairs + p0 + c], k = cosines[token * pairs + p0 + c], l = x.get(2 * c), r = x.get(2 * c + 1);
+                u[2 * c] = l * k - r * s;
+                u[2 * c + 1] = l * s + r * k;
+            }
+            x.set(u);
+            x.store(out + 2 * p0 * kBytes);
+        }
+    }
+}
+
+template <bool BF16, bool HALF, int V>
+void launch(Rope a, hipStream_t s) {
+    const bool tail = (a.q.heads > 0 && a.q.in != a.q.out) || (a.k.heads > 0 && a.k.in != a.k.out);
+    a.pieces = HALF ? a.rot / 2 / V : a.rot / V;
+    a.row_pieces = a.pieces + (tail ? (a.dim - a.rot) / V : 0);
+    // Tokens per block: so that each thread has a sine and cosine to compute, where there are blocks enough.
+    a.tokens = std::max(1, std::min(kThreads / (a.rot / 2), a.n / 2048));
+    hipLaunchKernelGGL((rope_kernel<BF16, HALF, V>), dim3((a.n + a.tokens - 1) / a.tokens), dim3(kThreads), 0, s, a);
+}
+
+template <bool BF16>
+void for_sizes(const Rope& a, bool half, hipStream_t s) {
+    const int run = half ? a.rot / 2 : a.rot;                // elements that lie together; as dim is a multiple of 16, what follows them does too
+    if constexpr (BF16)
+        if (run % 8 == 0) return half ? launch<BF16, true, 8>(a, s) : launch<BF16, false, 8>(a, s);
+    if (run % 4 == 0) return half ? launch<BF16, true, 4>(a, s) : launch<BF16, false, 4>(a, s);
+    if (run % 2 == 0) return half ? launch<BF16, true, 2>(a, s) : launch<BF16, false, 2>(a, s);
+    launch<BF16, true, 1>(a, s);                             // (of neighbours there is an even number)
+}
+
+}  // namespace
+
+int launch_rope(const moe_rope_cfg& c, int n, const int32_t* positions, const double* freqs, const RopeSide& q, const RopeSide& k, hipStream_t s) {
+    Rope a;
+    a.q = q;
+    a.k = k;
+    a.positions = positions;
+    a.freqs = freqs;
+    a.n = n;
+    a.dim = c.head_dim;
+    a.rot = c.rot_dim;
+    a.heads = q.heads + k.heads;
+    a.tokens = a.pieces = a.row_pieces = 0;                  // set where the pieces' width is chosen
+    a.over_heads = static_cast<uint32_t>(((uint64_t(1) << 32) + a.heads - 1) / a.heads);
+    a.amplitude = c.amplitude == 0.f ? 1.f : c.amplitude;
+    if (c.dtype == MOE_BF16) for_sizes<true>(a, c.pairs == MOE_PAIRS_HALF, s);
+    else for_sizes<false>(a, c.pairs == MOE_PAIRS_HALF, s);
+    MOE_LAUNCH_CHECK("rope_kernel");
+    return MOE_OK;
+}
+
+}  // namespace moe

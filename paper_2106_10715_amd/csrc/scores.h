@@ -1,0 +1,77 @@
+// Scores that are capped by a tanh or get a bias by distance, in the units of the attention kernels: logits times log2 e.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "common.h"
+
+namespace moe {
+
+constexpr float kLog2E = 1.4426950408889634f;
+
+struct ScoreArgs {
+    float cap = 0.f, over_cap = 0.f;        // times log2 e, and its inverse; 0: not capped
+    int back = 0, ahead = 0;
+    const float *slopes = nullptr, *bias = nullptr;
+    ScoreArgs() = default;
+    explicit ScoreArgs(const Scores& s) : cap(s.cap * kLog2E), over_cap(s.cap > 0.f ? 1.f / (s.cap * kLog2E) : 0.f), back(s.back), ahead(s.ahead), slopes(s.slopes), bias(s.bias) {}
+    // Whether keys at distances from `least` to `most` can have biases other than the last or the first one's alone.
+    __device__ bool near(int least, int most) const { return bias != nullptr && least < back && most > -ahead; }
+};
+
+// tanh to a few units in the last place.  Below 0.75 an odd polynomial, fitted to tanh(z) / z in z^2 for the least relative error (1.5e-9; the sum of
+// its rounding 1e-7): 1 - 2 / (e^2z + 1) alone loses there what z is smaller than 1 by, and with a cap of 50 that is most scores.  Above it, that form.
+// Most sets of scores need the polynomial only, which is 9 ordinary instructions where the other has 3 and two of a quarter of their rate.
+__device__ inline float small_tanh(float z) {
+    const float u = z * z;
+    float p = 0.00172035361f;
+    p = fmaf(p, u, -0.00762702851f);
+    p = fmaf(p, u, 0.0214308724f);
+    p = fmaf(p, u, -0.0538856313f);
+    p = fmaf(p, u, 0.133325785f);
+    p = fmaf(p, u, -0.333333075f);
+    p = fmaf(p, u, 1.f);
+    return p * z;
+}
+__device__ inline float large_tanh(float z) {
+    const float e = __builtin_amdgcn_exp2f(z * (2.f * kLog2E));
+    return 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
+}
+constexpr float kSmall = 0.75f;
+
+// N scores; `z` in, cap * tanh(z / cap) out.  All lanes of the wave.
+template <int N>
+__device__ inline void cap_scores(const ScoreArgs& a, float (&x)[N]) {
+    bool large = false;
+    float z[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        z[i] = x[i] * a.over_cap;
+        large |= !(fabsf(z[i]) < kSmall);
+        x[i] = a.cap * small_tanh(z[i]);
+    }
+    if (__any(large))
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (!(fabsf(z[i]) < kSmall)) x[i] = a.cap * large_tanh(z[i]);
+}
+
+// What scores have of their query's head.  AHEAD: there may be keys behind the query.
+template <bool AHEAD>
+struct HeadScores {
+    float slope, last, first[AHEAD ? 1 : 0];    // times log2 e: what a step of distance costs; the bias of far keys, before the query and after it
+    int row;                                    // of the biases
+    __device__ void load(const ScoreArgs& a, int head) {
+        row = head * (a.back + a.ahead + 1) + a.ahead;
+        slope = a.slopes != nullptr ? a.slopes[head] * kLog2E : 0.f;
+        last = a.bias != nullptr ? a.bias[row + a.back] * kLog2E : 0.f;
+        if constexpr (AHEAD) first[0] = a.bias != nullptr ? a.bias[row - a.ahead] * kLog2E : 0.f;
+    }
+    // The bias of the key at distance d; not `near`: all of the wave's keys are far, on the same side.
+    __device__ float bias(const ScoreArgs& a, int d, bool near) const {
+        if (near) return a.bias[row + min(max(d, -a.ahead), a.back)] * kLog2E;
+        if constexpr (AHEAD) return d >= a.back ? last : first[0];
+        return last;
+    }
+};
+
+}  // namespace moe
