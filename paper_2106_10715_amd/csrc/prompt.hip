@@ -1,4 +1,14 @@
 // Attention of many new tokens per sequence over a paged cache of keys and values.
+//
+// For query row n (a token and a query head) over the keys t of its stretch:  out = sum_t p_t v_t / sum_t p_t,  p_t = 2^(l_t log2 e - m), with a running m,
+// one pass over the keys.  The rows of a sequence are its new tokens' query heads of one key head, token by token: a block takes 32 of them for each of its
+// waves, so that all heads of a group read a key once, and goes through the keys in tiles that it keeps in LDS, the next one on its way in registers.
+//
+// Both products are matrix instructions of 32 x 32 with the query rows as columns:
+//   S^T[key, row] = K Q^T,     O^T[dim, row] += V^T P^T.
+// A lane's sums S are, of its row, the keys 8 a + 4 (lane / 32) + b, a and b from 0 to 3: what the second product wants of P^T in that lane, if V^T is given with
+// its keys in the same order.  So P never leaves its lane.  In 16 bits V^T comes from LDS by reads that turn blocks of 4 keys x 16 columns; in fp32 an operand
+// is one number and the order is that of the reads.
 #include <math.h>
 
 #include <algorithm>
@@ -9,6 +19,11 @@
 
 namespace moe {
 namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kSlack = 8.f;               // the running maximum is raised only where a logit passes it by more than this (as a power of two)
 
 struct Prompt {
     const void* q;
@@ -23,80 +38,610 @@ struct Prompt {
     ScoreArgs scores;
 };
 
-template <int CACHE>
-__device__ inline float cached(const char* row, int i) {
-    if constexpr (CACHE == MOE_F32) return reinterpret_cast<const float*>(row)[i];
-    else if constexpr (CACHE == MOE_BF16) return __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[i]) << 16);
-    else return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(static_cast<unsigned char>(row[i])), 0);
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline int wave_min(int v) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) v = min(v, __shfl_xor(v, o));
+    return uniform(v);
+}
+__device__ inline int wave_max(int v) { return -wave_min(-v); }
+// Over the two lanes that hold the same row.
+__device__ inline float halves_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float halves_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// A wave for each (token, query head): a lane for each of 64 keys, then for each four columns of the values.
-template <bool F32, int CACHE>
-__global__ __launch_bounds__(64) void prompt_kernel(Prompt a) {
-    constexpr int kWidth = CACHE == MOE_F32 ? 4 : CACHE == MOE_BF16 ? 2 : 1;
-    const int lane = threadIdx.x, token = blockIdx.x, head = blockIdx.y, kv = head / a.group;
-    int lo = 0, hi = a.B;                   // the sequence: the last that begins at or before the token
-    auto start = [&](int b) { return min(max(a.starts[b], 0), a.tokens); };
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (start(mid) <= token) lo = mid;
-        else hi = mid;
-    }
-    if (token < start(lo) || token >= start(lo + 1)) return;
-    const int b = lo, len = min(max(a.lens[b], 0), a.table_pages << a.page_bits), place = len - start(b + 1) + token;
-    int from = a.first != nullptr ? max(a.first[token], 0) : 0, to = min(a.end != nullptr ? a.end[token] : place + 1, len);
-    if (a.window > 0) from = max(from, place - a.window + 1);
-    __shared__ float q[256], weights[64];
-    __shared__ long rows[64];
-    for (int i = lane; i < a.dim; i += 64) {
-        const long at = token * a.q_stride + head * a.dim + i;
-        q[i] = F32 ? static_cast<const float*>(a.q)[at] : static_cast<float>(static_cast<const __bf16*>(a.q)[at]);
-    }
-    __syncthreads();
-    HeadScores<true> hs;
-    hs.load(a.scores, head);
-    float m = -INFINITY, l = 0.f, o[4] = {};
-    for (int t0 = from; t0 < to; t0 += 64) {
-        const int t = t0 + lane, page = t < to ? min(max(a.table[static_cast<long>(b) * a.table_pages + (t >> a.page_bits)], 0), a.pages - 1) : 0;
-        const long row = ((static_cast<long>(page) * a.heads + kv) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
-        float x[1] = {0.f};
-        if (t < to) {
-            for (int i = 0; i < a.dim; ++i) x[0] = fmaf(cached<CACHE>(a.k_pages + row * a.dim * kWidth, i), q[i], x[0]);
-            if constexpr (CACHE == MOE_E4M3) x[0] *= a.k_scales[row];
+// How a block of WAVES waves holds its tiles.
+template <bool F32, int CACHE, int DIM, int WAVES>
+struct Shape {
+    static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
+    static constexpr int kKeys = F32 && DIM > 128 ? 32 : 64;                        // keys of a tile
+    static constexpr int kBlocks = kKeys / 32, kColumns = DIM / 32;                 // S in 32 keys, O in 32 columns
+    static constexpr int kWidth = F32 ? 4 : 2, kCached = CACHE == MOE_F32 ? 4 : CACHE == MOE_BF16 ? 2 : 1;
+    static constexpr int kRowBytes = DIM * kWidth, kPieces = kRowBytes / 16;        // a row in LDS
+    static constexpr int kFrom = DIM * kCached / 16;                                // 16-byte pieces of a row as it comes
+    static constexpr int kTo = kWidth / kCached;                                    // of which each makes so many in LDS
+    static constexpr int kLoads = (kKeys * kFrom + kThreads - 1) / kThreads;
+    static constexpr int kTile = kKeys * kRowBytes;                                 // bytes
+    static constexpr bool kSpare = kKeys * kFrom < kThreads;                        // some of the waves have nothing to load
+    static_assert(64 / kFrom <= 16 && (kSpare || kLoads * kThreads == kKeys * kFrom), "a load of a wave lies in one run of 16 tokens");
+};
+
+// The item a block works on: a sequence, some of its rows, and the keys they see.
+struct Item {
+    int b, rows;                            // rows: of the sequence, in all of its tokens
+    int row0, token0, place0;               // the block's first row; the sequence's first token in q, and its place
+    int len;
+};
+
+// Tile `index` from the end of the list of all sequences' tiles of `rows` rows; false: there is none.  64 sequences at a time, the last first.
+__device__ inline bool find(const Prompt& a, int index, int rows, Item& it) {
+    const int lane = threadIdx.x % 64;
+    int before = 0;
+    for (int b0 = a.B - 1; b0 >= 0; b0 -= 64) {
+        const int b = b0 - lane;
+        int s = 0, n = 0;
+        if (b >= 0) {
+            s = min(max(a.starts[b], 0), a.tokens);
+            n = max(min(max(a.starts[b + 1], 0), a.tokens) - s, 0);
         }
-        x[0] *= a.scale;
-        if (a.scores.cap > 0.f) cap_scores(a.scores, x);
-        if (a.scores.slopes != nullptr) x[0] = fmaf(-hs.slope, fabsf(static_cast<float>(place - t)), x[0]);
-        if (a.scores.bias != nullptr) x[0] += hs.bias(a.scores, place - t, true);
-        if (t >= to) x[0] = -INFINITY;
-        const float now = fmaxf(m, lanes_max<64>(x[0])), ref = now == -INFINITY ? 0.f : now, keep = __builtin_amdgcn_exp2f(m - ref);
-        const float p = __builtin_amdgcn_exp2f(x[0] - ref);
-        m = now;
-        l = l * keep + lanes_sum<64>(p);
-        __syncthreads();
-        weights[lane] = CACHE == MOE_E4M3 && t < to ? p * a.v_scales[row] : p;
-        rows[lane] = row;
-        __syncthreads();
-        for (int c = 0; c < 4; ++c) o[c] *= keep;
-        for (int j = 0; j < min(64, to - t0); ++j)
-            for (int c = 0; c < 4; ++c)
-                if (lane + 64 * c < a.dim) o[c] = fmaf(weights[j], cached<CACHE>(a.v_pages + rows[j] * a.dim * kWidth, lane + 64 * c), o[c]);
+        const int tiles = (n * a.group + rows - 1) / rows;                          // (tokens * group < 2^31)
+        int upto = tiles;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int v = __shfl_up(upto, o);
+            if (lane >= o) upto += v;
+        }
+        const unsigned long long found = __ballot(before + upto > index);
+        if (found != 0) {
+            const int at = __builtin_ctzll(found);
+            it.b = b0 - at;
+            const int tile = before + __shfl(upto, at) - 1 - index;                 // of the sequence
+            const int new_tokens = __shfl(n, at);
+            it.rows = uniform(new_tokens * a.group);
+            it.row0 = uniform(tile * rows);
+            it.token0 = uniform(__shfl(s, at));
+            it.b = uniform(it.b);
+            it.len = uniform(min(max(a.lens[it.b], 0), a.table_pages << a.page_bits));
+            it.place0 = it.len - uniform(new_tokens);
+            return true;
+        }
+        before += __shfl(upto, 63);
     }
-    const long at = static_cast<long>(token) * a.heads * a.group + head;
-    for (int c = 0; c < 4; ++c) {
-        const float v = l == 0.f ? 0.f : o[c] / l;
-        if (lane + 64 * c >= a.dim) continue;
-        if constexpr (F32) static_cast<float*>(a.out)[at * a.dim + lane + 64 * c] = v;
-        else static_cast<__bf16*>(a.out)[at * a.dim + lane + 64 * c] = static_cast<__bf16>(v);
-    }
-    if (lane == 0 && a.lse != nullptr) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    return false;
 }
 
-template <bool F32, int CACHE>
+// The keys [lo, hi) that a token sees; lo = hi where there are none.
+__device__ inline void stretch_of(const Prompt& a, const Item& it, int token, int& lo, int& hi) {
+    const int place = it.place0 + token;
+    lo = a.first != nullptr ? max(a.first[it.token0 + token], 0) : 0;
+    hi = min(a.end != nullptr ? a.end[it.token0 + token] : place + 1, it.len);
+    if (a.window > 0) lo = max(lo, place - a.window + 1);
+    hi = max(hi, lo);
+}
+
+// Which of a dword's two bf16 values (or its fp32 value) are not finite.
+template <bool F32>
+__device__ inline bool not_finite(uint32_t u) {
+    if constexpr (F32) return (u & 0x7f800000u) == 0x7f800000u;
+    else return (u & 0x7f800000u) == 0x7f800000u || (u & 0x7f80u) == 0x7f80u;
+}
+
+template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
+struct Block {
+    using H = Shape<F32, CACHE, DIM, WAVES>;
+    struct Lds {
+        __attribute__((aligned(256))) char k[2][H::kTile], v[2][H::kTile];
+        float ks[2][H::kKeys], vs[2][H::kKeys];                                     // e4m3 and 16-bit products: scales of the keys, times a.scale, and of the values
+        int odd[2];                                                                 // 1 + the first key of a tile whose values are not all finite
+    };
+    const Prompt& a;
+    Lds& lds;
+    const Item& it;
+    int head, lane, wave;                                                           // key head
+    int first, end, all_from, all_to;                                               // keys that some of the block's rows see; that all of them see
+
+    // ---- a tile from the cache to LDS ----
+    u32x4 k_raw[H::kLoads], v_raw[H::kLoads];
+    float k_scale[F32 ? H::kLoads : 1], v_scale[F32 ? H::kLoads : 1];               // e4m3: of the rows, or (16-bit products) of key `lane`
+    int from[H::kLoads], at_row;                                                    // of this lane: bytes from its wave's first row; its first row
+    int k_to[H::kLoads][H::kTo], v_to[H::kLoads][H::kTo];
+
+    // Pieces of a row lie in LDS at places that differ from row to row, so that rows of a column are in different banks: a column of K is read 16 bytes by row,
+    // of V in 64 bytes of four rows.
+    __device__ static int k_place(int row, int piece) { return row * H::kRowBytes + 16 * (piece ^ (H::kPieces >= 16 ? row & 15 : (row >> 1) & 7)); }
+    __device__ static int v_place(int row, int piece) {
+        if constexpr (F32) return row * H::kRowBytes + 16 * piece;
+        else return row * H::kRowBytes + 16 * (piece ^ (H::kPieces >= 16 ? 4 * (row & 3) : 4 * ((row >> 1) & 1)));
+    }
+    __device__ void lay_out() {
+        const int row_bytes = a.dim * H::kCached;
+#pragma unroll
+        for (int j = 0; j < H::kLoads; ++j) {
+            const int i = j * H::kThreads + 64 * wave + lane, row = i / H::kFrom, piece = i % H::kFrom;
+            from[j] = 16 * piece < row_bytes ? (lane / H::kFrom) * row_bytes + 16 * piece : 0x7fffff00;
+#pragma unroll
+            for (int c = 0; c < H::kTo; ++c) {
+                k_to[j][c] = k_place(row, piece * H::kTo + c);
+                v_to[j][c] = v_place(row, piece * H::kTo + c);
+            }
+        }
+    }
+    // Requests keys [t0, t0 + kKeys); zeros outside of [first, end).
+    __device__ bool idle() const { return H::kSpare && 64 * wave >= H::kKeys * H::kFrom; }
+    __device__ void load(int t0) {
+        const int row_bytes = a.dim * H::kCached;
+#pragma unroll
+        for (int j = 0; j < H::kLoads; ++j) {
+            if (idle()) break;
+            const int row = (j * H::kThreads + 64 * wave) / H::kFrom, t = t0 + row, mine = t + lane / H::kFrom;
+            const int page = min(max(a.table[static_cast<long>(it.b) * a.table_pages + (min(t, end - 1) >> a.page_bits)], 0), a.pages - 1);
+            const long at = ((static_cast<long>(page) * a.heads + head) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
+            const int there = mine >= first && mine < end ? from[j] : 0x7fffff00;
+            const auto kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.k_pages) + at * row_bytes, 0, 16 * row_bytes, 0x00027000);
+            const auto vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.v_pages) + at * row_bytes, 0, 16 * row_bytes, 0x00027000);
+            k_raw[j] = __builtin_amdgcn_raw_buffer_load_b128(kr, there, 0, 0);
+            v_raw[j] = __builtin_amdgcn_raw_buffer_load_b128(vr, there, 0, 0);
+            if constexpr (CACHE == MOE_E4M3 && F32) {
+                const int row4 = mine >= first && mine < end ? 4 * (lane / H::kFrom) : 0x7fffff00;
+                k_scale[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.k_scales) + at, 0, 64, 0x00027000), row4, 0, 0));
+                v_scale[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.v_scales) + at, 0, 64, 0x00027000), row4, 0, 0));
+            }
+        }
+        if constexpr (CACHE == MOE_E4M3 && !F32)
+            if (wave == 0) {
+                const int t = t0 + lane;
+                k_scale[0] = v_scale[0] = 0.f;
+                if (t >= first && t < end) {
+                    const int page = min(max(a.table[static_cast<long>(it.b) * a.table_pages + (t >> a.page_bits)], 0), a.pages - 1);
+                    const long at = ((static_cast<long>(page) * a.heads + head) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
+                    k_scale[0] = a.k_scales[at];
+                    v_scale[0] = a.v_scales[at];
+                }
+            }
+    }
+    // One piece as it came in the form of the products.
+    __device__ static void widen(const u32x4& raw, float scale, u32x4 (&out)[H::kTo]) {
+        if constexpr (H::kTo == 1) {
+            out[0] = raw;
+        } else if constexpr (!F32) {                                                // e4m3 values are bf16 values
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                out[c / 4][c % 4] = __builtin_bit_cast(uint32_t, c % 2 == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c / 2], 1.f, false) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c / 2], 1.f, true));
+        } else if constexpr (CACHE == MOE_BF16) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                out[c / 2][2 * (c % 2)] = raw[c] << 16;
+                out[c / 2][2 * (c % 2) + 1] = raw[c] & 0xffff0000u;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float v[4];
+                from_e4m3x4(raw[c], v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[c][e] = __float_as_uint(v[e] * scale);
+            }
+        }
+    }
+    // Puts what came into buffer `to`.  `edge`: some row does not see some key of it, so that values that are not finite are looked for.
+    __device__ void store(int to, int t0, bool edge) {
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < H::kLoads; ++j) {
+            if (idle()) break;
+            u32x4 out[H::kTo];
+            widen(k_raw[j], F32 ? k_scale[F32 ? j : 0] : 1.f, out);
+#pragma unroll
+            for (int c = 0; c < H::kTo; ++c) *reinterpret_cast<u32x4*>(lds.k[to] + k_to[j][c]) = out[c];
+            widen(v_raw[j], F32 ? v_scale[F32 ? j : 0] : 1.f, out);
+#pragma unroll
+            for (int c = 0; c < H::kTo; ++c) *reinterpret_cast<u32x4*>(lds.v[to] + v_to[j][c]) = out[c];
+            if (edge)
+#pragma unroll
+                for (int c = 0; c < H::kTo; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) odd |= not_finite<F32>(out[c][e]);
+        }
+        if (odd) lds.odd[to] = t0 + 1;
+        if constexpr (CACHE == MOE_E4M3 && !F32)
+            if (wave == 0) {
+                lds.ks[to][lane] = k_scale[0] * a.scale;
+                lds.vs[to][lane] = v_scale[0];
+            }
+    }
+
+    // ---- a wave's 32 rows ----
+    static constexpr int kSteps = F32 ? DIM / 8 : DIM / 16;                         // pieces of Q that a lane holds, 16 bytes each
+    u32x4 q[kSteps];
+    f32x16 o[H::kColumns];
+    float m, l;
+    int lo, hi, place;                                                              // of this lane's row
+    int wave_first, wave_end, whole_from, whole_to;                                 // keys that some of the wave's rows see; that all of them see
+    HeadScores<true> hs;
+
+    // A lane's part of S^T of a tile, as logits.
+    __device__ void products(int buf, f32x16 (&s)[H::kBlocks]) const {
+        const char* k = lds.k[buf];
+        const int row = lane % 32, h = lane / 32;
+#pragma unroll
+        for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb) {
+                const u32x4 u = *reinterpret_cast<const u32x4*>(k + k_place(row, 2 * st + h) + 32 * kb * H::kRowBytes);
+                if constexpr (F32) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(u[c]), __uint_as_float(q[st][c]), s[kb], 0, 0, 0);
+                } else {
+                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u), __builtin_bit_cast(bf16x8, q[st]), s[kb], 0, 0, 0);
+                }
+            }
+    }
+    // The key of sum i of a lane in block kb, from the tile's first.
+    __device__ static constexpr int key_of(int kb, int i) { return 32 * kb + 8 * (i / 4) + i % 4; }
+
+    // O^T += V^T P^T for 16 keys (bf16) and 32 columns: what a lane reads of V.
+    __device__ bf16x8 turned(const char* v, int ks, int column) const {
+        const int r = (lane % 16) / 4, h = lane / 32;
+        const char* at = v + v_place(4 * h + r, 4 * column) + 32 * ((lane / 16) % 2) + 8 * (lane % 4) + 16 * ks * H::kRowBytes;
+        typedef __attribute__((address_space(3))) i16x4* Place;
+        const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 8 * H::kRowBytes));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // In fp32 a lane reads the kColumns (up to four) neighbouring columns of one key that are its row of as many blocks.
+    static constexpr int kNear = H::kColumns < 4 ? H::kColumns : 4;
+    __device__ void beside(const char* v, int key, int group4, float (&x)[kNear]) const {
+        const char* at = v + (key + 4 * (lane / 32)) * H::kRowBytes + 512 * group4 + 4 * kNear * (lane % 32);
+        if constexpr (kNear == 4) {
+            const f32x4 u = *reinterpret_cast<const f32x4*>(at);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = u[c];
+        } else {
+            const f32x2 u = *reinterpret_cast<const f32x2*>(at);
+            x[0] = u[0];
+            x[1] = u[1];
+        }
+    }
+
+    __device__ void attend(int buf, int t0) {
+        f32x16 s[H::kBlocks];
+        products(buf, s);
+        const int h = lane / 32;
+        const bool edge = t0 < whole_from || t0 + H::kKeys > whole_to;
+        constexpr bool kScaled = CACHE == MOE_E4M3 && !F32;                         // scales of its own for each key
+        const float scale = SCORED || kScaled ? 1.f : a.scale;
+        if constexpr (SCORED || kScaled)
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const f32x4 each = kScaled ? *reinterpret_cast<const f32x4*>(&lds.ks[buf][key_of(kb, i) + 4 * h]) : f32x4{a.scale, a.scale, a.scale, a.scale};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) s[kb][i + c] *= each[c];
+                }
+        if constexpr (SCORED) score(s, t0);
+        if (edge)
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int t = t0 + key_of(kb, i) + 4 * h;
+                    if (static_cast<uint32_t>(t - lo) >= static_cast<uint32_t>(hi - lo)) s[kb][i] = -INFINITY;
+                }
+        float top = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+        top = halves_max(top) * scale;
+        if (__any(top > m + kSlack)) {                                              // (always where m is still -inf and some key counts)
+            const float now = fmaxf(m, top), keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= keep;
+#pragma unroll
+            for (int c = 0; c < H::kColumns; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[c][i] *= keep;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        const bool odd = edge && uniform(lds.odd[buf]) == t0 + 1;
+        uint32_t seen = 0;                                                          // odd: the lane's keys that count, 16 of a block
+        if (odd)
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) seen |= s[kb][i] == -INFINITY ? 0u : 1u << (16 * kb + i);
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], scale, -ref));
+                sum[i % 4] += s[kb][i];
+            }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if constexpr (kScaled)
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const f32x4 each = *reinterpret_cast<const f32x4*>(&lds.vs[buf][key_of(kb, i) + 4 * h]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) s[kb][i + c] = edge && s[kb][i + c] == 0.f ? 0.f : s[kb][i + c] * each[c];
+                }
+        if (odd) values<true>(buf, s, seen);
+        else values<false>(buf, s, 0);
+    }
+
+    // O^T += V^T P^T.  ODD: values that are not finite, under rows of which not all see them.  A weight of zero times such a value would be no number, so it
+    // is left out of the product, and put into the rows that see it: two further products count, for each row and column, the infinities of either sign
+    // (and NaN, which is both).
+    template <bool ODD>
+    __device__ void values(int buf, f32x16 (&p)[H::kBlocks], uint32_t seen) {
+        const char* v = lds.v[buf];
+        if constexpr (F32) {
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int g = 0; g < H::kColumns / kNear; ++g) {
+                    f32x16 more[ODD ? kNear : 1], less[ODD ? kNear : 1];
+                    if constexpr (ODD)
+#pragma unroll
+                        for (int c = 0; c < kNear; ++c)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) more[c][i] = less[c][i] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float x[kNear];
+                        beside(v, key_of(kb, i), g, x);
+#pragma unroll
+                        for (int c = 0; c < kNear; ++c) {
+                            if constexpr (ODD) {
+                                const float count = seen >> (16 * kb + i) & 1 ? 1.f : 0.f;
+                                const float up = x[c] < INFINITY ? 0.f : 1.f, down = x[c] > -INFINITY ? 0.f : 1.f;          // (both for NaN)
+                                more[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(up, count, more[c], 0, 0, 0);
+                                less[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(down, count, less[c], 0, 0, 0);
+                                x[c] = up + down == 0.f ? x[c] : 0.f;
+                            }
+                            o[kNear * g + c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[c], p[kb][i], o[kNear * g + c], 0, 0, 0);
+                        }
+                    }
+                    if constexpr (ODD)
+#pragma unroll
+                        for (int c = 0; c < kNear; ++c) add(o[kNear * g + c], more[c], less[c]);
+                }
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < 2 * H::kBlocks; ++ks) {
+                u32x4 w, count;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int i = 8 * (ks % 2) + 2 * c;
+                    w[c] = to_bf16x2(p[ks / 2][i], p[ks / 2][i + 1]);
+                    if constexpr (ODD) count[c] = (seen >> (8 * ks + 2 * c) & 1 ? 0x3f80u : 0u) | (seen >> (8 * ks + 2 * c + 1) & 1 ? 0x3f800000u : 0u);
+                }
+                const bf16x8 weights = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+                for (int c = 0; c < H::kColumns; ++c) {
+                    bf16x8 x = turned(v, ks, c);
+                    if constexpr (ODD) {
+                        const bf16x8 counts = __builtin_bit_cast(bf16x8, count);
+                        f32x16 more, less;
+                        bf16x8 up, down;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) more[i] = less[i] = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float f = static_cast<float>(x[i]);
+                            const bool u = !(f < INFINITY), d = !(f > -INFINITY);
+                            up[i] = static_cast<__bf16>(u ? 1.f : 0.f);
+                            down[i] = static_cast<__bf16>(d ? 1.f : 0.f);
+                            x[i] = u || d ? static_cast<__bf16>(0.f) : x[i];
+                        }
+                        more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, counts, more, 0, 0, 0);
+                        less = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down, counts, less, 0, 0, 0);
+                        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, weights, o[c], 0, 0, 0);
+                        add(o[c], more, less);
+                    } else {
+                        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, weights, o[c], 0, 0, 0);
+                    }
+                }
+            }
+        }
+    }
+    __device__ static void add(f32x16& o, const f32x16& more, const f32x16& less) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            o[i] = more[i] > 0.f ? o[i] + INFINITY : o[i];
+            o[i] = less[i] > 0.f ? o[i] - INFINITY : o[i];
+        }
+    }
+
+    __device__ void score(f32x16 (&s)[H::kBlocks], int t0) const {
+        const int d0 = place - t0 - 4 * (lane / 32);                                // the distance of the lane's first key
+        if (a.scores.cap > 0.f)
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; i += 8) {
+                    float x[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) x[c] = s[kb][i + c];
+                    cap_scores(a.scores, x);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) s[kb][i + c] = x[c];
+                }
+        if (a.scores.slopes != nullptr)
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(-hs.slope, fabsf(static_cast<float>(d0 - key_of(kb, i))), s[kb][i]);
+        if (a.scores.bias != nullptr) {
+            const int far = H::kKeys - 1;
+            const bool behind = __all(d0 - far >= a.scores.back), ahead = __all(d0 <= -a.scores.ahead);
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kb][i] += hs.bias(a.scores, d0 - key_of(kb, i), !behind && !ahead);
+        }
+    }
+
+    // The block's rows, the keys they see, and the wave's queries.
+    __device__ void begin() {
+        const int tokens = (it.rows + a.group - 1) / a.group;
+        const int from_token = it.row0 / a.group, to_token = min((it.row0 + H::kRows - 1) / a.group, tokens - 1);
+        int low = 0x7fffffff, high = 0, last_low = 0, first_high = 0x7fffffff;
+        for (int i = from_token + lane; i <= to_token; i += 64) {
+            int x, y;
+            stretch_of(a, it, i, x, y);
+            last_low = max(last_low, x);
+            first_high = min(first_high, x < y ? y : -1);
+            if (x < y) {
+                low = min(low, x);
+                high = max(high, y);
+            }
+        }
+        first = wave_min(low);
+        end = wave_max(high);
+        all_from = wave_max(last_low);
+        all_to = wave_min(first_high);
+        const int row = it.row0 + 32 * wave + lane % 32;
+        const bool real = row < it.rows;
+        const int token = real ? row / a.group : 0, in_group = real ? row - token * a.group : 0;
+        place = it.place0 + token;
+        stretch_of(a, it, token, lo, hi);
+        if (!real) {                                                                // rows past the last: as if they saw all, and not stored
+            lo = 0;
+            hi = 0x7fffffff;
+        }
+        const bool some = real && lo < hi;
+        wave_first = wave_min(some ? lo : 0x7fffffff);
+        wave_end = wave_max(some ? hi : 0);
+        whole_from = wave_max(real ? lo : 0);
+        whole_to = wave_min(some || !real ? hi : -1);
+        const long at = (it.token0 + token) * a.q_stride + (static_cast<long>(head) * a.group + in_group) * a.dim;
+        constexpr int kElements = 16 / H::kWidth;
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+            const int d = (2 * st + lane / 32) * kElements;
+            q[st] = u32x4{0, 0, 0, 0};
+            if (real && d < a.dim) q[st] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + (at + d) * H::kWidth);
+        }
+        if constexpr (SCORED) hs.load(a.scores, head * a.group + in_group);
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int c = 0; c < H::kColumns; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
+    }
+
+    __device__ void finish() {
+        l = halves_sum(l);
+        const int row = it.row0 + 32 * wave + lane % 32, h = lane / 32;
+        if (row >= it.rows) return;
+        const int token = row / a.group;
+        const long at = static_cast<long>(it.token0 + token) * a.heads * a.group + head * a.group + (row - token * a.group);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (h == 0 && a.lse != nullptr) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        if constexpr (F32) {
+#pragma unroll
+            for (int g = 0; g < H::kColumns / kNear; ++g)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int d = 128 * g + kNear * (8 * (i / 4) + 4 * h + i % 4);
+                    float* to = static_cast<float*>(a.out) + at * a.dim + d;
+                    if (d >= a.dim) continue;
+                    if constexpr (kNear == 4) *reinterpret_cast<f32x4*>(to) = f32x4{o[4 * g][i], o[4 * g + 1][i], o[4 * g + 2][i], o[4 * g + 3][i]} * inv;
+                    else *reinterpret_cast<f32x2*>(to) = f32x2{o[0][i] * inv, o[1][i] * inv};
+                }
+        } else {
+#pragma unroll
+            for (int c = 0; c < H::kColumns; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const int d = 32 * c + 8 * (i / 4) + 4 * h;
+                    if (d >= a.dim) continue;
+                    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at * a.dim + d) =
+                        u32x2{to_bf16x2(o[c][i] * inv, o[c][i + 1] * inv), to_bf16x2(o[c][i + 2] * inv, o[c][i + 3] * inv)};
+                }
+        }
+    }
+
+    __device__ void run() {
+        lay_out();
+        begin();
+        if (first < end) {
+            const int base = first & ~(H::kKeys - 1);
+            auto edge = [&](int t0) { return t0 < all_from || t0 + H::kKeys > all_to; };
+            load(base);
+            if (threadIdx.x < 2) lds.odd[threadIdx.x] = 0;
+            __syncthreads();
+            store(0, base, edge(base));
+            int buf = 0;
+            for (int t0 = base; t0 < end; t0 += H::kKeys, buf ^= 1) {
+                __syncthreads();
+                const int next = t0 + H::kKeys;
+                if (next < end) load(next);
+                if (t0 < wave_end && next > wave_first) attend(buf, t0);
+                if (next < end) store(buf ^ 1, next, edge(next));
+            }
+        }
+        finish();
+    }
+};
+
+// Waves that a SIMD has room for: with two, a wave has 256 registers.
+constexpr int waves_of(bool f32, int dim) { return f32 || dim > 128 ? 1 : 2; }
+
+template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
+__global__ __launch_bounds__(64 * WAVES, waves_of(F32, DIM)) void prompt_kernel(Prompt a) {
+    using B = Block<F32, CACHE, DIM, WAVES, SCORED>;
+    __shared__ typename B::Lds lds;
+    Item it;
+    // the key heads first: blocks that read the same keys are a multiple of the heads apart, with eight of them on one XCD
+    if (!find(a, blockIdx.x / a.heads, B::H::kRows, it)) return;
+    B block{a, lds, it};
+    block.head = blockIdx.x % a.heads;
+    block.lane = threadIdx.x % 64;
+    block.wave = uniform(threadIdx.x / 64);
+    block.run();
+}
+
+template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
 int launch(const Prompt& a, hipStream_t s) {
-    hipLaunchKernelGGL((prompt_kernel<F32, CACHE>), dim3(a.tokens, a.heads * a.group), dim3(64), 0, s, a);
+    const long tiles = static_cast<long>(a.tokens) * a.group / (32 * WAVES) + std::min(a.B, a.tokens);       // (a sequence's last tile may not be full)
+    hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED>), dim3(static_cast<unsigned>(tiles * a.heads)), dim3(64 * WAVES), 0, s, a);
     MOE_LAUNCH_CHECK("prompt_kernel");
     return MOE_OK;
+}
+
+template <bool F32, int CACHE, int DIM, bool SCORED>
+int for_waves(const Prompt& a, hipStream_t s) {
+    if constexpr (!F32 && DIM <= 128)
+        if (static_cast<long>(a.tokens) * a.group * a.heads >= 256 * 256L) return launch<F32, CACHE, DIM, 8, SCORED>(a, s);
+    return launch<F32, CACHE, DIM, 4, SCORED>(a, s);
+}
+
+template <bool F32, int CACHE, bool SCORED>
+int for_sizes(const Prompt& a, hipStream_t s) {
+    if (a.dim <= 64) return for_waves<F32, CACHE, 64, SCORED>(a, s);
+    return a.dim <= 128 ? for_waves<F32, CACHE, 128, SCORED>(a, s) : for_waves<F32, CACHE, 256, SCORED>(a, s);
+}
+
+template <bool SCORED>
+int for_types(const moe_kv_cfg& kv, const Prompt& a, hipStream_t s) {
+    if (kv.dtype == MOE_BF16) return kv.cache_dtype == MOE_BF16 ? for_sizes<false, MOE_BF16, SCORED>(a, s) : for_sizes<false, MOE_E4M3, SCORED>(a, s);
+    if (kv.cache_dtype == MOE_F32) return for_sizes<true, MOE_F32, SCORED>(a, s);
+    return kv.cache_dtype == MOE_BF16 ? for_sizes<true, MOE_BF16, SCORED>(a, s) : for_sizes<true, MOE_E4M3, SCORED>(a, s);
 }
 
 }  // namespace
@@ -131,9 +676,7 @@ int launch_attn_prompt(const moe_kv_cfg& kv, const moe_prompt_cfg& c, const Scor
     a.window = c.window;
     a.scale = (c.scale > 0.f ? c.scale : 1.f / sqrtf(static_cast<float>(kv.head_dim))) * kLog2E;
     a.scores = ScoreArgs(scores);
-    if (kv.dtype == MOE_BF16) return kv.cache_dtype == MOE_BF16 ? launch<false, MOE_BF16>(a, s) : launch<false, MOE_E4M3>(a, s);
-    if (kv.cache_dtype == MOE_F32) return launch<true, MOE_F32>(a, s);
-    return kv.cache_dtype == MOE_BF16 ? launch<true, MOE_BF16>(a, s) : launch<true, MOE_E4M3>(a, s);
+    return scores.any() ? for_types<true>(kv, a, s) : for_types<false>(kv, a, s);
 }
 
 }  // namespace moe
