@@ -69,6 +69,8 @@ struct Shape {
     static constexpr int kTile = kKeys * kRowBytes;                                 // bytes
     static constexpr bool kSpare = kKeys * kFrom < kThreads;                        // some of the waves have nothing to load
     static_assert(64 / kFrom <= 16 && (kSpare || kLoads * kThreads == kKeys * kFrom), "a load of a wave lies in one run of 16 tokens");
+    static constexpr int kStep = kThreads / kFrom;                                  // rows from a lane's load to its next
+    static_assert(kThreads % kFrom == 0 && kStep % 4 == 0, "a lane's loads have the same piece of their rows");
 };
 
 // The item a block works on: a sequence, some of its rows, and the keys they see.
@@ -124,20 +126,16 @@ __device__ inline void stretch_of(const Prompt& a, const Item& it, int token, in
     hi = max(hi, lo);
 }
 
-// Which of a dword's two bf16 values (or its fp32 value) are not finite.
-template <bool F32>
-__device__ inline bool not_finite(uint32_t u) {
-    if constexpr (F32) return (u & 0x7f800000u) == 0x7f800000u;
-    else return (u & 0x7f800000u) == 0x7f800000u || (u & 0x7f80u) == 0x7f80u;
-}
-
 template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
 struct Block {
     using H = Shape<F32, CACHE, DIM, WAVES>;
     struct Lds {
         __attribute__((aligned(256))) char k[2][H::kTile], v[2][H::kTile];
         float ks[2][H::kKeys], vs[2][H::kKeys];                                     // e4m3 and 16-bit products: scales of the keys, times a.scale, and of the values
-        int odd[2];                                                                 // 1 + the first key of a tile whose values are not all finite
+        // Values that are not finite lie in v as zeros.  odd: 1 + the first key of a tile that has any; up, down: the bits of a piece's elements that
+        // were infinity or NaN, and -infinity or NaN.
+        int odd[2];
+        unsigned char up[2][H::kKeys][H::kPieces], down[2][H::kKeys][H::kPieces];
     };
     const Prompt& a;
     Lds& lds;
@@ -148,28 +146,21 @@ struct Block {
     // ---- a tile from the cache to LDS ----
     u32x4 k_raw[H::kLoads], v_raw[H::kLoads];
     float k_scale[F32 ? H::kLoads : 1], v_scale[F32 ? H::kLoads : 1];               // e4m3: of the rows, or (16-bit products) of key `lane`
-    int from[H::kLoads], at_row;                                                    // of this lane: bytes from its wave's first row; its first row
-    int k_to[H::kLoads][H::kTo], v_to[H::kLoads][H::kTo];
+    int from;                                                                       // of this lane: bytes from its wave's first row
+    int at_row, at_piece;                                                           // of this lane: row and piece (as it comes) of its first load
 
     // Pieces of a row lie in LDS at places that differ from row to row, so that rows of a column are in different banks: a column of K is read 16 bytes by row,
-    // of V in 64 bytes of four rows.
+    // of V in 64 bytes of four rows.  A piece's number and the row's change of it are combined by exclusive or, so that from one piece's place the others' follow.
     __device__ static int k_place(int row, int piece) { return row * H::kRowBytes + 16 * (piece ^ (H::kPieces >= 16 ? row & 15 : (row >> 1) & 7)); }
     __device__ static int v_place(int row, int piece) {
         if constexpr (F32) return row * H::kRowBytes + 16 * piece;
         else return row * H::kRowBytes + 16 * (piece ^ (H::kPieces >= 16 ? 4 * (row & 3) : 4 * ((row >> 1) & 1)));
     }
     __device__ void lay_out() {
-        const int row_bytes = a.dim * H::kCached;
-#pragma unroll
-        for (int j = 0; j < H::kLoads; ++j) {
-            const int i = j * H::kThreads + 64 * wave + lane, row = i / H::kFrom, piece = i % H::kFrom;
-            from[j] = 16 * piece < row_bytes ? (lane / H::kFrom) * row_bytes + 16 * piece : 0x7fffff00;
-#pragma unroll
-            for (int c = 0; c < H::kTo; ++c) {
-                k_to[j][c] = k_place(row, piece * H::kTo + c);
-                v_to[j][c] = v_place(row, piece * H::kTo + c);
-            }
-        }
+        const int row_bytes = a.dim * H::kCached, i = 64 * wave + lane;
+        at_row = i / H::kFrom;
+        at_piece = i % H::kFrom;                                                    // (the same in all loads)
+        from = 16 * at_piece < row_bytes ? (lane / H::kFrom) * row_bytes + 16 * at_piece : 0x7fffff00;
     }
     // Requests keys [t0, t0 + kKeys); zeros outside of [first, end).
     __device__ bool idle() const { return H::kSpare && 64 * wave >= H::kKeys * H::kFrom; }
@@ -181,7 +172,7 @@ struct Block {
             const int row = (j * H::kThreads + 64 * wave) / H::kFrom, t = t0 + row, mine = t + lane / H::kFrom;
             const int page = min(max(a.table[static_cast<long>(it.b) * a.table_pages + (min(t, end - 1) >> a.page_bits)], 0), a.pages - 1);
             const long at = ((static_cast<long>(page) * a.heads + head) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
-            const int there = mine >= first && mine < end ? from[j] : 0x7fffff00;
+            const int there = mine >= first && mine < end ? from : 0x7fffff00;
             const auto kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.k_pages) + at * row_bytes, 0, 16 * row_bytes, 0x00027000);
             const auto vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.v_pages) + at * row_bytes, 0, 16 * row_bytes, 0x00027000);
             k_raw[j] = __builtin_amdgcn_raw_buffer_load_b128(kr, there, 0, 0);
@@ -230,29 +221,45 @@ struct Block {
     }
     // Puts what came into buffer `to`.  `edge`: some row does not see some key of it, so that values that are not finite are looked for.
     __device__ void store(int to, int t0, bool edge) {
-        bool odd = false;
+        char *const k = lds.k[to], *const v = lds.v[to];
 #pragma unroll
         for (int j = 0; j < H::kLoads; ++j) {
             if (idle()) break;
             u32x4 out[H::kTo];
             widen(k_raw[j], F32 ? k_scale[F32 ? j : 0] : 1.f, out);
 #pragma unroll
-            for (int c = 0; c < H::kTo; ++c) *reinterpret_cast<u32x4*>(lds.k[to] + k_to[j][c]) = out[c];
+            for (int c = 0; c < H::kTo; ++c) *reinterpret_cast<u32x4*>(k + (k_place(at_row, at_piece * H::kTo + c) ^ 16 * (j * H::kStep & 15)) + j * H::kStep * H::kRowBytes) = out[c];
             widen(v_raw[j], F32 ? v_scale[F32 ? j : 0] : 1.f, out);
-#pragma unroll
-            for (int c = 0; c < H::kTo; ++c) *reinterpret_cast<u32x4*>(lds.v[to] + v_to[j][c]) = out[c];
             if (edge)
 #pragma unroll
-                for (int c = 0; c < H::kTo; ++c)
+                for (int c = 0; c < H::kTo; ++c) clear(to, t0, at_row + j * H::kStep, at_piece * H::kTo + c, out[c]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) odd |= not_finite<F32>(out[c][e]);
+            for (int c = 0; c < H::kTo; ++c) *reinterpret_cast<u32x4*>(v + v_place(at_row, at_piece * H::kTo + c) + j * H::kStep * H::kRowBytes) = out[c];
         }
-        if (odd) lds.odd[to] = t0 + 1;
         if constexpr (CACHE == MOE_E4M3 && !F32)
             if (wave == 0) {
                 lds.ks[to][lane] = k_scale[0] * a.scale;
                 lds.vs[to][lane] = v_scale[0];
             }
+    }
+    // Takes what is not finite out of a piece of V, and notes it.
+    __device__ void clear(int to, int t0, int row, int piece, u32x4& u) {
+        uint32_t up = 0, down = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int part = 0; part < (F32 ? 1 : 2); ++part) {
+                const uint32_t bits = F32 ? u[c] : part == 0 ? u[c] << 16 : u[c] & 0xffff0000u;
+                const float f = __uint_as_float(bits);
+                const bool more = !(f < INFINITY), less = !(f > -INFINITY);
+                const int bit = F32 ? c : 2 * c + part;
+                up |= more ? 1u << bit : 0u;
+                down |= less ? 1u << bit : 0u;
+                if (more || less) u[c] &= F32 ? 0u : part == 0 ? 0xffff0000u : 0xffffu;
+            }
+        lds.up[to][row][piece] = static_cast<unsigned char>(up);
+        lds.down[to][row][piece] = static_cast<unsigned char>(down);
+        if ((up | down) != 0) lds.odd[to] = t0 + 1;
     }
 
     // ---- a wave's 32 rows ----
@@ -266,8 +273,7 @@ struct Block {
 
     // A lane's part of S^T of a tile, as logits.
     __device__ void products(int buf, f32x16 (&s)[H::kBlocks]) const {
-        const char* k = lds.k[buf];
-        const int row = lane % 32, h = lane / 32;
+        const int at = buf * H::kTile + k_place(lane % 32, lane / 32);
 #pragma unroll
         for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
@@ -276,7 +282,7 @@ struct Block {
         for (int st = 0; st < kSteps; ++st)
 #pragma unroll
             for (int kb = 0; kb < H::kBlocks; ++kb) {
-                const u32x4 u = *reinterpret_cast<const u32x4*>(k + k_place(row, 2 * st + h) + 32 * kb * H::kRowBytes);
+                const u32x4 u = *reinterpret_cast<const u32x4*>(lds.k[0] + (at ^ (32 * st)) + 32 * kb * H::kRowBytes);
                 if constexpr (F32) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(u[c]), __uint_as_float(q[st][c]), s[kb], 0, 0, 0);
@@ -288,12 +294,12 @@ struct Block {
     // The key of sum i of a lane in block kb, from the tile's first.
     __device__ static constexpr int key_of(int kb, int i) { return 32 * kb + 8 * (i / 4) + i % 4; }
 
-    // O^T += V^T P^T for 16 keys (bf16) and 32 columns: what a lane reads of V.
-    __device__ bf16x8 turned(const char* v, int ks, int column) const {
-        const int r = (lane % 16) / 4, h = lane / 32;
-        const char* at = v + v_place(4 * h + r, 4 * column) + 32 * ((lane / 16) % 2) + 8 * (lane % 4) + 16 * ks * H::kRowBytes;
+    // What a lane reads of V for 16 keys (bf16) and 32 columns; at: v_at.
+    __device__ int v_at(int buf) const { return buf * H::kTile + v_place(4 * (lane / 32) + (lane % 16) / 4, 0) + 32 * ((lane / 16) % 2) + 8 * (lane % 4); }
+    __device__ bf16x8 turned(int at, int ks, int column) const {
+        const char* const from = lds.v[0] + (at ^ (64 * column)) + 16 * ks * H::kRowBytes;
         typedef __attribute__((address_space(3))) i16x4* Place;
-        const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 8 * H::kRowBytes));
+        const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(from)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(from + 8 * H::kRowBytes));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     }
     // In fp32 a lane reads the kColumns (up to four) neighbouring columns of one key that are its row of as many blocks.
@@ -311,7 +317,8 @@ struct Block {
         }
     }
 
-    __device__ void attend(int buf, int t0) {
+    // block_edge: some of the block's rows do not see some of the keys.
+    __device__ void attend(int buf, int t0, bool block_edge) {
         f32x16 s[H::kBlocks];
         products(buf, s);
         const int h = lane / 32;
@@ -352,7 +359,7 @@ struct Block {
                 for (int i = 0; i < 16; ++i) o[c][i] *= keep;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        const bool odd = edge && uniform(lds.odd[buf]) == t0 + 1;
+        const bool odd = block_edge && uniform(lds.odd[buf]) == t0 + 1;              // (then all waves' products have zeros there)
         uint32_t seen = 0;                                                          // odd: the lane's keys that count, 16 of a block
         if (odd)
 #pragma unroll
@@ -375,93 +382,60 @@ struct Block {
                 for (int i = 0; i < 16; i += 4) {
                     const f32x4 each = *reinterpret_cast<const f32x4*>(&lds.vs[buf][key_of(kb, i) + 4 * h]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) s[kb][i + c] = edge && s[kb][i + c] == 0.f ? 0.f : s[kb][i + c] * each[c];
+                    for (int c = 0; c < 4; ++c) s[kb][i + c] = edge && s[kb][i + c] == 0.f ? 0.f : s[kb][i + c] * each[c];           // (a scale that is not finite, of a key the row does not see)
                 }
-        if (odd) values<true>(buf, s, seen);
-        else values<false>(buf, s, 0);
+        values(buf, s);
+        if (odd) add_odd(buf, seen);
     }
 
-    // O^T += V^T P^T.  ODD: values that are not finite, under rows of which not all see them.  A weight of zero times such a value would be no number, so it
-    // is left out of the product, and put into the rows that see it: two further products count, for each row and column, the infinities of either sign
-    // (and NaN, which is both).
-    template <bool ODD>
-    __device__ void values(int buf, f32x16 (&p)[H::kBlocks], uint32_t seen) {
-        const char* v = lds.v[buf];
+    // O^T += V^T P^T.
+    __device__ void values(int buf, const f32x16 (&p)[H::kBlocks]) {
         if constexpr (F32) {
+            const char* const v = lds.v[buf];
 #pragma unroll
             for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
-                for (int g = 0; g < H::kColumns / kNear; ++g) {
-                    f32x16 more[ODD ? kNear : 1], less[ODD ? kNear : 1];
-                    if constexpr (ODD)
+                for (int i = 0; i < 16; ++i)
 #pragma unroll
-                        for (int c = 0; c < kNear; ++c)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) more[c][i] = less[c][i] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
+                    for (int g = 0; g < H::kColumns / kNear; ++g) {
                         float x[kNear];
                         beside(v, key_of(kb, i), g, x);
 #pragma unroll
-                        for (int c = 0; c < kNear; ++c) {
-                            if constexpr (ODD) {
-                                const float count = seen >> (16 * kb + i) & 1 ? 1.f : 0.f;
-                                const float up = x[c] < INFINITY ? 0.f : 1.f, down = x[c] > -INFINITY ? 0.f : 1.f;          // (both for NaN)
-                                more[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(up, count, more[c], 0, 0, 0);
-                                less[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(down, count, less[c], 0, 0, 0);
-                                x[c] = up + down == 0.f ? x[c] : 0.f;
-                            }
-                            o[kNear * g + c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[c], p[kb][i], o[kNear * g + c], 0, 0, 0);
-                        }
+                        for (int c = 0; c < kNear; ++c) o[kNear * g + c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[c], p[kb][i], o[kNear * g + c], 0, 0, 0);
                     }
-                    if constexpr (ODD)
-#pragma unroll
-                        for (int c = 0; c < kNear; ++c) add(o[kNear * g + c], more[c], less[c]);
-                }
         } else {
+            const int at = v_at(buf);
 #pragma unroll
             for (int ks = 0; ks < 2 * H::kBlocks; ++ks) {
-                u32x4 w, count;
+                u32x4 w;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int i = 8 * (ks % 2) + 2 * c;
-                    w[c] = to_bf16x2(p[ks / 2][i], p[ks / 2][i + 1]);
-                    if constexpr (ODD) count[c] = (seen >> (8 * ks + 2 * c) & 1 ? 0x3f80u : 0u) | (seen >> (8 * ks + 2 * c + 1) & 1 ? 0x3f800000u : 0u);
-                }
-                const bf16x8 weights = __builtin_bit_cast(bf16x8, w);
+                for (int c = 0; c < 4; ++c) w[c] = to_bf16x2(p[ks / 2][8 * (ks % 2) + 2 * c], p[ks / 2][8 * (ks % 2) + 2 * c + 1]);
 #pragma unroll
-                for (int c = 0; c < H::kColumns; ++c) {
-                    bf16x8 x = turned(v, ks, c);
-                    if constexpr (ODD) {
-                        const bf16x8 counts = __builtin_bit_cast(bf16x8, count);
-                        f32x16 more, less;
-                        bf16x8 up, down;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) more[i] = less[i] = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float f = static_cast<float>(x[i]);
-                            const bool u = !(f < INFINITY), d = !(f > -INFINITY);
-                            up[i] = static_cast<__bf16>(u ? 1.f : 0.f);
-                            down[i] = static_cast<__bf16>(d ? 1.f : 0.f);
-                            x[i] = u || d ? static_cast<__bf16>(0.f) : x[i];
-                        }
-                        more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, counts, more, 0, 0, 0);
-                        less = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down, counts, less, 0, 0, 0);
-                        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, weights, o[c], 0, 0, 0);
-                        add(o[c], more, less);
-                    } else {
-                        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, weights, o[c], 0, 0, 0);
-                    }
-                }
+                for (int c = 0; c < H::kColumns; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(at, ks, c), __builtin_bit_cast(bf16x8, w), o[c], 0, 0, 0);
             }
         }
     }
-    __device__ static void add(f32x16& o, const f32x16& more, const f32x16& less) {
+    // The column of sum i of a lane in block c.
+    __device__ int column_of(int c, int i) const {
+        const int row = 8 * (i / 4) + 4 * (lane / 32) + i % 4;
+        return F32 ? 128 * (c / kNear) + kNear * row + c % kNear : 32 * c + row;
+    }
+    // Values that are not finite under rows of which some may not see them: a weight of zero times such a value would be no number, so the product has zeros in
+    // their places, and the rows that see them get them here.
+    __device__ void add_odd(int buf, uint32_t seen) {
+        constexpr int kEach = 16 / H::kWidth;
+        const auto halves = __builtin_amdgcn_permlane32_swap(seen, seen, false, false);
+#pragma unroll 1
+        for (int key = 0; key < H::kKeys; ++key) {
+            const bool counts = halves[key / 4 % 2] >> (16 * (key / 32) + 4 * (key % 32 / 8) + key % 4) & 1;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            o[i] = more[i] > 0.f ? o[i] + INFINITY : o[i];
-            o[i] = less[i] > 0.f ? o[i] - INFINITY : o[i];
+            for (int c = 0; c < H::kColumns; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int column = column_of(c, i);
+                    if (counts && lds.up[buf][key][column / kEach] >> column % kEach & 1) o[c][i] += INFINITY;
+                    if (counts && lds.down[buf][key][column / kEach] >> column % kEach & 1) o[c][i] -= INFINITY;
+                }
         }
     }
 
@@ -591,7 +565,7 @@ struct Block {
                 __syncthreads();
                 const int next = t0 + H::kKeys;
                 if (next < end) load(next);
-                if (t0 < wave_end && next > wave_first) attend(buf, t0);
+                if (t0 < wave_end && next > wave_first) attend(buf, t0, edge(t0));
                 if (next < end) store(buf ^ 1, next, edge(next));
             }
         }
