@@ -45,6 +45,12 @@ __device__ inline int wave_min(int v) {
     return uniform(v);
 }
 __device__ inline int wave_max(int v) { return -wave_min(-v); }
+// A barrier for what lies in LDS: loads from memory stay on their way across it.
+__device__ inline void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
 // Over the two lanes that hold the same row.
 __device__ inline float halves_max(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -61,6 +67,9 @@ struct Shape {
     static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
     static constexpr int kKeys = F32 && DIM > 128 ? 32 : 64;                        // keys of a tile
     static constexpr int kBlocks = kKeys / 32, kColumns = DIM / 32;                 // S in 32 keys, O in 32 columns
+    static constexpr int kPerWord = F32 ? 1 : 2;                                    // weights in a register
+    static constexpr bool kTurns = WAVES == 8;                                      // two waves of the block share a SIMD: one multiplies while the other weighs
+    static constexpr int kDeep = kTurns ? 3 : 2;                                    // tiles in LDS
     static constexpr int kWidth = F32 ? 4 : 2, kCached = CACHE == MOE_F32 ? 4 : CACHE == MOE_BF16 ? 2 : 1;
     static constexpr int kRowBytes = DIM * kWidth, kPieces = kRowBytes / 16;        // a row in LDS
     static constexpr int kFrom = DIM * kCached / 16;                                // 16-byte pieces of a row as it comes
@@ -129,13 +138,14 @@ __device__ inline void stretch_of(const Prompt& a, const Item& it, int token, in
 template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
 struct Block {
     using H = Shape<F32, CACHE, DIM, WAVES>;
+    static constexpr bool kScaled = CACHE == MOE_E4M3 && !F32;                      // keys and values have scales, which their products do not
     struct Lds {
-        __attribute__((aligned(256))) char k[2][H::kTile], v[2][H::kTile];
-        float ks[2][H::kKeys], vs[2][H::kKeys];                                     // e4m3 and 16-bit products: scales of the keys, times a.scale, and of the values
+        __attribute__((aligned(256))) char k[H::kDeep][H::kTile], v[H::kDeep][H::kTile];
+        float ks[H::kDeep][H::kKeys], vs[H::kDeep][H::kKeys];                                    // kScaled: scales of the keys, times a.scale, and of the values, a tile ahead of them
         // Values that are not finite lie in v as zeros.  odd: 1 + the first key of a tile that has any; up, down: the bits of a piece's elements that
         // were infinity or NaN, and -infinity or NaN.
-        int odd[2];
-        unsigned char up[2][H::kKeys][H::kPieces], down[2][H::kKeys][H::kPieces];
+        int odd[H::kDeep];
+        unsigned char up[H::kDeep][H::kKeys][H::kPieces], down[H::kDeep][H::kKeys][H::kPieces];
     };
     const Prompt& a;
     Lds& lds;
@@ -162,37 +172,59 @@ struct Block {
         at_piece = i % H::kFrom;                                                    // (the same in all loads)
         from = 16 * at_piece < row_bytes ? (lane / H::kFrom) * row_bytes + 16 * at_piece : 0x7fffff00;
     }
-    // Requests keys [t0, t0 + kKeys); zeros outside of [first, end).
     __device__ bool idle() const { return H::kSpare && 64 * wave >= H::kKeys * H::kFrom; }
-    __device__ void load(int t0) {
+    // Where the rows of the wave's loads begin, looked up for kAsked tiles at once: lane kSlots s + j has load j of the s-th of them.
+    static constexpr int kSlots = H::kLoads <= 1 ? 1 : H::kLoads <= 2 ? 2 : H::kLoads <= 4 ? 4 : 8, kAsked = 64 / kSlots;
+    int ids, own_id;                                                                // the pages of the next kAsked tiles; kScaled, the first wave: of key `lane` of the next tile
+    uint32_t held[2];                                                               // rows of the present ones
+    struct Rows {
+        long at[H::kLoads];
+    };
+    __device__ long row_of(int id, int t) const {
+        return ((static_cast<long>(min(max(id, 0), a.pages - 1)) * a.heads + head) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
+    }
+    __device__ int page_of(int t) const { return a.table[static_cast<long>(it.b) * a.table_pages + (min(t, end - 1) >> a.page_bits)]; }
+    __device__ int asked(int t0) const { return t0 + lane / kSlots * H::kKeys + (lane % kSlots * H::kThreads + 64 * wave) / H::kFrom; }
+    __device__ void locate(int t0, int index, Rows& r) {                            // index: of the tile, from the first
+        if (index % kAsked == 0) {
+            const long row = row_of(ids, asked(t0));
+            held[0] = static_cast<uint32_t>(row);
+            held[1] = static_cast<uint32_t>(row >> 32);
+            ids = page_of(asked(t0 + kAsked * H::kKeys));
+        }
+#pragma unroll
+        for (int j = 0; j < H::kLoads; ++j) {
+            const int from_lane = (index % kAsked) * kSlots + j;
+            r.at[j] = static_cast<long>(static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(held[1], from_lane))) << 32 |
+                                        static_cast<uint32_t>(__builtin_amdgcn_readlane(held[0], from_lane)));
+        }
+    }
+    // Requests keys [t0, t0 + kKeys) of one side; zeros outside of [first, end).
+    __device__ void load(const char* pages, const float* scales, const Rows& r, int t0, u32x4 (&raw)[H::kLoads], float (&scale)[F32 ? H::kLoads : 1]) const {
         const int row_bytes = a.dim * H::kCached;
+        const bool whole = t0 >= first && t0 + H::kKeys <= end;
 #pragma unroll
         for (int j = 0; j < H::kLoads; ++j) {
             if (idle()) break;
-            const int row = (j * H::kThreads + 64 * wave) / H::kFrom, t = t0 + row, mine = t + lane / H::kFrom;
-            const int page = min(max(a.table[static_cast<long>(it.b) * a.table_pages + (min(t, end - 1) >> a.page_bits)], 0), a.pages - 1);
-            const long at = ((static_cast<long>(page) * a.heads + head) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
-            const int there = mine >= first && mine < end ? from : 0x7fffff00;
-            const auto kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.k_pages) + at * row_bytes, 0, 16 * row_bytes, 0x00027000);
-            const auto vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.v_pages) + at * row_bytes, 0, 16 * row_bytes, 0x00027000);
-            k_raw[j] = __builtin_amdgcn_raw_buffer_load_b128(kr, there, 0, 0);
-            v_raw[j] = __builtin_amdgcn_raw_buffer_load_b128(vr, there, 0, 0);
-            if constexpr (CACHE == MOE_E4M3 && F32) {
-                const int row4 = mine >= first && mine < end ? 4 * (lane / H::kFrom) : 0x7fffff00;
-                k_scale[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.k_scales) + at, 0, 64, 0x00027000), row4, 0, 0));
-                v_scale[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.v_scales) + at, 0, 64, 0x00027000), row4, 0, 0));
-            }
+            const int t = t0 + (j * H::kThreads + 64 * wave) / H::kFrom + lane / H::kFrom;
+            const bool there = whole || (t >= first && t < end);
+            const auto rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pages) + r.at[j] * row_bytes, 0, 16 * row_bytes, 0x00027000);
+            raw[j] = __builtin_amdgcn_raw_buffer_load_b128(rows, there ? from : 0x7fffff00, 0, 0);
+            if constexpr (CACHE == MOE_E4M3 && F32)
+                scale[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(scales) + r.at[j], 0, 64, 0x00027000),
+                                                                                there ? 4 * (lane / H::kFrom) : 0x7fffff00, 0, 0));
         }
-        if constexpr (CACHE == MOE_E4M3 && !F32)
+    }
+    __device__ void load_k(const Rows& r, int t0) {
+        load(a.k_pages, a.k_scales, r, t0, k_raw, k_scale);
+        if constexpr (kScaled)                                                      // the scales of keys and values, both a tile ahead: weights are made with them
             if (wave == 0) {
                 const int t = t0 + lane;
-                k_scale[0] = v_scale[0] = 0.f;
-                if (t >= first && t < end) {
-                    const int page = min(max(a.table[static_cast<long>(it.b) * a.table_pages + (t >> a.page_bits)], 0), a.pages - 1);
-                    const long at = ((static_cast<long>(page) * a.heads + head) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
-                    k_scale[0] = a.k_scales[at];
-                    v_scale[0] = a.v_scales[at];
-                }
+                const long row = row_of(own_id, t);
+                const bool there = t >= first && t < end;
+                k_scale[0] = there ? a.k_scales[row] : 0.f;
+                v_scale[0] = there ? a.v_scales[row] : 0.f;
+                own_id = page_of(t + H::kKeys);
             }
     }
     // One piece as it came in the form of the products.
@@ -219,9 +251,9 @@ struct Block {
             }
         }
     }
-    // Puts what came into buffer `to`.  `edge`: some row does not see some key of it, so that values that are not finite are looked for.
-    __device__ void store(int to, int t0, bool edge) {
-        char *const k = lds.k[to], *const v = lds.v[to];
+    // Put what came into buffer `to`.
+    __device__ void store_k(int to) {
+        char* const k = lds.k[to];
 #pragma unroll
         for (int j = 0; j < H::kLoads; ++j) {
             if (idle()) break;
@@ -229,6 +261,20 @@ struct Block {
             widen(k_raw[j], F32 ? k_scale[F32 ? j : 0] : 1.f, out);
 #pragma unroll
             for (int c = 0; c < H::kTo; ++c) *reinterpret_cast<u32x4*>(k + (k_place(at_row, at_piece * H::kTo + c) ^ 16 * (j * H::kStep & 15)) + j * H::kStep * H::kRowBytes) = out[c];
+        }
+        if constexpr (kScaled)
+            if (wave == 0) {
+                lds.ks[to][lane] = k_scale[0] * a.scale;
+                lds.vs[to][lane] = v_scale[0];
+            }
+    }
+    // `edge`: some row does not see some of these keys, so that values that are not finite are looked for.
+    __device__ void store_v(int to, int t0, bool edge) {
+        char* const v = lds.v[to];
+#pragma unroll
+        for (int j = 0; j < H::kLoads; ++j) {
+            if (idle()) break;
+            u32x4 out[H::kTo];
             widen(v_raw[j], F32 ? v_scale[F32 ? j : 0] : 1.f, out);
             if (edge)
 #pragma unroll
@@ -236,11 +282,6 @@ struct Block {
 #pragma unroll
             for (int c = 0; c < H::kTo; ++c) *reinterpret_cast<u32x4*>(v + v_place(at_row, at_piece * H::kTo + c) + j * H::kStep * H::kRowBytes) = out[c];
         }
-        if constexpr (CACHE == MOE_E4M3 && !F32)
-            if (wave == 0) {
-                lds.ks[to][lane] = k_scale[0] * a.scale;
-                lds.vs[to][lane] = v_scale[0];
-            }
     }
     // Takes what is not finite out of a piece of V, and notes it.
     __device__ void clear(int to, int t0, int row, int piece, u32x4& u) {
@@ -317,13 +358,22 @@ struct Block {
         }
     }
 
-    // block_edge: some of the block's rows do not see some of the keys.
-    __device__ void attend(int buf, int t0, bool block_edge) {
-        f32x16 s[H::kBlocks];
-        products(buf, s);
+    struct Weights {
+        uint32_t u[H::kBlocks][16 / H::kPerWord];
+        __device__ void set(int kb, int i, float x, float y) { u[kb][i / H::kPerWord] = F32 ? __float_as_uint(x) : to_bf16x2(x, y); }
+        __device__ void clear() {
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16 / H::kPerWord; ++i) u[kb][i] = 0;
+        }
+        // bf16: the operand of 16 keys
+        __device__ bf16x8 keys(int ks) const { return __builtin_bit_cast(bf16x8, u32x4{u[ks / 2][4 * (ks % 2)], u[ks / 2][4 * (ks % 2) + 1], u[ks / 2][4 * (ks % 2) + 2], u[ks / 2][4 * (ks % 2) + 3]}); }
+    };
+    // The weights of the keys of the tile at t0 from their products, as operands of the next product.  The sums of earlier tiles are brought to the maximum.
+    __device__ void weigh(f32x16 (&s)[H::kBlocks], Weights& w, int buf, int t0) {
         const int h = lane / 32;
         const bool edge = t0 < whole_from || t0 + H::kKeys > whole_to;
-        constexpr bool kScaled = CACHE == MOE_E4M3 && !F32;                         // scales of its own for each key
         const float scale = SCORED || kScaled ? 1.f : a.scale;
         if constexpr (SCORED || kScaled)
 #pragma unroll
@@ -359,37 +409,49 @@ struct Block {
                 for (int i = 0; i < 16; ++i) o[c][i] *= keep;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        const bool odd = block_edge && uniform(lds.odd[buf]) == t0 + 1;              // (then all waves' products have zeros there)
-        uint32_t seen = 0;                                                          // odd: the lane's keys that count, 16 of a block
-        if (odd)
-#pragma unroll
-            for (int kb = 0; kb < H::kBlocks; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) seen |= s[kb][i] == -INFINITY ? 0u : 1u << (16 * kb + i);
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], scale, -ref));
-                sum[i % 4] += s[kb][i];
-            }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        if constexpr (kScaled)
+            for (int i = 0; i < 16; i += 4) {
+                float p[4];
 #pragma unroll
-            for (int kb = 0; kb < H::kBlocks; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
+                for (int c = 0; c < 4; ++c) {
+                    p[c] = __builtin_amdgcn_exp2f(fmaf(s[kb][i + c], scale, -ref));
+                    sum[c] += p[c];
+                }
+                if constexpr (kScaled) {                                            // (a scale that is not finite may be that of a key the row does not see)
                     const f32x4 each = *reinterpret_cast<const f32x4*>(&lds.vs[buf][key_of(kb, i) + 4 * h]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) s[kb][i + c] = edge && s[kb][i + c] == 0.f ? 0.f : s[kb][i + c] * each[c];           // (a scale that is not finite, of a key the row does not see)
+                    for (int c = 0; c < 4; ++c) p[c] = edge && p[c] == 0.f ? 0.f : p[c] * each[c];
                 }
-        values(buf, s);
-        if (odd) add_odd(buf, seen);
+#pragma unroll
+                for (int c = 0; c < 4; c += H::kPerWord) w.set(kb, i + c, p[c], p[c + H::kPerWord - 1]);
+            }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+    // The order of the products of a tile: reads from LDS some of them ahead.
+    template <bool NEXT, bool THIS>
+    __device__ static void schedule() {
+        constexpr int kRead = 0x100, kProduct = 0x008, kAhead = 6;
+        constexpr int kFirst = NEXT ? kSteps * H::kBlocks : 0, kSecond = THIS ? 2 * H::kBlocks * H::kColumns : 0;
+        if constexpr (!F32) {
+            __builtin_amdgcn_sched_group_barrier(kRead, kAhead, 0);
+#pragma unroll
+            for (int i = 0; i < kFirst - kAhead; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+            }
+#pragma unroll
+            for (int i = kFirst > kAhead ? kFirst - kAhead : 0; i < kFirst + kSecond; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+            }
+        }
     }
 
     // O^T += V^T P^T.
-    __device__ void values(int buf, const f32x16 (&p)[H::kBlocks]) {
+    __device__ void values(int buf, const Weights& w) {
         if constexpr (F32) {
             const char* const v = lds.v[buf];
 #pragma unroll
@@ -401,18 +463,14 @@ struct Block {
                         float x[kNear];
                         beside(v, key_of(kb, i), g, x);
 #pragma unroll
-                        for (int c = 0; c < kNear; ++c) o[kNear * g + c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[c], p[kb][i], o[kNear * g + c], 0, 0, 0);
+                        for (int c = 0; c < kNear; ++c) o[kNear * g + c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[c], __uint_as_float(w.u[kb][i / H::kPerWord]), o[kNear * g + c], 0, 0, 0);
                     }
         } else {
             const int at = v_at(buf);
 #pragma unroll
-            for (int ks = 0; ks < 2 * H::kBlocks; ++ks) {
-                u32x4 w;
+            for (int ks = 0; ks < 2 * H::kBlocks; ++ks)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) w[c] = to_bf16x2(p[ks / 2][8 * (ks % 2) + 2 * c], p[ks / 2][8 * (ks % 2) + 2 * c + 1]);
-#pragma unroll
-                for (int c = 0; c < H::kColumns; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(at, ks, c), __builtin_bit_cast(bf16x8, w), o[c], 0, 0, 0);
-            }
+                for (int c = 0; c < H::kColumns; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(at, ks, c), w.keys(ks), o[c], 0, 0, 0);
         }
     }
     // The column of sum i of a lane in block c.
@@ -422,12 +480,11 @@ struct Block {
     }
     // Values that are not finite under rows of which some may not see them: a weight of zero times such a value would be no number, so the product has zeros in
     // their places, and the rows that see them get them here.
-    __device__ void add_odd(int buf, uint32_t seen) {
+    __device__ void add_odd(int buf, int t0) {
         constexpr int kEach = 16 / H::kWidth;
-        const auto halves = __builtin_amdgcn_permlane32_swap(seen, seen, false, false);
 #pragma unroll 1
         for (int key = 0; key < H::kKeys; ++key) {
-            const bool counts = halves[key / 4 % 2] >> (16 * (key / 32) + 4 * (key % 32 / 8) + key % 4) & 1;
+            const bool counts = static_cast<uint32_t>(t0 + key - lo) < static_cast<uint32_t>(hi - lo);
 #pragma unroll
             for (int c = 0; c < H::kColumns; ++c)
 #pragma unroll
@@ -550,23 +607,75 @@ struct Block {
         }
     }
 
+    // A wave weighs tile t (the exponentials), then multiplies: the keys of tile t + 1, the values of tile t.  With two waves of the block on a SIMD (kTurns) the
+    // second half of them, `late`, does it the other way round between two barriers, so that one of the two has the matrix pipes while the other weighs:
+    //     the first half   | weigh 0    multiply 0 | weigh 1    multiply 1 | ..
+    //     the second half  |            weigh 0    | multiply 0 weigh 1    | ..
+    // K of t + 1 and t and V of t and t - 1 are read between these barriers, and K of t + 2 and V of t + 1 put into LDS, by all waves while they weigh t: three
+    // buffers.  Where all waves are late, K of t and V of t - 1 are read, and K of t + 1 and V of t put there: two.
     __device__ void run() {
         lay_out();
         begin();
         if (first < end) {
+            const bool late = !H::kTurns || wave >= 4;
             const int base = first & ~(H::kKeys - 1);
             auto edge = [&](int t0) { return t0 < all_from || t0 + H::kKeys > all_to; };
-            load(base);
-            if (threadIdx.x < 2) lds.odd[threadIdx.x] = 0;
-            __syncthreads();
-            store(0, base, edge(base));
+            auto mine = [&](int t0) { return t0 < end && t0 < wave_end && t0 + H::kKeys > wave_first; };
+            auto after = [](int buf) { return buf == H::kDeep - 1 ? 0 : buf + 1; };
+            ids = page_of(asked(base));
+            own_id = kScaled ? page_of(base + lane) : 0;
+            Rows rows;                                                              // of the K that is on its way
+            locate(base, 0, rows);
+            load_k(rows, base);
+            if (threadIdx.x < H::kDeep) lds.odd[threadIdx.x] = 0;
+            if constexpr (H::kTurns) load(a.v_pages, a.v_scales, rows, base, v_raw, v_scale);
+            lds_barrier();
+            store_k(0);
+            int next = base, index = 0, to = 0;                                     // the tile whose K is on its way, its number and buffer; the V on its way is that before it
+            auto ask = [&](bool v) {
+                if (v && next < end) load(a.v_pages, a.v_scales, rows, next, v_raw, v_scale);
+                next += H::kKeys;
+                ++index;
+                to = after(to);
+                if (next < end) {
+                    locate(next, index, rows);
+                    load_k(rows, next);
+                }
+            };
+            auto put = [&] {
+                const int before = next - H::kKeys;
+                if (before < end) store_v(to == 0 ? H::kDeep - 1 : to - 1, before, edge(before));
+                if (next < end) store_k(to);
+            };
+            ask(!H::kTurns);
+            if constexpr (H::kTurns) {
+                put();
+                ask(true);
+            }
+            lds_barrier();
+            f32x16 s[H::kBlocks];
+            if (mine(base)) {
+                products(0, s);
+                schedule<true, false>();
+            }
             int buf = 0;
-            for (int t0 = base; t0 < end; t0 += H::kKeys, buf ^= 1) {
-                __syncthreads();
-                const int next = t0 + H::kKeys;
-                if (next < end) load(next);
-                if (t0 < wave_end && next > wave_first) attend(buf, t0, edge(t0));
-                if (next < end) store(buf ^ 1, next, edge(next));
+            for (int t0 = base; t0 < end; t0 += H::kKeys) {
+                if (!late) lds_barrier();
+                put();
+                ask(true);
+                const bool now = mine(t0);
+                Weights w;
+                if (now) weigh(s, w, buf, t0);
+                else w.clear();
+                if (late) lds_barrier();
+                const int then = after(buf);
+                if (now || mine(t0 + H::kKeys)) {                                   // (both products where one would do: the other's weights are zero, or its sums not used)
+                    products(then, s);
+                    values(buf, w);
+                    schedule<true, true>();
+                }
+                if (edge(t0) && uniform(lds.odd[buf]) == t0 + 1) add_odd(buf, t0);
+                buf = then;
             }
         }
         finish();
