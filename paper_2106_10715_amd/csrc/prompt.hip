@@ -12,6 +12,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "convert.h"
@@ -199,15 +200,15 @@ struct Block {
                                         static_cast<uint32_t>(__builtin_amdgcn_readlane(held[0], from_lane)));
         }
     }
-    // Requests keys [t0, t0 + kKeys) of one side; zeros outside of [first, end).
+    // Requests keys [t0, t0 + kKeys) of one side; zeros outside of [first, end), which a WHOLE tile does not reach.
+    template <bool WHOLE>
     __device__ void load(const char* pages, const float* scales, const Rows& r, int t0, u32x4 (&raw)[H::kLoads], float (&scale)[F32 ? H::kLoads : 1]) const {
         const int row_bytes = a.dim * H::kCached;
-        const bool whole = t0 >= first && t0 + H::kKeys <= end;
 #pragma unroll
         for (int j = 0; j < H::kLoads; ++j) {
             if (idle()) break;
             const int t = t0 + (j * H::kThreads + 64 * wave) / H::kFrom + lane / H::kFrom;
-            const bool there = whole || (t >= first && t < end);
+            const bool there = WHOLE || (t >= first && t < end);
             const auto rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pages) + r.at[j] * row_bytes, 0, 16 * row_bytes, 0x00027000);
             raw[j] = __builtin_amdgcn_raw_buffer_load_b128(rows, there ? from : 0x7fffff00, 0, 0);
             if constexpr (CACHE == MOE_E4M3 && F32)
@@ -215,13 +216,14 @@ struct Block {
                                                                                 there ? 4 * (lane / H::kFrom) : 0x7fffff00, 0, 0));
         }
     }
+    template <bool WHOLE>
     __device__ void load_k(const Rows& r, int t0) {
-        load(a.k_pages, a.k_scales, r, t0, k_raw, k_scale);
+        load<WHOLE>(a.k_pages, a.k_scales, r, t0, k_raw, k_scale);
         if constexpr (kScaled)                                                      // the scales of keys and values, both a tile ahead: weights are made with them
             if (wave == 0) {
                 const int t = t0 + lane;
                 const long row = row_of(own_id, t);
-                const bool there = t >= first && t < end;
+                const bool there = WHOLE || (t >= first && t < end);
                 k_scale[0] = there ? a.k_scales[row] : 0.f;
                 v_scale[0] = there ? a.v_scales[row] : 0.f;
                 own_id = page_of(t + H::kKeys);
@@ -371,9 +373,11 @@ struct Block {
         __device__ bf16x8 keys(int ks) const { return __builtin_bit_cast(bf16x8, u32x4{u[ks / 2][4 * (ks % 2)], u[ks / 2][4 * (ks % 2) + 1], u[ks / 2][4 * (ks % 2) + 2], u[ks / 2][4 * (ks % 2) + 3]}); }
     };
     // The weights of the keys of the tile at t0 from their products, as operands of the next product.  The sums of earlier tiles are brought to the maximum.
+    // PLAIN: the wave's rows see all of them.
+    template <bool PLAIN>
     __device__ void weigh(f32x16 (&s)[H::kBlocks], Weights& w, int buf, int t0) {
         const int h = lane / 32;
-        const bool edge = t0 < whole_from || t0 + H::kKeys > whole_to;
+        const bool edge = !PLAIN && (t0 < whole_from || t0 + H::kKeys > whole_to);
         const float scale = SCORED || kScaled ? 1.f : a.scale;
         if constexpr (SCORED || kScaled)
 #pragma unroll
@@ -626,31 +630,34 @@ struct Block {
             own_id = kScaled ? page_of(base + lane) : 0;
             Rows rows;                                                              // of the K that is on its way
             locate(base, 0, rows);
-            load_k(rows, base);
+            load_k<false>(rows, base);
             if (threadIdx.x < H::kDeep) lds.odd[threadIdx.x] = 0;
-            if constexpr (H::kTurns) load(a.v_pages, a.v_scales, rows, base, v_raw, v_scale);
+            if constexpr (H::kTurns) load<false>(a.v_pages, a.v_scales, rows, base, v_raw, v_scale);
             lds_barrier();
             store_k(0);
             int next = base, index = 0, to = 0;                                     // the tile whose K is on its way, its number and buffer; the V on its way is that before it
-            auto ask = [&](bool v) {
-                if (v && next < end) load(a.v_pages, a.v_scales, rows, next, v_raw, v_scale);
+            auto ask = [&](auto plain, bool v) {
+                constexpr bool kPlain = decltype(plain)::value;
+                if (kPlain || (v && next < end)) load<kPlain>(a.v_pages, a.v_scales, rows, next, v_raw, v_scale);
                 next += H::kKeys;
                 ++index;
                 to = after(to);
-                if (next < end) {
+                if (kPlain || next < end) {
                     locate(next, index, rows);
-                    load_k(rows, next);
+                    load_k<kPlain>(rows, next);
                 }
             };
-            auto put = [&] {
+            auto put = [&](auto plain) {
+                constexpr bool kPlain = decltype(plain)::value;
                 const int before = next - H::kKeys;
-                if (before < end) store_v(to == 0 ? H::kDeep - 1 : to - 1, before, edge(before));
-                if (next < end) store_k(to);
+                if (kPlain || before < end) store_v(to == 0 ? H::kDeep - 1 : to - 1, before, !kPlain && edge(before));
+                if (kPlain || next < end) store_k(to);
             };
-            ask(!H::kTurns);
+            constexpr std::false_type kAny;
+            ask(kAny, !H::kTurns);
             if constexpr (H::kTurns) {
-                put();
-                ask(true);
+                put(kAny);
+                ask(kAny, true);
             }
             lds_barrier();
             f32x16 s[H::kBlocks];
@@ -658,24 +665,37 @@ struct Block {
                 products(0, s);
                 schedule<true, false>();
             }
-            int buf = 0;
-            for (int t0 = base; t0 < end; t0 += H::kKeys) {
+            // Tiles at t0 from plain_from to plain_to: the wave's rows see all of it and the block's all of the tiles that are put or asked for meanwhile.
+            constexpr int kLead = H::kDeep - 1;
+            const int plain_from = max(max(all_from, whole_from), max(first, wave_first));
+            const int plain_to = min(min(end - (kLead + 2) * H::kKeys, all_to - kLead * H::kKeys), min(whole_to - H::kKeys, wave_end - 2 * H::kKeys));
+            int buf = 0, t0 = base;
+            auto step = [&](auto plain) {
+                constexpr bool kPlain = decltype(plain)::value;
                 if (!late) lds_barrier();
-                put();
-                ask(true);
-                const bool now = mine(t0);
+                put(plain);
+                ask(plain, true);
+                const bool now = kPlain || mine(t0);
                 Weights w;
-                if (now) weigh(s, w, buf, t0);
+                if (now) weigh<kPlain>(s, w, buf, t0);
                 else w.clear();
                 if (late) lds_barrier();
+                __builtin_amdgcn_sched_barrier(0);
                 const int then = after(buf);
                 if (now || mine(t0 + H::kKeys)) {                                   // (both products where one would do: the other's weights are zero, or its sums not used)
                     products(then, s);
                     values(buf, w);
                     schedule<true, true>();
                 }
-                if (edge(t0) && uniform(lds.odd[buf]) == t0 + 1) add_odd(buf, t0);
+                if (!kPlain && edge(t0) && uniform(lds.odd[buf]) == t0 + 1) add_odd(buf, t0);
+                __builtin_amdgcn_sched_barrier(0);
                 buf = then;
+                t0 += H::kKeys;
+            };
+            while (t0 < end) {
+                step(kAny);
+#pragma unroll 1
+                while (t0 >= plain_from && t0 <= plain_to) step(std::true_type());
             }
         }
         finish();
