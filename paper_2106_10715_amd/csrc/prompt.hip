@@ -369,6 +369,13 @@ struct Block {
 #pragma unroll
                 for (int i = 0; i < 16 / H::kPerWord; ++i) u[kb][i] = 0;
         }
+        // They are made before what follows (the compiler would move the exponentials past the barrier, to the products).
+        __device__ void hold() {
+#pragma unroll
+            for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16 / H::kPerWord; ++i) asm volatile("" : "+v"(u[kb][i]));
+        }
         // bf16: the operand of 16 keys
         __device__ bf16x8 keys(int ks) const { return __builtin_bit_cast(bf16x8, u32x4{u[ks / 2][4 * (ks % 2)], u[ks / 2][4 * (ks % 2) + 1], u[ks / 2][4 * (ks % 2) + 2], u[ks / 2][4 * (ks % 2) + 3]}); }
     };
@@ -679,13 +686,16 @@ struct Block {
                 Weights w;
                 if (now) weigh<kPlain>(s, w, buf, t0);
                 else w.clear();
+                w.hold();
                 if (late) lds_barrier();
                 __builtin_amdgcn_sched_barrier(0);
                 const int then = after(buf);
                 if (now || mine(t0 + H::kKeys)) {                                   // (both products where one would do: the other's weights are zero, or its sums not used)
+                    __builtin_amdgcn_s_setprio(1);
                     products(then, s);
                     values(buf, w);
                     schedule<true, true>();
+                    __builtin_amdgcn_s_setprio(0);
                 }
                 if (!kPlain && edge(t0) && uniform(lds.odd[buf]) == t0 + 1) add_odd(buf, t0);
                 __builtin_amdgcn_sched_barrier(0);
