@@ -71,6 +71,7 @@ struct Shape {
     static constexpr int kPerWord = F32 ? 1 : 2;                                    // weights in a register
     static constexpr bool kTurns = WAVES == 8;                                      // two waves of the block share a SIMD: one multiplies while the other weighs
     static constexpr int kDeep = kTurns ? 3 : 2;                                    // tiles in LDS
+    static constexpr int kBias = F32 || DIM > 64 ? 2240 : 4096;                     // biases in LDS, a block's share of it left
     static constexpr int kWidth = F32 ? 4 : 2, kCached = CACHE == MOE_F32 ? 4 : CACHE == MOE_BF16 ? 2 : 1;
     static constexpr int kRowBytes = DIM * kWidth, kPieces = kRowBytes / 16;        // a row in LDS
     static constexpr int kFrom = DIM * kCached / 16;                                // 16-byte pieces of a row as it comes
@@ -146,12 +147,17 @@ struct Block {
         // Values that are not finite lie in v as zeros.  odd: 1 + the first key of a tile that has any; up, down: the bits of a piece's elements that
         // were infinity or NaN, and -infinity or NaN.
         int odd[H::kDeep];
-        unsigned char up[H::kDeep][H::kKeys][H::kPieces], down[H::kDeep][H::kKeys][H::kPieces];
+        __attribute__((aligned(16))) unsigned char up[H::kDeep][H::kKeys][H::kPieces], down[H::kDeep][H::kKeys][H::kPieces];
+        float bias[SCORED ? H::kBias : 1];                                          // the group's biases times log2 e, if there is room for them, their ends repeated
     };
+    // A wave's rows are of up to 32 neighbouring tokens: a tile that has a distance within the biases has none that is further outside of them than this.
+    static constexpr int kPad = 100;
     const Prompt& a;
     Lds& lds;
     const Item& it;
     int head, lane, wave;                                                           // key head
+    int width;                                                                      // a head's biases in LDS
+    bool tabled;                                                                    // whether they are there
     int first, end, all_from, all_to;                                               // keys that some of the block's rows see; that all of them see
 
     // ---- a tile from the cache to LDS ----
@@ -159,6 +165,7 @@ struct Block {
     float k_scale[F32 ? H::kLoads : 1], v_scale[F32 ? H::kLoads : 1];               // e4m3: of the rows, or (16-bit products) of key `lane`
     int from;                                                                       // of this lane: bytes from its wave's first row
     int at_row, at_piece;                                                           // of this lane: row and piece (as it comes) of its first load
+    uint32_t stale;                                                                 // the buffers, by bits, for which the wave has noted values that are not finite
 
     // Pieces of a row lie in LDS at places that differ from row to row, so that rows of a column are in different banks: a column of K is read 16 bytes by row,
     // of V in 64 bytes of four rows.  A piece's number and the row's change of it are combined by exclusive or, so that from one piece's place the others' follow.
@@ -167,7 +174,27 @@ struct Block {
         if constexpr (F32) return row * H::kRowBytes + 16 * piece;
         else return row * H::kRowBytes + 16 * (piece ^ (H::kPieces >= 16 ? 4 * (row & 3) : 4 * ((row >> 1) & 1)));
     }
+    // What lies in LDS from the beginning.
+    __device__ void set_up() {
+        if (threadIdx.x < H::kDeep) lds.odd[threadIdx.x] = 0;
+        stale = 0;
+        static_assert(sizeof(lds.up) % 16 == 0, "cleared 16 bytes at a time");
+        for (int i = threadIdx.x; i < static_cast<int>(sizeof(lds.up) / 16); i += H::kThreads) {
+            reinterpret_cast<u32x4*>(lds.up)[i] = u32x4{0, 0, 0, 0};
+            reinterpret_cast<u32x4*>(lds.down)[i] = u32x4{0, 0, 0, 0};
+        }
+        if constexpr (SCORED)
+            if (tabled)
+                for (int i = threadIdx.x; i < a.group * width; i += H::kThreads) {
+                    const int h = i / width, d = i - h * width - kPad;
+                    lds.bias[i] = a.scores.bias[static_cast<long>(head * a.group + h) * (width - 2 * kPad) + min(max(d, 0), width - 2 * kPad - 1)] * kLog2E;
+                }
+    }
     __device__ void lay_out() {
+        if constexpr (SCORED) {
+            width = a.scores.back + a.scores.ahead + 1 + 2 * kPad;
+            tabled = a.scores.bias != nullptr && static_cast<long>(a.group) * width <= H::kBias;
+        }
         const int row_bytes = a.dim * H::kCached, i = 64 * wave + lane;
         at_row = i / H::kFrom;
         at_piece = i % H::kFrom;                                                    // (the same in all loads)
@@ -272,13 +299,42 @@ struct Block {
     }
     // `edge`: some row does not see some of these keys, so that values that are not finite are looked for.
     __device__ void store_v(int to, int t0, bool edge) {
+        if (edge) {
+            uint32_t most = 0;                                                      // (bf16: of two, side by side)
+#pragma unroll
+            for (int j = 0; j < H::kLoads; ++j) {
+                if (idle()) break;
+                u32x4 out[H::kTo];
+                widen(v_raw[j], F32 ? v_scale[F32 ? j : 0] : 1.f, out);
+#pragma unroll
+                for (int c = 0; c < 4 * H::kTo; ++c) {
+                    const uint32_t u = out[c / 4][c % 4];
+                    if constexpr (F32) {
+                        most = max(most, u & 0x7fffffffu);
+                    } else {
+                        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+                        most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most), __builtin_bit_cast(u16x2, u & 0x7fff7fffu)));
+                    }
+                }
+            }
+            const bool odd = most >= 0x7f800000u || (!F32 && (most & 0xffffu) >= 0x7f80u);
+            if (__any(odd) || (stale >> to & 1) != 0) {
+                put_v<true>(to, t0);
+                stale = (stale & ~(1u << to)) | (__any(odd) ? 1u << to : 0u);
+                return;
+            }
+        }
+        put_v<false>(to, t0);
+    }
+    template <bool ODD>
+    __device__ void put_v(int to, int t0) {
         char* const v = lds.v[to];
 #pragma unroll
         for (int j = 0; j < H::kLoads; ++j) {
             if (idle()) break;
             u32x4 out[H::kTo];
             widen(v_raw[j], F32 ? v_scale[F32 ? j : 0] : 1.f, out);
-            if (edge)
+            if constexpr (ODD)
 #pragma unroll
                 for (int c = 0; c < H::kTo; ++c) clear(to, t0, at_row + j * H::kStep, at_piece * H::kTo + c, out[c]);
 #pragma unroll
@@ -310,7 +366,7 @@ struct Block {
     u32x4 q[kSteps];
     f32x16 o[H::kColumns];
     float m, l;
-    int lo, hi, place;                                                              // of this lane's row
+    int lo, hi, place, own;                                                         // of this lane's row; own: its query head in the group
     int wave_first, wave_end, whole_from, whole_to;                                 // keys that some of the wave's rows see; that all of them see
     HeadScores<true> hs;
 
@@ -385,17 +441,17 @@ struct Block {
     __device__ void weigh(f32x16 (&s)[H::kBlocks], Weights& w, int buf, int t0) {
         const int h = lane / 32;
         const bool edge = !PLAIN && (t0 < whole_from || t0 + H::kKeys > whole_to);
-        const float scale = SCORED || kScaled ? 1.f : a.scale;
-        if constexpr (SCORED || kScaled)
+        float mult = kScaled ? 1.f : a.scale, shift = 0.f;
+        if constexpr (kScaled)
 #pragma unroll
             for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
-                    const f32x4 each = kScaled ? *reinterpret_cast<const f32x4*>(&lds.ks[buf][key_of(kb, i) + 4 * h]) : f32x4{a.scale, a.scale, a.scale, a.scale};
+                    const f32x4 each = *reinterpret_cast<const f32x4*>(&lds.ks[buf][key_of(kb, i) + 4 * h]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) s[kb][i + c] *= each[c];
                 }
-        if constexpr (SCORED) score(s, t0);
+        if constexpr (SCORED) score(s, t0, mult, shift);
         if (edge)
 #pragma unroll
             for (int kb = 0; kb < H::kBlocks; ++kb)
@@ -409,7 +465,7 @@ struct Block {
         for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-        top = halves_max(top) * scale;
+        top = halves_max(fmaf(top, mult, shift));
         if (__any(top > m + kSlack)) {                                              // (always where m is still -inf and some key counts)
             const float now = fmaxf(m, top), keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
             m = now;
@@ -428,7 +484,7 @@ struct Block {
                 float p[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    p[c] = __builtin_amdgcn_exp2f(fmaf(s[kb][i + c], scale, -ref));
+                    p[c] = __builtin_amdgcn_exp2f(fmaf(s[kb][i + c], mult, shift - ref));
                     sum[c] += p[c];
                 }
                 if constexpr (kScaled) {                                            // (a scale that is not finite may be that of a key the row does not see)
@@ -507,32 +563,56 @@ struct Block {
         }
     }
 
-    __device__ void score(f32x16 (&s)[H::kBlocks], int t0) const {
+    // Logits are then s * mult + shift.
+    __device__ void score(f32x16 (&s)[H::kBlocks], int t0, float& mult, float& shift) const {
         const int d0 = place - t0 - 4 * (lane / 32);                                // the distance of the lane's first key
-        if (a.scores.cap > 0.f)
+        if (a.scores.cap > 0.f) {
 #pragma unroll
             for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; i += 8) {
                     float x[8];
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) x[c] = s[kb][i + c];
+                    for (int c = 0; c < 8; ++c) x[c] = s[kb][i + c] * mult;
                     cap_scores(a.scores, x);
 #pragma unroll
                     for (int c = 0; c < 8; ++c) s[kb][i + c] = x[c];
                 }
-        if (a.scores.slopes != nullptr)
+            mult = 1.f;
+        }
+        if (a.scores.slopes != nullptr) {
+            const float slope = hs.slope / mult;
+            if (__all(d0 >= H::kKeys - 1)) {                                        // all of the keys before the rows: |d| = d0 - key
+                shift = -hs.slope * static_cast<float>(d0);
 #pragma unroll
-            for (int kb = 0; kb < H::kBlocks; ++kb)
+                for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(-hs.slope, fabsf(static_cast<float>(d0 - key_of(kb, i))), s[kb][i]);
+                    for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(slope, static_cast<float>(key_of(kb, i)), s[kb][i]);
+            } else {
+#pragma unroll
+                for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(-slope, fabsf(static_cast<float>(d0 - key_of(kb, i))), s[kb][i]);
+            }
+        }
         if (a.scores.bias != nullptr) {
-            const int far = H::kKeys - 1;
-            const bool behind = __all(d0 - far >= a.scores.back), ahead = __all(d0 <= -a.scores.ahead);
+            const bool behind = __all(d0 - (H::kKeys - 1) >= a.scores.back), ahead = __all(d0 <= -a.scores.ahead);
+            if (behind || ahead) {
+                shift += behind ? hs.last : hs.first[0];
+            } else if (tabled) {
+                const float* const from = &lds.bias[own * width + d0 + a.scores.ahead + kPad - (H::kKeys - 1)];
 #pragma unroll
-            for (int kb = 0; kb < H::kBlocks; ++kb)
+                for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[kb][i] += hs.bias(a.scores, d0 - key_of(kb, i), !behind && !ahead);
+                    for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(s[kb][i], mult, from[H::kKeys - 1 - key_of(kb, i)]);
+                mult = 1.f;
+            } else {
+#pragma unroll
+                for (int kb = 0; kb < H::kBlocks; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(s[kb][i], mult, hs.bias(a.scores, d0 - key_of(kb, i), true));
+                mult = 1.f;
+            }
         }
     }
 
@@ -557,8 +637,9 @@ struct Block {
         all_to = wave_min(first_high);
         const int row = it.row0 + 32 * wave + lane % 32;
         const bool real = row < it.rows;
-        const int token = real ? row / a.group : 0, in_group = real ? row - token * a.group : 0;
+        const int token = real ? row / a.group : tokens - 1, in_group = real ? row - token * a.group : 0;
         place = it.place0 + token;
+        own = in_group;
         stretch_of(a, it, token, lo, hi);
         if (!real) {                                                                // rows past the last: as if they saw all, and not stored
             lo = 0;
@@ -638,7 +719,7 @@ struct Block {
             Rows rows;                                                              // of the K that is on its way
             locate(base, 0, rows);
             load_k<false>(rows, base);
-            if (threadIdx.x < H::kDeep) lds.odd[threadIdx.x] = 0;
+            set_up();
             if constexpr (H::kTurns) load<false>(a.v_pages, a.v_scales, rows, base, v_raw, v_scale);
             lds_barrier();
             store_k(0);
