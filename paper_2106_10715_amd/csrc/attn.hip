@@ -1044,7 +1044,7 @@ int launch_attn_decode(const moe_kv_cfg& kv, const moe_attn_cfg& c, const void* 
 int launch_attn_decode_scored(const moe_kv_cfg& kv, const moe_attn_cfg& c, const Scores& scores, const void* q, long q_stride, const void* k_pages,
                               const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens,
                               void* out, float* lse, void* ws, hipStream_t s) {
-    return for_types<true>(kv, c, ScoreArgs(scores), q, q_stride, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws, s);
+    return for_types<true>(kv, c, ScoreArgs(scores, kv.dtype), q, q_stride, k_pages, v_pages, k_scales, v_scales, table, lens, out, lse, ws, s);
 }
 #endif
 

@@ -65,9 +65,12 @@ __device__ inline float halves_sum(float v) {
 // How a block of WAVES waves holds its tiles.
 template <bool F32, int CACHE, int DIM, int WAVES>
 struct Shape {
-    static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
-    static constexpr int kKeys = F32 && DIM > 128 ? 32 : 64;                        // keys of a tile
-    static constexpr int kBlocks = kKeys / 32, kColumns = DIM / 32;                 // S in 32 keys, O in 32 columns
+    // Rows of over 128 columns in 16 bits have two waves, which both make their weights and have half of the columns of O each: with all of them a wave has no room
+    // in 256 registers, and with 512 the compiler moves O from accumulation registers and back in every tile (8192 tokens in documents, 16 heads: 328 us).
+    static constexpr int kShare = !F32 && DIM > 128 ? 2 : 1;
+    static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES / kShare;
+    static constexpr int kKeys = DIM > 128 ? 32 : 64;                               // keys of a tile
+    static constexpr int kBlocks = kKeys / 32, kColumns = DIM / 32 / kShare;        // S in 32 keys, O of a wave in 32 columns
     static constexpr int kPerWord = F32 ? 1 : 2;                                    // weights in a register
     static constexpr bool kTurns = WAVES == 8;                                      // two waves of the block share a SIMD: one multiplies while the other weighs
     static constexpr int kDeep = kTurns ? 3 : 2;                                    // tiles in LDS
@@ -156,6 +159,7 @@ struct Block {
     Lds& lds;
     const Item& it;
     int head, lane, wave;                                                           // key head
+    int wave_rows, wave_column;                                                     // a wave's first row in the block, and its first 32 columns of O
     int width;                                                                      // a head's biases in LDS
     bool tabled;                                                                    // whether they are there
     int first, end, all_from, all_to;                                               // keys that some of the block's rows see; that all of them see
@@ -292,7 +296,7 @@ struct Block {
             for (int c = 0; c < H::kTo; ++c) *reinterpret_cast<u32x4*>(k + (k_place(at_row, at_piece * H::kTo + c) ^ 16 * (j * H::kStep & 15)) + j * H::kStep * H::kRowBytes) = out[c];
         }
         if constexpr (kScaled)
-            if (wave == 0) {
+            if (wave == 0 && lane < H::kKeys) {
                 lds.ks[to][lane] = k_scale[0] * a.scale;
                 lds.vs[to][lane] = v_scale[0];
             }
@@ -537,13 +541,13 @@ struct Block {
 #pragma unroll
             for (int ks = 0; ks < 2 * H::kBlocks; ++ks)
 #pragma unroll
-                for (int c = 0; c < H::kColumns; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(at, ks, c), w.keys(ks), o[c], 0, 0, 0);
+                for (int c = 0; c < H::kColumns; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(at, ks, wave_column + c), w.keys(ks), o[c], 0, 0, 0);
         }
     }
     // The column of sum i of a lane in block c.
     __device__ int column_of(int c, int i) const {
         const int row = 8 * (i / 4) + 4 * (lane / 32) + i % 4;
-        return F32 ? 128 * (c / kNear) + kNear * row + c % kNear : 32 * c + row;
+        return F32 ? 128 * (c / kNear) + kNear * row + c % kNear : 32 * (wave_column + c) + row;
     }
     // Values that are not finite under rows of which some may not see them: a weight of zero times such a value would be no number, so the product has zeros in
     // their places, and the rows that see them get them here.
@@ -635,7 +639,7 @@ struct Block {
         end = wave_max(high);
         all_from = wave_max(last_low);
         all_to = wave_min(first_high);
-        const int row = it.row0 + 32 * wave + lane % 32;
+        const int row = it.row0 + wave_rows + lane % 32;
         const bool real = row < it.rows;
         const int token = real ? row / a.group : tokens - 1, in_group = real ? row - token * a.group : 0;
         place = it.place0 + token;
@@ -669,12 +673,12 @@ struct Block {
 
     __device__ void finish() {
         l = halves_sum(l);
-        const int row = it.row0 + 32 * wave + lane % 32, h = lane / 32;
+        const int row = it.row0 + wave_rows + lane % 32, h = lane / 32;
         if (row >= it.rows) return;
         const int token = row / a.group;
         const long at = static_cast<long>(it.token0 + token) * a.heads * a.group + head * a.group + (row - token * a.group);
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        if (h == 0 && a.lse != nullptr) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        if (h == 0 && wave_column == 0 && a.lse != nullptr) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
         if constexpr (F32) {
 #pragma unroll
             for (int g = 0; g < H::kColumns / kNear; ++g)
@@ -691,7 +695,7 @@ struct Block {
             for (int c = 0; c < H::kColumns; ++c)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
-                    const int d = 32 * c + 8 * (i / 4) + 4 * h;
+                    const int d = 32 * (wave_column + c) + 8 * (i / 4) + 4 * h;
                     if (d >= a.dim) continue;
                     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at * a.dim + d) =
                         u32x2{to_bf16x2(o[c][i] * inv, o[c][i + 1] * inv), to_bf16x2(o[c][i + 2] * inv, o[c][i + 3] * inv)};
@@ -794,10 +798,10 @@ struct Block {
 };
 
 // Waves that a SIMD has room for: with two, a wave has 256 registers.
-constexpr int waves_of(bool f32, int dim) { return f32 || dim > 128 ? 1 : 2; }
+constexpr int waves_of(bool f32) { return f32 ? 1 : 2; }
 
 template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
-__global__ __launch_bounds__(64 * WAVES, waves_of(F32, DIM)) void prompt_kernel(Prompt a) {
+__global__ __launch_bounds__(64 * WAVES, waves_of(F32)) void prompt_kernel(Prompt a) {
     using B = Block<F32, CACHE, DIM, WAVES, SCORED>;
     __shared__ typename B::Lds lds;
     Item it;
@@ -807,12 +811,14 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(F32, DIM)) void prompt_kernel(
     block.head = blockIdx.x % a.heads;
     block.lane = threadIdx.x % 64;
     block.wave = uniform(threadIdx.x / 64);
+    block.wave_rows = 32 * (block.wave % (WAVES / B::H::kShare));
+    block.wave_column = block.wave / (WAVES / B::H::kShare) * B::H::kColumns;
     block.run();
 }
 
 template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
 int launch(const Prompt& a, hipStream_t s) {
-    const long tiles = static_cast<long>(a.tokens) * a.group / (32 * WAVES) + std::min(a.B, a.tokens);       // (a sequence's last tile may not be full)
+    const long tiles = static_cast<long>(a.tokens) * a.group / Shape<F32, CACHE, DIM, WAVES>::kRows + std::min(a.B, a.tokens);       // (a sequence's last tile may not be full)
     hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED>), dim3(static_cast<unsigned>(tiles * a.heads)), dim3(64 * WAVES), 0, s, a);
     MOE_LAUNCH_CHECK("prompt_kernel");
     return MOE_OK;
@@ -820,7 +826,8 @@ int launch(const Prompt& a, hipStream_t s) {
 
 template <bool F32, int CACHE, int DIM, bool SCORED>
 int for_waves(const Prompt& a, hipStream_t s) {
-    if constexpr (!F32 && DIM <= 128)
+    if constexpr (!F32 && DIM > 128) return launch<F32, CACHE, DIM, 8, SCORED>(a, s);
+    else if constexpr (!F32)
         if (static_cast<long>(a.tokens) * a.group * a.heads >= 256 * 256L) return launch<F32, CACHE, DIM, 8, SCORED>(a, s);
     return launch<F32, CACHE, DIM, 4, SCORED>(a, s);
 }
@@ -869,7 +876,7 @@ int launch_attn_prompt(const moe_kv_cfg& kv, const moe_prompt_cfg& c, const Scor
     a.table_pages = c.table_pages;
     a.window = c.window;
     a.scale = (c.scale > 0.f ? c.scale : 1.f / sqrtf(static_cast<float>(kv.head_dim))) * kLog2E;
-    a.scores = ScoreArgs(scores);
+    a.scores = ScoreArgs(scores, kv.dtype);
     return scores.any() ? for_types<true>(kv, a, s) : for_types<false>(kv, a, s);
 }
 

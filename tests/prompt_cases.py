@@ -3,7 +3,9 @@
 Tolerance, per element, of an attention row of n keys with weights p (they sum to 1), A = sum p |v| and logits l:
   the sum q . k in fp32 (dim + 8 roundings of at most sum |q k| scale), its scaling, the tanh (within 8 * 2^-24 of its value), the bias and the slope's
   product, each within 2^-23 of the largest term: a logit is off by
-      off = 2^-24 ((dim + 8) scale max sum |q k| + 16 max |l| + 4 max |bias| + 4 max |slope distance|),
+      off = 2^-24 ((dim + 8) scale max sum |q k| + 16 max |l| + 4 max |bias| + 4 max |slope distance| + 8 cap),
+  (the last with bf16 activations and caps up to 64, where the tanh is 1 - 2 / (e + 1), e = exp 2z: its exponent and e are off by 2^-23 of e each, what
+  changes the quotient by at most 2^-23, which is off by 2^-23 itself, and the difference by 2^-24: 5 * 2^-24 in all, of the cap)
   which changes numerator and total by as much relatively each; their sums over runs, lanes, waves and parts by (n / 16 + 64) 2^-24 each;
   weights and output are rounded to bf16 where the activations are (2^-8 each, of A and of the result)."""
 import math
@@ -74,7 +76,8 @@ def check_rows(out, lse, q, k, v, scale, dtype, place, first, end, window, score
     ref, ref_lse, logits, p = D.masked_attention(q, k, v, scale, place, first, end, window, **scores.of(head))
     n = len(k)
     qk = (np.abs(q) @ np.abs(k).T).max(axis=1, initial=0.0) if n else np.zeros(len(q))
-    off = 2 ** -24 * ((q.shape[1] + 8) * scale * qk + 16 * np.abs(logits).max(axis=1, initial=0.0) + 4 * scores.largest(head, n))
+    off = 2 ** -24 * ((q.shape[1] + 8) * scale * qk + 16 * np.abs(logits).max(axis=1, initial=0.0) + 4 * scores.largest(head, n)
+                    + (8 * scores.cap if dtype == "bf16" and scores.cap <= 64 else 0.0))
     sums = (n / 16 + 64) * 2 ** -24
     none = ref_lse == -np.inf
     assert (out[none] == 0).all() and (lse[none] == -np.inf).all(), f"{what}: rows without keys"
