@@ -35,6 +35,8 @@ struct Prompt {
     void* out;
     float* lse;
     int tokens, B, heads, group, dim, pages, page_bits, table_pages, window;
+    int parts;                              // stretches that an item's keys are cut into, each a block's
+    float *part_o, *part_ml;                // [parts][tokens * query heads][dim], [parts][tokens * query heads][2]: unscaled sums; their maximum and weight
     float scale;                            // times log2 e
     ScoreArgs scores;
 };
@@ -89,9 +91,9 @@ struct Shape {
 
 // The item a block works on: a sequence, some of its rows, and the keys they see.
 struct Item {
-    int b, rows;                            // rows: of the sequence, in all of its tokens
+    int b, rows;                            // the sequence; where the block's rows end
     int row0, token0, place0;               // the block's first row; the sequence's first token in q, and its place
-    int len;
+    int len, part;
 };
 
 // Tile `index` from the end of the list of all sequences' tiles of `rows` rows; false: there is none.  64 sequences at a time, the last first.
@@ -117,9 +119,10 @@ __device__ inline bool find(const Prompt& a, int index, int rows, Item& it) {
             const int at = __builtin_ctzll(found);
             it.b = b0 - at;
             const int tile = before + __shfl(upto, at) - 1 - index;                 // of the sequence
-            const int new_tokens = __shfl(n, at);
-            it.rows = uniform(new_tokens * a.group);
-            it.row0 = uniform(tile * rows);
+            const int new_tokens = __shfl(n, at), all = new_tokens * a.group, of = (all + rows - 1) / rows;
+            const int each = ((all + of - 1) / of + 31) & ~31;                      // as many in each of the sequence's tiles, in whole waves
+            it.row0 = uniform(min(tile * each, all));
+            it.rows = uniform(min(tile * each + each, all));
             it.token0 = uniform(__shfl(s, at));
             it.b = uniform(it.b);
             it.len = uniform(min(max(a.lens[it.b], 0), a.table_pages << a.page_bits));
@@ -623,7 +626,7 @@ struct Block {
     // The block's rows, the keys they see, and the wave's queries.
     __device__ void begin() {
         const int tokens = (it.rows + a.group - 1) / a.group;
-        const int from_token = it.row0 / a.group, to_token = min((it.row0 + H::kRows - 1) / a.group, tokens - 1);
+        const int from_token = it.row0 / a.group, to_token = tokens - 1;
         int low = 0x7fffffff, high = 0, last_low = 0, first_high = 0x7fffffff;
         for (int i = from_token + lane; i <= to_token; i += 64) {
             int x, y;
@@ -637,6 +640,12 @@ struct Block {
         }
         first = wave_min(low);
         end = wave_max(high);
+        if (a.parts > 1 && first < end) {                                           // a part of the keys' tiles
+            const int base = first & ~(H::kKeys - 1), tiles = (end - base + H::kKeys - 1) / H::kKeys;
+            const int from = static_cast<int>(static_cast<long>(tiles) * it.part / a.parts), to = static_cast<int>(static_cast<long>(tiles) * (it.part + 1) / a.parts);
+            first = max(first, base + from * H::kKeys);
+            end = min(end, base + to * H::kKeys);
+        }
         all_from = wave_max(last_low);
         all_to = wave_min(first_high);
         const int row = it.row0 + wave_rows + lane % 32;
@@ -677,15 +686,21 @@ struct Block {
         if (row >= it.rows) return;
         const int token = row / a.group;
         const long at = static_cast<long>(it.token0 + token) * a.heads * a.group + head * a.group + (row - token * a.group);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        if (h == 0 && wave_column == 0 && a.lse != nullptr) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        const bool part = a.parts > 1;
+        const float inv = part ? 1.f : l == 0.f ? 0.f : 1.f / l;
+        float* const part_o = a.part_o + (static_cast<long>(it.part) * a.tokens * a.heads * a.group + at) * a.dim;
+        if (h == 0 && wave_column == 0) {
+            if (part) *reinterpret_cast<f32x2*>(a.part_ml + (static_cast<long>(it.part) * a.tokens * a.heads * a.group + at) * 2) = f32x2{m, l};
+            else if (a.lse != nullptr) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        }
+        if (part && first >= end) return;                                           // (a part without keys: its maximum says so)
         if constexpr (F32) {
 #pragma unroll
             for (int g = 0; g < H::kColumns / kNear; ++g)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int d = 128 * g + kNear * (8 * (i / 4) + 4 * h + i % 4);
-                    float* to = static_cast<float*>(a.out) + at * a.dim + d;
+                    float* to = part ? part_o + d : static_cast<float*>(a.out) + at * a.dim + d;
                     if (d >= a.dim) continue;
                     if constexpr (kNear == 4) *reinterpret_cast<f32x4*>(to) = f32x4{o[4 * g][i], o[4 * g + 1][i], o[4 * g + 2][i], o[4 * g + 3][i]} * inv;
                     else *reinterpret_cast<f32x2*>(to) = f32x2{o[0][i] * inv, o[1][i] * inv};
@@ -697,7 +712,8 @@ struct Block {
                 for (int i = 0; i < 16; i += 4) {
                     const int d = 32 * (wave_column + c) + 8 * (i / 4) + 4 * h;
                     if (d >= a.dim) continue;
-                    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at * a.dim + d) =
+                    if (part) *reinterpret_cast<f32x4*>(part_o + d) = f32x4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]};
+                    else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at * a.dim + d) =
                         u32x2{to_bf16x2(o[c][i] * inv, o[c][i + 1] * inv), to_bf16x2(o[c][i + 2] * inv, o[c][i + 3] * inv)};
                 }
         }
@@ -806,7 +822,9 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(F32)) void prompt_kernel(Promp
     __shared__ typename B::Lds lds;
     Item it;
     // the key heads first: blocks that read the same keys are a multiple of the heads apart, with eight of them on one XCD
-    if (!find(a, blockIdx.x / a.heads, B::H::kRows, it)) return;
+    const int index = blockIdx.x / a.heads;
+    it.part = index % a.parts;
+    if (!find(a, index / a.parts, B::H::kRows, it) || it.row0 >= it.rows) return;
     B block{a, lds, it};
     block.head = blockIdx.x % a.heads;
     block.lane = threadIdx.x % 64;
@@ -816,38 +834,101 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(F32)) void prompt_kernel(Promp
     block.run();
 }
 
+// Joins an item's parts: the row of a token and query head by DIM / 4 neighbouring threads, in the order of the keys.
+template <bool F32, int DIM>
+__global__ __launch_bounds__(256) void prompt_join_kernel(Prompt a) {
+    const long rows = static_cast<long>(a.tokens) * a.heads * a.group, row = static_cast<long>(blockIdx.x) * (1024 / DIM) + threadIdx.x / (DIM / 4);
+    const int d = 4 * (threadIdx.x % (DIM / 4));
+    if (row >= rows || d >= a.dim) return;
+    const int token = static_cast<int>(row / (a.heads * a.group));
+    if (token < a.starts[0] || token >= a.starts[a.B]) return;
+    float top = -INFINITY, weight = 0.f;
+    for (int i = 0; i < a.parts; ++i) top = fmaxf(top, a.part_ml[(i * rows + row) * 2]);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < a.parts; ++i) {
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + (i * rows + row) * 2);
+        if (ml[0] == -INFINITY) continue;                                           // nothing counts there, and nothing may have been written
+        const float f = __builtin_amdgcn_exp2f(ml[0] - top);
+        const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + (i * rows + row) * a.dim + d);
+        weight = fmaf(ml[1], f, weight);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = fmaf(o[c], f, v[c]);
+    }
+    const float inv = weight == 0.f ? 0.f : 1.f / weight;
+    if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + row * a.dim + d) = v * inv;
+    else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + row * a.dim + d) = u32x2{to_bf16x2(v[0] * inv, v[1] * inv), to_bf16x2(v[2] * inv, v[3] * inv)};
+    if (d == 0 && a.lse != nullptr) a.lse[row] = (top + __builtin_amdgcn_logf(weight)) * 0.6931471805599453f;
+}
+
+// How a call is cut.
+struct Plan {
+    int dim, waves, rows;           // the kernel's columns, a block's waves and rows
+    long tiles;                     // of rows, at most (a sequence's last may not be full)
+    int parts;
+};
+constexpr int kUnits = 256;         // compute units, also of the plan that sizes the workspace
+Plan plan_of(const moe_kv_cfg& kv, const moe_prompt_cfg& c) {
+    Plan p;
+    const bool f32 = kv.dtype == MOE_F32;
+    const int group = c.q_heads / kv.heads, sequences = std::max(1, std::min(c.B, c.tokens));
+    const long rows = static_cast<long>(c.tokens) * group, each = (rows + sequences - 1) / sequences;      // of a key head; of a sequence, in the mean
+    p.dim = kv.head_dim <= 64 ? 64 : kv.head_dim <= 128 ? 128 : 256;
+    p.waves = f32 ? 4 : p.dim > 128 ? 8 : rows * kv.heads >= 256 * 256L ? 8 : 4;
+    p.rows = p.waves == 8 && p.dim <= 128 ? 256 : 128;
+    p.tiles = rows / p.rows + sequences;
+    // Few items: their keys are cut, down to 256 of them.
+    const long items = p.tiles * kv.heads, slots = (p.waves == 4 && !f32 ? 2 : 1) * kUnits;
+    const long room = static_cast<long>(c.table_pages) * kv.page_size, keys = c.window > 0 ? std::min(room, c.window + each / group + 64) : room;
+    p.parts = static_cast<int>(std::max(1L, std::min({slots / std::max(items, 1L), keys / 256, 16L})));
+    return p;
+}
+// The workspace: the parts' sums, their maxima and weights.
+struct Parts {
+    size_t ml, bytes;
+    Parts(const moe_kv_cfg& kv, const moe_prompt_cfg& c) {
+        const int parts = plan_of(kv, c).parts;
+        const size_t rows = parts == 1 ? 0 : static_cast<size_t>(parts) * c.tokens * c.q_heads;
+        ml = align256(rows * kv.head_dim * 4);
+        bytes = std::max(ml + align256(rows * 8), size_t(256));
+    }
+};
+
 template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
-int launch(const Prompt& a, hipStream_t s) {
-    const long tiles = static_cast<long>(a.tokens) * a.group / Shape<F32, CACHE, DIM, WAVES>::kRows + std::min(a.B, a.tokens);       // (a sequence's last tile may not be full)
-    hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED>), dim3(static_cast<unsigned>(tiles * a.heads)), dim3(64 * WAVES), 0, s, a);
+int launch(const Prompt& a, const Plan& p, hipStream_t s) {
+    static_assert(Shape<F32, CACHE, DIM, WAVES>::kRows == (WAVES == 8 && DIM <= 128 ? 256 : 128), "as plan_of says");
+    hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED>), dim3(static_cast<unsigned>(p.tiles * a.heads * a.parts)), dim3(64 * WAVES), 0, s, a);
     MOE_LAUNCH_CHECK("prompt_kernel");
+    if (a.parts > 1) {
+        const long rows = static_cast<long>(a.tokens) * a.heads * a.group, each = 1024 / DIM;
+        hipLaunchKernelGGL((prompt_join_kernel<F32, DIM>), dim3(static_cast<unsigned>((rows + each - 1) / each)), dim3(256), 0, s, a);
+        MOE_LAUNCH_CHECK("prompt_join_kernel");
+    }
     return MOE_OK;
 }
 
 template <bool F32, int CACHE, int DIM, bool SCORED>
-int for_waves(const Prompt& a, hipStream_t s) {
-    if constexpr (!F32 && DIM > 128) return launch<F32, CACHE, DIM, 8, SCORED>(a, s);
-    else if constexpr (!F32)
-        if (static_cast<long>(a.tokens) * a.group * a.heads >= 256 * 256L) return launch<F32, CACHE, DIM, 8, SCORED>(a, s);
-    return launch<F32, CACHE, DIM, 4, SCORED>(a, s);
+int for_waves(const Prompt& a, const Plan& p, hipStream_t s) {
+    if constexpr (!F32 && DIM > 128) return launch<F32, CACHE, DIM, 8, SCORED>(a, p, s);
+    else if constexpr (F32) return launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
+    else return p.waves == 8 ? launch<F32, CACHE, DIM, 8, SCORED>(a, p, s) : launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
 }
 
 template <bool F32, int CACHE, bool SCORED>
-int for_sizes(const Prompt& a, hipStream_t s) {
-    if (a.dim <= 64) return for_waves<F32, CACHE, 64, SCORED>(a, s);
-    return a.dim <= 128 ? for_waves<F32, CACHE, 128, SCORED>(a, s) : for_waves<F32, CACHE, 256, SCORED>(a, s);
+int for_sizes(const Prompt& a, const Plan& p, hipStream_t s) {
+    if (p.dim == 64) return for_waves<F32, CACHE, 64, SCORED>(a, p, s);
+    return p.dim == 128 ? for_waves<F32, CACHE, 128, SCORED>(a, p, s) : for_waves<F32, CACHE, 256, SCORED>(a, p, s);
 }
 
 template <bool SCORED>
-int for_types(const moe_kv_cfg& kv, const Prompt& a, hipStream_t s) {
-    if (kv.dtype == MOE_BF16) return kv.cache_dtype == MOE_BF16 ? for_sizes<false, MOE_BF16, SCORED>(a, s) : for_sizes<false, MOE_E4M3, SCORED>(a, s);
-    if (kv.cache_dtype == MOE_F32) return for_sizes<true, MOE_F32, SCORED>(a, s);
-    return kv.cache_dtype == MOE_BF16 ? for_sizes<true, MOE_BF16, SCORED>(a, s) : for_sizes<true, MOE_E4M3, SCORED>(a, s);
+int for_types(const moe_kv_cfg& kv, const Prompt& a, const Plan& p, hipStream_t s) {
+    if (kv.dtype == MOE_BF16) return kv.cache_dtype == MOE_BF16 ? for_sizes<false, MOE_BF16, SCORED>(a, p, s) : for_sizes<false, MOE_E4M3, SCORED>(a, p, s);
+    if (kv.cache_dtype == MOE_F32) return for_sizes<true, MOE_F32, SCORED>(a, p, s);
+    return kv.cache_dtype == MOE_BF16 ? for_sizes<true, MOE_BF16, SCORED>(a, p, s) : for_sizes<true, MOE_E4M3, SCORED>(a, p, s);
 }
 
 }  // namespace
 
-size_t attn_prompt_workspace_bytes(const moe_kv_cfg& kv, const moe_prompt_cfg& c) { return 256; }
+size_t attn_prompt_workspace_bytes(const moe_kv_cfg& kv, const moe_prompt_cfg& c) { return Parts(kv, c).bytes; }
 
 int launch_attn_prompt(const moe_kv_cfg& kv, const moe_prompt_cfg& c, const Scores& scores, const void* q, long q_stride, const void* k_pages,
                        const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* table, const int32_t* lens,
@@ -877,7 +958,12 @@ int launch_attn_prompt(const moe_kv_cfg& kv, const moe_prompt_cfg& c, const Scor
     a.window = c.window;
     a.scale = (c.scale > 0.f ? c.scale : 1.f / sqrtf(static_cast<float>(kv.head_dim))) * kLog2E;
     a.scores = ScoreArgs(scores, kv.dtype);
-    return scores.any() ? for_types<true>(kv, a, s) : for_types<false>(kv, a, s);
+    const Plan p = plan_of(kv, c);
+    const Parts parts(kv, c);
+    a.parts = p.parts;
+    a.part_o = static_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + parts.ml);
+    return scores.any() ? for_types<true>(kv, a, p, s) : for_types<false>(kv, a, p, s);
 }
 
 }  // namespace moe
