@@ -15,8 +15,9 @@ LIB = os.path.join(HERE, "libmoe355.so")
 ARGS = os.path.join(HERE, "_args.so")
 SOURCES = ["api.hip", "route.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "combine.hip", "schedule.hip",
            "api_decoder.hip", "norm.hip", "kv.hip", "attn.hip", "rope.hip", "prompt.hip"]
-# ffn.hip is compiled in parts, side by side: each of its large kernels is an object of its own.  So are attn.hip's kernels with and without scores of their own.
-PARTS = {"ffn.hip": 5, "attn.hip": 2}
+# ffn.hip is compiled in parts, side by side: each of its large kernels is an object of its own.  So are attn.hip's and prompt.hip's kernels with and
+# without scores of their own, prompt.hip's by type too.
+PARTS = {"ffn.hip": 5, "attn.hip": 2, "prompt.hip": 4}
 UNITS = [(src, part) for src in SOURCES for part in range(PARTS.get(src, 1))]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

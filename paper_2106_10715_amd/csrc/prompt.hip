@@ -19,12 +19,9 @@
 #include "scores.h"
 
 namespace moe {
-namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-
-constexpr float kSlack = 8.f;               // the running maximum is raised only where a logit passes it by more than this (as a power of two)
+// What the objects that this file is compiled to share (PROMPT_PART: 0 and 1 16-bit activations without and with scores of their own, 2 and 3 fp32).
+namespace prompt {
 
 struct Prompt {
     const void* q;
@@ -40,6 +37,30 @@ struct Prompt {
     float scale;                            // times log2 e
     ScoreArgs scores;
 };
+
+// How a call is cut.
+struct Plan {
+    int dim, waves, rows;                   // the kernel's columns, a block's waves and rows
+    long tiles;                             // of rows, at most (a sequence's last may not be full)
+    int parts;
+};
+
+int launch_bf16(const Prompt& a, const Plan& p, int cache, hipStream_t s);
+int launch_bf16_scored(const Prompt& a, const Plan& p, int cache, hipStream_t s);
+int launch_f32(const Prompt& a, const Plan& p, int cache, hipStream_t s);
+int launch_f32_scored(const Prompt& a, const Plan& p, int cache, hipStream_t s);
+
+}  // namespace prompt
+
+namespace {
+
+using prompt::Plan;
+using prompt::Prompt;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kSlack = 8.f;               // the running maximum is raised only where a logit passes it by more than this (as a power of two)
 
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ inline int wave_min(int v) {
@@ -143,7 +164,8 @@ __device__ inline void stretch_of(const Prompt& a, const Item& it, int token, in
     hi = max(hi, lo);
 }
 
-template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
+// SCORED: scores may be capped or get a bias by distance.  PARTS: an item's keys may be cut, and the sums are left for the join.
+template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED, bool PARTS>
 struct Block {
     using H = Shape<F32, CACHE, DIM, WAVES>;
     static constexpr bool kScaled = CACHE == MOE_E4M3 && !F32;                      // keys and values have scales, which their products do not
@@ -640,7 +662,7 @@ struct Block {
         }
         first = wave_min(low);
         end = wave_max(high);
-        if (a.parts > 1 && first < end) {                                           // a part of the keys' tiles
+        if (PARTS && first < end) {                                           // a part of the keys' tiles
             const int base = first & ~(H::kKeys - 1), tiles = (end - base + H::kKeys - 1) / H::kKeys;
             const int from = static_cast<int>(static_cast<long>(tiles) * it.part / a.parts), to = static_cast<int>(static_cast<long>(tiles) * (it.part + 1) / a.parts);
             first = max(first, base + from * H::kKeys);
@@ -686,7 +708,7 @@ struct Block {
         if (row >= it.rows) return;
         const int token = row / a.group;
         const long at = static_cast<long>(it.token0 + token) * a.heads * a.group + head * a.group + (row - token * a.group);
-        const bool part = a.parts > 1;
+        constexpr bool part = PARTS;
         const float inv = part ? 1.f : l == 0.f ? 0.f : 1.f / l;
         float* const part_o = a.part_o + (static_cast<long>(it.part) * a.tokens * a.heads * a.group + at) * a.dim;
         if (h == 0 && wave_column == 0) {
@@ -816,15 +838,15 @@ struct Block {
 // Waves that a SIMD has room for: with two, a wave has 256 registers.
 constexpr int waves_of(bool f32) { return f32 ? 1 : 2; }
 
-template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
+template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED, bool PARTS>
 __global__ __launch_bounds__(64 * WAVES, waves_of(F32)) void prompt_kernel(Prompt a) {
-    using B = Block<F32, CACHE, DIM, WAVES, SCORED>;
+    using B = Block<F32, CACHE, DIM, WAVES, SCORED, PARTS>;
     __shared__ typename B::Lds lds;
     Item it;
     // the key heads first: blocks that read the same keys are a multiple of the heads apart, with eight of them on one XCD
     const int index = blockIdx.x / a.heads;
-    it.part = index % a.parts;
-    if (!find(a, index / a.parts, B::H::kRows, it) || it.row0 >= it.rows) return;
+    it.part = PARTS ? index % a.parts : 0;
+    if (!find(a, PARTS ? index / a.parts : index, B::H::kRows, it) || it.row0 >= it.rows) return;
     B block{a, lds, it};
     block.head = blockIdx.x % a.heads;
     block.lane = threadIdx.x % 64;
@@ -860,12 +882,63 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(Prompt a) {
     if (d == 0 && a.lse != nullptr) a.lse[row] = (top + __builtin_amdgcn_logf(weight)) * 0.6931471805599453f;
 }
 
-// How a call is cut.
-struct Plan {
-    int dim, waves, rows;           // the kernel's columns, a block's waves and rows
-    long tiles;                     // of rows, at most (a sequence's last may not be full)
-    int parts;
-};
+template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
+int launch(const Prompt& a, const Plan& p, hipStream_t s) {
+    static_assert(Shape<F32, CACHE, DIM, WAVES>::kRows == (WAVES == 8 && DIM <= 128 ? 256 : 128), "as plan_of says");
+    const dim3 blocks(static_cast<unsigned>(p.tiles * a.heads * a.parts));
+    if (a.parts == 1) hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED, false>), blocks, dim3(64 * WAVES), 0, s, a);
+    else hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED, true>), blocks, dim3(64 * WAVES), 0, s, a);
+    MOE_LAUNCH_CHECK("prompt_kernel");
+    if (a.parts > 1) {
+        const long rows = static_cast<long>(a.tokens) * a.heads * a.group, each = 1024 / DIM;
+        hipLaunchKernelGGL((prompt_join_kernel<F32, DIM>), dim3(static_cast<unsigned>((rows + each - 1) / each)), dim3(256), 0, s, a);
+        MOE_LAUNCH_CHECK("prompt_join_kernel");
+    }
+    return MOE_OK;
+}
+
+template <bool F32, int CACHE, int DIM, bool SCORED>
+int for_waves(const Prompt& a, const Plan& p, hipStream_t s) {
+    if constexpr (!F32 && DIM > 128) return launch<F32, CACHE, DIM, 8, SCORED>(a, p, s);
+    else if constexpr (F32) return launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
+    else return p.waves == 8 ? launch<F32, CACHE, DIM, 8, SCORED>(a, p, s) : launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
+}
+
+template <bool F32, int CACHE, bool SCORED>
+int for_sizes(const Prompt& a, const Plan& p, hipStream_t s) {
+    if (p.dim == 64) return for_waves<F32, CACHE, 64, SCORED>(a, p, s);
+    return p.dim == 128 ? for_waves<F32, CACHE, 128, SCORED>(a, p, s) : for_waves<F32, CACHE, 256, SCORED>(a, p, s);
+}
+
+}  // namespace
+
+namespace prompt {
+
+#if PROMPT_PART == 0
+int launch_bf16(const Prompt& a, const Plan& p, int cache, hipStream_t s) {
+    return cache == MOE_BF16 ? for_sizes<false, MOE_BF16, false>(a, p, s) : for_sizes<false, MOE_E4M3, false>(a, p, s);
+}
+#elif PROMPT_PART == 1
+int launch_bf16_scored(const Prompt& a, const Plan& p, int cache, hipStream_t s) {
+    return cache == MOE_BF16 ? for_sizes<false, MOE_BF16, true>(a, p, s) : for_sizes<false, MOE_E4M3, true>(a, p, s);
+}
+#elif PROMPT_PART == 2
+int launch_f32(const Prompt& a, const Plan& p, int cache, hipStream_t s) {
+    if (cache == MOE_F32) return for_sizes<true, MOE_F32, false>(a, p, s);
+    return cache == MOE_BF16 ? for_sizes<true, MOE_BF16, false>(a, p, s) : for_sizes<true, MOE_E4M3, false>(a, p, s);
+}
+#else
+int launch_f32_scored(const Prompt& a, const Plan& p, int cache, hipStream_t s) {
+    if (cache == MOE_F32) return for_sizes<true, MOE_F32, true>(a, p, s);
+    return cache == MOE_BF16 ? for_sizes<true, MOE_BF16, true>(a, p, s) : for_sizes<true, MOE_E4M3, true>(a, p, s);
+}
+#endif
+
+}  // namespace prompt
+
+#if PROMPT_PART == 0
+namespace {
+
 constexpr int kUnits = 256;         // compute units, also of the plan that sizes the workspace
 Plan plan_of(const moe_kv_cfg& kv, const moe_prompt_cfg& c) {
     Plan p;
@@ -892,39 +965,6 @@ struct Parts {
         bytes = std::max(ml + align256(rows * 8), size_t(256));
     }
 };
-
-template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
-int launch(const Prompt& a, const Plan& p, hipStream_t s) {
-    static_assert(Shape<F32, CACHE, DIM, WAVES>::kRows == (WAVES == 8 && DIM <= 128 ? 256 : 128), "as plan_of says");
-    hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED>), dim3(static_cast<unsigned>(p.tiles * a.heads * a.parts)), dim3(64 * WAVES), 0, s, a);
-    MOE_LAUNCH_CHECK("prompt_kernel");
-    if (a.parts > 1) {
-        const long rows = static_cast<long>(a.tokens) * a.heads * a.group, each = 1024 / DIM;
-        hipLaunchKernelGGL((prompt_join_kernel<F32, DIM>), dim3(static_cast<unsigned>((rows + each - 1) / each)), dim3(256), 0, s, a);
-        MOE_LAUNCH_CHECK("prompt_join_kernel");
-    }
-    return MOE_OK;
-}
-
-template <bool F32, int CACHE, int DIM, bool SCORED>
-int for_waves(const Prompt& a, const Plan& p, hipStream_t s) {
-    if constexpr (!F32 && DIM > 128) return launch<F32, CACHE, DIM, 8, SCORED>(a, p, s);
-    else if constexpr (F32) return launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
-    else return p.waves == 8 ? launch<F32, CACHE, DIM, 8, SCORED>(a, p, s) : launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
-}
-
-template <bool F32, int CACHE, bool SCORED>
-int for_sizes(const Prompt& a, const Plan& p, hipStream_t s) {
-    if (p.dim == 64) return for_waves<F32, CACHE, 64, SCORED>(a, p, s);
-    return p.dim == 128 ? for_waves<F32, CACHE, 128, SCORED>(a, p, s) : for_waves<F32, CACHE, 256, SCORED>(a, p, s);
-}
-
-template <bool SCORED>
-int for_types(const moe_kv_cfg& kv, const Prompt& a, const Plan& p, hipStream_t s) {
-    if (kv.dtype == MOE_BF16) return kv.cache_dtype == MOE_BF16 ? for_sizes<false, MOE_BF16, SCORED>(a, p, s) : for_sizes<false, MOE_E4M3, SCORED>(a, p, s);
-    if (kv.cache_dtype == MOE_F32) return for_sizes<true, MOE_F32, SCORED>(a, p, s);
-    return kv.cache_dtype == MOE_BF16 ? for_sizes<true, MOE_BF16, SCORED>(a, p, s) : for_sizes<true, MOE_E4M3, SCORED>(a, p, s);
-}
 
 }  // namespace
 
@@ -963,7 +1003,9 @@ int launch_attn_prompt(const moe_kv_cfg& kv, const moe_prompt_cfg& c, const Scor
     a.parts = p.parts;
     a.part_o = static_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + parts.ml);
-    return scores.any() ? for_types<true>(kv, a, p, s) : for_types<false>(kv, a, p, s);
+    if (kv.dtype == MOE_BF16) return scores.any() ? prompt::launch_bf16_scored(a, p, kv.cache_dtype, s) : prompt::launch_bf16(a, p, kv.cache_dtype, s);
+    return scores.any() ? prompt::launch_f32_scored(a, p, kv.cache_dtype, s) : prompt::launch_f32(a, p, kv.cache_dtype, s);
 }
+#endif
 
 }  // namespace moe
