@@ -169,6 +169,7 @@ template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED, bool PARTS>
 struct Block {
     using H = Shape<F32, CACHE, DIM, WAVES>;
     static constexpr bool kScaled = CACHE == MOE_E4M3 && !F32;                      // keys and values have scales, which their products do not
+    static constexpr bool kRowScales = CACHE == MOE_E4M3 && F32;                    // their rows are multiplied with them
     struct Lds {
         __attribute__((aligned(256))) char k[H::kDeep][H::kTile], v[H::kDeep][H::kTile];
         float ks[H::kDeep][H::kKeys], vs[H::kDeep][H::kKeys];                                    // kScaled: scales of the keys, times a.scale, and of the values, a tile ahead of them
@@ -233,27 +234,36 @@ struct Block {
     // Where the rows of the wave's loads begin, looked up for kAsked tiles at once: lane kSlots s + j has load j of the s-th of them.
     static constexpr int kSlots = H::kLoads <= 1 ? 1 : H::kLoads <= 2 ? 2 : H::kLoads <= 4 ? 4 : 8, kAsked = 64 / kSlots;
     int ids, own_id;                                                                // the pages of the next kAsked tiles; kScaled, the first wave: of key `lane` of the next tile
-    uint32_t held[2];                                                               // rows of the present ones
+    uint32_t held[2], held4[kRowScales ? 2 : 1];                                    // where the rows of the present ones lie, in bytes; and their scales
     struct Rows {
-        long at[H::kLoads];
+        uint32_t lo[H::kLoads], hi[H::kLoads], lo4[kRowScales ? H::kLoads : 1], hi4[kRowScales ? H::kLoads : 1];
     };
+    __device__ static uint64_t both(uint32_t lo, uint32_t hi) { return static_cast<uint64_t>(hi) << 32 | lo; }
     __device__ long row_of(int id, int t) const {
         return ((static_cast<long>(min(max(id, 0), a.pages - 1)) * a.heads + head) << a.page_bits) + (t & ((1 << a.page_bits) - 1));
     }
     __device__ int page_of(int t) const { return a.table[static_cast<long>(it.b) * a.table_pages + (min(t, end - 1) >> a.page_bits)]; }
     __device__ int asked(int t0) const { return t0 + lane / kSlots * H::kKeys + (lane % kSlots * H::kThreads + 64 * wave) / H::kFrom; }
-    __device__ void locate(int t0, int index, Rows& r) {                            // index: of the tile, from the first
+    __device__ void locate(int t0, uint32_t index, Rows& r) {                       // index: of the tile, from the first
         if (index % kAsked == 0) {
-            const long row = row_of(ids, asked(t0));
-            held[0] = static_cast<uint32_t>(row);
-            held[1] = static_cast<uint32_t>(row >> 32);
+            const long row = row_of(ids, asked(t0)), bytes = row * (a.dim * H::kCached);
+            held[0] = static_cast<uint32_t>(bytes);
+            held[1] = static_cast<uint32_t>(bytes >> 32);
+            if constexpr (kRowScales) {
+                held4[0] = static_cast<uint32_t>(4 * row);
+                held4[1] = static_cast<uint32_t>(4 * row >> 32);
+            }
             ids = page_of(asked(t0 + kAsked * H::kKeys));
         }
 #pragma unroll
         for (int j = 0; j < H::kLoads; ++j) {
             const int from_lane = (index % kAsked) * kSlots + j;
-            r.at[j] = static_cast<long>(static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(held[1], from_lane))) << 32 |
-                                        static_cast<uint32_t>(__builtin_amdgcn_readlane(held[0], from_lane)));
+            r.lo[j] = __builtin_amdgcn_readlane(held[0], from_lane);
+            r.hi[j] = __builtin_amdgcn_readlane(held[1], from_lane);
+            if constexpr (kRowScales) {
+                r.lo4[j] = __builtin_amdgcn_readlane(held4[0], from_lane);
+                r.hi4[j] = __builtin_amdgcn_readlane(held4[1], from_lane);
+            }
         }
     }
     // Requests keys [t0, t0 + kKeys) of one side; zeros outside of [first, end), which a WHOLE tile does not reach.
@@ -265,11 +275,13 @@ struct Block {
             if (idle()) break;
             const int t = t0 + (j * H::kThreads + 64 * wave) / H::kFrom + lane / H::kFrom;
             const bool there = WHOLE || (t >= first && t < end);
-            const auto rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pages) + r.at[j] * row_bytes, 0, 16 * row_bytes, 0x00027000);
+            const auto rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pages) + both(r.lo[j], r.hi[j]), 0, 16 * row_bytes, 0x00027000);
             raw[j] = __builtin_amdgcn_raw_buffer_load_b128(rows, there ? from : 0x7fffff00, 0, 0);
-            if constexpr (CACHE == MOE_E4M3 && F32)
-                scale[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(scales) + r.at[j], 0, 64, 0x00027000),
+            if constexpr (kRowScales) {
+                const auto from4 = reinterpret_cast<const char*>(scales) + both(r.lo4[j], r.hi4[j]);
+                scale[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from4), 0, 64, 0x00027000),
                                                                                 there ? 4 * (lane / H::kFrom) : 0x7fffff00, 0, 0));
+            }
         }
     }
     template <bool WHOLE>
@@ -505,7 +517,7 @@ struct Block {
                 for (int i = 0; i < 16; ++i) o[c][i] *= keep;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        float sum[4];
 #pragma unroll
         for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
@@ -514,7 +526,7 @@ struct Block {
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     p[c] = __builtin_amdgcn_exp2f(fmaf(s[kb][i + c], mult, shift - ref));
-                    sum[c] += p[c];
+                    sum[c] = kb == 0 && i == 0 ? p[c] : sum[c] + p[c];
                 }
                 if constexpr (kScaled) {                                            // (a scale that is not finite may be that of a key the row does not see)
                     const f32x4 each = *reinterpret_cast<const f32x4*>(&lds.vs[buf][key_of(kb, i) + 4 * h]);
@@ -525,6 +537,8 @@ struct Block {
                 for (int c = 0; c < 4; c += H::kPerWord) w.set(kb, i + c, p[c], p[c + H::kPerWord - 1]);
             }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        asm volatile("" : "+v"(l));
+        w.hold();
     }
     // The order of the products of a tile: reads from LDS some of them ahead.
     template <bool NEXT, bool THIS>
@@ -765,7 +779,8 @@ struct Block {
             if constexpr (H::kTurns) load<false>(a.v_pages, a.v_scales, rows, base, v_raw, v_scale);
             lds_barrier();
             store_k(0);
-            int next = base, index = 0, to = 0;                                     // the tile whose K is on its way, its number and buffer; the V on its way is that before it
+            int next = base, to = 0;
+            uint32_t index = 0;                                                     // the tile whose K is on its way, its number and buffer; the V on its way is that before it
             auto ask = [&](auto plain, bool v) {
                 constexpr bool kPlain = decltype(plain)::value;
                 if (kPlain || (v && next < end)) load<kPlain>(a.v_pages, a.v_scales, rows, next, v_raw, v_scale);
@@ -809,7 +824,6 @@ struct Block {
                 Weights w;
                 if (now) weigh<kPlain>(s, w, buf, t0);
                 else w.clear();
-                w.hold();
                 if (late) lds_barrier();
                 __builtin_amdgcn_sched_barrier(0);
                 const int then = after(buf);
