@@ -900,10 +900,12 @@ template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
 int launch(const Prompt& a, const Plan& p, hipStream_t s) {
     static_assert(Shape<F32, CACHE, DIM, WAVES>::kRows == (WAVES == 8 && DIM <= 128 ? 256 : 128), "as plan_of says");
     const dim3 blocks(static_cast<unsigned>(p.tiles * a.heads * a.parts));
-    if (a.parts == 1) hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED, false>), blocks, dim3(64 * WAVES), 0, s, a);
-    else hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED, true>), blocks, dim3(64 * WAVES), 0, s, a);
-    MOE_LAUNCH_CHECK("prompt_kernel");
-    if (a.parts > 1) {
+    if (a.parts == 1) {
+        hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED, false>), blocks, dim3(64 * WAVES), 0, s, a);
+        MOE_LAUNCH_CHECK("prompt_kernel");
+    } else if constexpr (Shape<F32, CACHE, DIM, WAVES>::kRows == 128) {
+        hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED, true>), blocks, dim3(64 * WAVES), 0, s, a);
+        MOE_LAUNCH_CHECK("prompt_kernel");
         const long rows = static_cast<long>(a.tokens) * a.heads * a.group, each = 1024 / DIM;
         hipLaunchKernelGGL((prompt_join_kernel<F32, DIM>), dim3(static_cast<unsigned>((rows + each - 1) / each)), dim3(256), 0, s, a);
         MOE_LAUNCH_CHECK("prompt_join_kernel");
@@ -915,7 +917,8 @@ template <bool F32, int CACHE, int DIM, bool SCORED>
 int for_waves(const Prompt& a, const Plan& p, hipStream_t s) {
     if constexpr (!F32 && DIM > 128) return launch<F32, CACHE, DIM, 8, SCORED>(a, p, s);
     else if constexpr (F32) return launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
-    else return p.waves == 8 ? launch<F32, CACHE, DIM, 8, SCORED>(a, p, s) : launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
+    else if constexpr (DIM == 128 && !SCORED) return p.waves == 8 ? launch<F32, CACHE, DIM, 8, SCORED>(a, p, s) : launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
+    else return launch<F32, CACHE, DIM, 4, SCORED>(a, p, s);
 }
 
 template <bool F32, int CACHE, bool SCORED>
@@ -954,26 +957,39 @@ int launch_f32_scored(const Prompt& a, const Plan& p, int cache, hipStream_t s) 
 namespace {
 
 constexpr int kUnits = 256;         // compute units, also of the plan that sizes the workspace
-Plan plan_of(const moe_kv_cfg& kv, const moe_prompt_cfg& c) {
+// Blocks of four waves, two to a compute unit, or of eight that take turns, one to a unit: these read keys half as often, but all rows of a block wait for each other,
+// and where weights cost more than products nothing is gained by turns.  us with four / eight (ragged lengths where there are several):
+//   32 over 8 of 128, bf16:   1 x 2048 59.3 / 62.7, 4 x 2048 79.9 / 83.3, 40 x 500 90.4 / 102, but 1 x 4096 168.7 / 147.6, 8 x 4096 487 / 469, 1 x 8192 567 / 526;
+//                             with a cap 1 x 8192 778 / 800;  e4m3 cache: 64 x 500 (64 over 8) 307 / 348, but 1 x 16384 2457 / 2344
+//   64 heads of 64, bf16:     8 x 2048 176 / 208 (with a table of biases 246 / 278), 1 x 4096 177 / 188
+bool in_turns(const moe_kv_cfg& kv, const Plan& p, long rows, long each, bool scored) {
+    return kv.dtype == MOE_BF16 && p.dim == 128 && !scored && p.parts == 1 && each >= 8192 && rows * kv.heads >= 1 << 17;
+}
+Plan plan_of(const moe_kv_cfg& kv, const moe_prompt_cfg& c, bool scored) {
     Plan p;
     const bool f32 = kv.dtype == MOE_F32;
     const int group = c.q_heads / kv.heads, sequences = std::max(1, std::min(c.B, c.tokens));
     const long rows = static_cast<long>(c.tokens) * group, each = (rows + sequences - 1) / sequences;      // of a key head; of a sequence, in the mean
     p.dim = kv.head_dim <= 64 ? 64 : kv.head_dim <= 128 ? 128 : 256;
-    p.waves = f32 ? 4 : p.dim > 128 ? 8 : rows * kv.heads >= 256 * 256L ? 8 : 4;
-    p.rows = p.waves == 8 && p.dim <= 128 ? 256 : 128;
+    p.rows = 128;
     p.tiles = rows / p.rows + sequences;
     // Few items: their keys are cut, down to 256 of them.
-    const long items = p.tiles * kv.heads, slots = (p.waves == 4 && !f32 ? 2 : 1) * kUnits;
+    const long items = p.tiles * kv.heads, slots = (f32 || p.dim > 128 ? 1 : 2) * kUnits;
     const long room = static_cast<long>(c.table_pages) * kv.page_size, keys = c.window > 0 ? std::min(room, c.window + each / group + 64) : room;
     p.parts = static_cast<int>(std::max(1L, std::min({slots / std::max(items, 1L), keys / 256, 16L})));
+    p.waves = !f32 && p.dim > 128 ? 8 : 4;
+    if (in_turns(kv, p, rows, each, scored)) {
+        p.waves = 8;
+        p.rows = 256;
+        p.tiles = rows / p.rows + sequences;
+    }
     return p;
 }
 // The workspace: the parts' sums, their maxima and weights.
 struct Parts {
     size_t ml, bytes;
     Parts(const moe_kv_cfg& kv, const moe_prompt_cfg& c) {
-        const int parts = plan_of(kv, c).parts;
+        const int parts = plan_of(kv, c, false).parts;                              // (the same for all scores)
         const size_t rows = parts == 1 ? 0 : static_cast<size_t>(parts) * c.tokens * c.q_heads;
         ml = align256(rows * kv.head_dim * 4);
         bytes = std::max(ml + align256(rows * 8), size_t(256));
@@ -1012,7 +1028,7 @@ int launch_attn_prompt(const moe_kv_cfg& kv, const moe_prompt_cfg& c, const Scor
     a.window = c.window;
     a.scale = (c.scale > 0.f ? c.scale : 1.f / sqrtf(static_cast<float>(kv.head_dim))) * kLog2E;
     a.scores = ScoreArgs(scores, kv.dtype);
-    const Plan p = plan_of(kv, c);
+    const Plan p = plan_of(kv, c, scores.any());
     const Parts parts(kv, c);
     a.parts = p.parts;
     a.part_o = static_cast<float*>(ws);
