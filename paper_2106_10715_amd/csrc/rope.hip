@@ -28,91 +28,123 @@ struct Rope {
 template <bool BF16, int V>
 struct Piece {
     static constexpr int kBytes = V * (BF16 ? 2 : 4);
+    typedef uint32_t Words __attribute__((ext_vector_type(kBytes > 4 ? kBytes / 4 : 2)));
     uint32_t u[kBytes >= 4 ? kBytes / 4 : 1];
+    template <bool STREAM>
     __device__ void load(const void* p) {
-        if constexpr (kBytes == 16) { const u32x4 r = *static_cast<const u32x4*>(p); for (int c = 0; c < 4; ++c) u[c] = r[c]; }
-        else if constexpr (kBytes == 8) { const u32x2 r = *static_cast<const u32x2*>(p); u[0] = r[0]; u[1] = r[1]; }
-        else if constexpr (kBytes == 4) u[0] = *static_cast<const uint32_t*>(p);
-        else u[0] = *static_cast<const uint16_t*>(p);
+        if constexpr (kBytes > 4) {
+            const Words r = load_from<STREAM>(static_cast<const Words*>(p));
+#pragma unroll
+            for (int c = 0; c < kBytes / 4; ++c) u[c] = r[c];
+        } else if constexpr (kBytes == 4) {
+            u[0] = *static_cast<const uint32_t*>(p);
+        } else {
+            u[0] = *static_cast<const uint16_t*>(p);
+        }
     }
+    template <bool STREAM>
     __device__ void store(void* p) const {
-        if constexpr (kBytes == 16) *static_cast<u32x4*>(p) = u32x4{u[0], u[1], u[2], u[3]};
-        else if constexpr (kBytes == 8) *static_cast<u32x2*>(p) = u32x2{u[0], u[1]};
-        else if constexpr (kBytes == 4) *static_cast<uint32_t*>(p) = u[0];
-        else *static_cast<uint16_t*>(p) = static_cast<uint16_t>(u[0]);
+        if constexpr (kBytes > 4) {
+            Words r;
+#pragma unroll
+            for (int c = 0; c < kBytes / 4; ++c) r[c] = u[c];
+            store_to<STREAM>(static_cast<Words*>(p), r);
+        } else if constexpr (kBytes == 4) {
+            *static_cast<uint32_t*>(p) = u[0];
+        } else {
+            *static_cast<uint16_t*>(p) = static_cast<uint16_t>(u[0]);
+        }
     }
     __device__ float get(int i) const {
         if constexpr (!BF16) return __uint_as_float(u[i]);
         else return i % 2 == 0 ? bf16_lo(u[i / 2]) : bf16_hi(u[i / 2]);
     }
     __device__ void set(const float (&v)[V]) {
-        if constexpr (!BF16) for (int c = 0; c < V; ++c) u[c] = __float_as_uint(v[c]);
-        else if constexpr (V == 1) u[0] = to_bf16x2(v[0], 0.f);
-        else for (int c = 0; c < V / 2; ++c) u[c] = to_bf16x2(v[2 * c], v[2 * c + 1]);
+#pragma unroll
+        for (int c = 0; c < (BF16 ? (V + 1) / 2 : V); ++c) {
+            if constexpr (!BF16) u[c] = __float_as_uint(v[c]);
+            else if constexpr (V == 1) u[c] = to_bf16x2(v[0], 0.f);
+            else u[c] = to_bf16x2(v[2 * c], v[2 * c + 1]);
+        }
     }
 };
 
-// HALF: an item is V pairs, a piece of either half; else V / 2 pairs in one piece.  Items past the turned columns copy one piece.
-template <bool BF16, bool HALF, int V>
+// HALF: an item is V pairs, a piece of either half; else V / 2 pairs in one piece.  Items past the turned columns copy one piece.  A thread has the same
+// piece of every row it works on, and requests kBatch of them at once, the first before the sines are computed.  STREAM 1: non-temporal stores, 2: loads too.
+constexpr int kBatch = 4;
+template <bool BF16, bool HALF, int V, int STREAM>
 __global__ __launch_bounds__(kThreads) void rope_kernel(Rope a) {
     __shared__ float sines[kThreads], cosines[kThreads];
+    constexpr int kBytes = BF16 ? 2 : 4;
     const int tid = threadIdx.x, pairs = a.rot / 2, first = blockIdx.x * a.tokens, tokens = min(a.tokens, a.n - first);
+    const int rows = tokens * a.heads, per = kThreads / a.row_pieces, piece = tid % a.row_pieces, begin = tid < per * a.row_pieces ? tid / a.row_pieces : rows;
+    const bool turns = piece < a.pieces;
+    const int at = turns ? piece * V * kBytes : (a.rot + (piece - a.pieces) * V) * kBytes, half = pairs * kBytes;
+    Piece<BF16, V> x[kBatch], y[HALF ? kBatch : 1];
+    int token[kBatch];
+    char* out[kBatch];
+    auto ask = [&](int row0) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int row = row0 + i * per;
+            out[i] = nullptr;
+            if (row >= rows) continue;
+            token[i] = a.heads == 1 ? row : static_cast<int>(__umulhi(static_cast<uint32_t>(row), a.over_heads));
+            const int in_token = row - token[i] * a.heads;
+            const RopeSide& side = in_token < a.q.heads ? a.q : a.k;
+            const int head = in_token < a.q.heads ? in_token : in_token - a.q.heads;
+            const char* in = static_cast<const char*>(side.in) + ((first + token[i]) * side.in_stride + head * a.dim) * kBytes + at;
+            char* to = static_cast<char*>(side.out) + ((first + token[i]) * side.out_stride + head * a.dim) * kBytes + at;
+            if (!turns && in == to) continue;
+            out[i] = to;
+            x[i].template load<STREAM == 2>(in);
+            if constexpr (HALF)
+                if (turns) y[i].template load<STREAM == 2>(in + half);
+        }
+    };
+    ask(begin);
     if (tid < tokens * pairs) {
-        const int token = tid / pairs, pair = tid - token * pairs;
-        const double turns = static_cast<double>(a.positions[first + token]) * a.freqs[pair] * 0.15915494309189533577;
+        const int of = tid / pairs, pair = tid - of * pairs;
+        const double turn = static_cast<double>(a.positions[first + of]) * a.freqs[pair] * 0.15915494309189533577;
         float s, c;
-        sincospif(2.f * static_cast<float>(turns - rint(turns)), &s, &c);
+        sincospif(2.f * static_cast<float>(turn - rint(turn)), &s, &c);
         sines[tid] = s * a.amplitude;
         cosines[tid] = c * a.amplitude;
     }
     __syncthreads();
-    constexpr int kBytes = BF16 ? 2 : 4;
-    const int rows = tokens * a.heads, per = kThreads / a.row_pieces;
-    const int piece = tid % a.row_pieces;
-    if (tid >= per * a.row_pieces) return;
-    for (int row = tid / a.row_pieces; row < rows; row += per) {
-        const int token = a.heads == 1 ? row : static_cast<int>(__umulhi(static_cast<uint32_t>(row), a.over_heads)), in_token = row - token * a.heads;
-        const RopeSide& side = in_token < a.q.heads ? a.q : a.k;
-        const int head = in_token < a.q.heads ? in_token : in_token - a.q.heads;
-        const char* in = static_cast<const char*>(side.in) + ((first + token) * side.in_stride + head * a.dim) * kBytes;
-        char* out = static_cast<char*>(side.out) + ((first + token) * side.out_stride + head * a.dim) * kBytes;
-        if (piece >= a.pieces) {
-            if (in == out) continue;
-            const long at = static_cast<long>(a.rot + (piece - a.pieces) * V) * kBytes;
-            Piece<BF16, V> x;
-            x.load(in + at);
-            x.store(out + at);
-            continue;
-        }
-        if constexpr (HALF) {
-            const int p0 = piece * V;
-            Piece<BF16, V> x, y;
-            x.load(in + p0 * kBytes);
-            y.load(in + (pairs + p0) * kBytes);
-            float u[V], v[V];
+    for (int row0 = begin; row0 < rows; row0 += kBatch * per) {
+        if (row0 != begin) ask(row0);
 #pragma unroll
-            for (int c = 0; c < V; ++c) {
-                const float s = sines[token * pairs + p0 + c], k = cosines[token * pairs + p0 + c], l = x.get(c), r = y.get(c);
-                u[c] = l * k - r * s;
-                v[c] = l * s + r * k;
+        for (int i = 0; i < kBatch; ++i) {
+            if (out[i] == nullptr) continue;
+            if (!turns) {
+                x[i].template store<STREAM != 0>(out[i]);
+                continue;
             }
-            x.set(u);
-            y.set(v);
-            x.store(out + p0 * kBytes);
-            y.store(out + (pairs + p0) * kBytes);
-        } else {
-            const int p0 = piece * (V / 2);
-            Piece<BF16, V> x;
-            x.load(in + 2 * p0 * kBytes);
-            float u[V];
+            const float *s = sines + token[i] * pairs + piece * (HALF ? V : V / 2), *k = cosines + (s - sines);
+            if constexpr (HALF) {
+                float u[V], v[V];
 #pragma unroll
-            for (int c = 0; c < V / 2; ++c) {
-                const float s = sines[token * pairs + p0 + c], k = cosines[token * pairs + p0 + c], l = x.get(2 * c), r = x.get(2 * c + 1);
-                u[2 * c] = l * k - r * s;
-                u[2 * c + 1] = l * s + r * k;
+                for (int c = 0; c < V; ++c) {
+                    const float l = x[i].get(c), r = y[i].get(c);
+                    u[c] = l * k[c] - r * s[c];
+                    v[c] = l * s[c] + r * k[c];
+                }
+                x[i].set(u);
+                y[i].set(v);
+                x[i].template store<STREAM != 0>(out[i]);
+                y[i].template store<STREAM != 0>(out[i] + half);
+            } else {
+                float u[V];
+#pragma unroll
+                for (int c = 0; c < V / 2; ++c) {
+                    const float l = x[i].get(2 * c), r = x[i].get(2 * c + 1);
+                    u[2 * c] = l * k[c] - r * s[c];
+                    u[2 * c + 1] = l * s[c] + r * k[c];
+                }
+                x[i].set(u);
+                x[i].template store<STREAM != 0>(out[i]);
             }
-            x.set(u);
-            x.store(out + 2 * p0 * kBytes);
         }
     }
 }
@@ -122,9 +154,14 @@ void launch(Rope a, hipStream_t s) {
     const bool tail = (a.q.heads > 0 && a.q.in != a.q.out) || (a.k.heads > 0 && a.k.in != a.k.out);
     a.pieces = HALF ? a.rot / 2 / V : a.rot / V;
     a.row_pieces = a.pieces + (tail ? (a.dim - a.rot) / V : 0);
-    // Tokens per block: so that each thread has a sine and cosine to compute, where there are blocks enough.
+    // Tokens per block: so that each thread has a sine and cosine to compute, where there are blocks enough (16384 x 40 heads of 128: four).
+    // What is more than the caches hold does better without them, as the norm's arrays and the cache's.
     a.tokens = std::max(1, std::min(kThreads / (a.rot / 2), a.n / 2048));
-    hipLaunchKernelGGL((rope_kernel<BF16, HALF, V>), dim3((a.n + a.tokens - 1) / a.tokens), dim3(kThreads), 0, s, a);
+    const dim3 blocks((a.n + a.tokens - 1) / a.tokens);
+    const size_t moved = 2 * static_cast<size_t>(a.n) * a.heads * a.dim * (BF16 ? 2 : 4);
+    if (moved <= size_t(100) << 20) hipLaunchKernelGGL((rope_kernel<BF16, HALF, V, 0>), blocks, dim3(kThreads), 0, s, a);
+    else if (moved <= size_t(300) << 20) hipLaunchKernelGGL((rope_kernel<BF16, HALF, V, 1>), blocks, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((rope_kernel<BF16, HALF, V, 2>), blocks, dim3(kThreads), 0, s, a);
 }
 
 template <bool BF16>
