@@ -89,6 +89,29 @@ def test_long_prompts(dtype, cache, dim):
     run_and_check(cfg, arrays, q, table, news, "prefix", heads_only=[3], scores=Scores("table", 8, back=127, ahead=127))
 
 
+@pytest.mark.parametrize("kind,window", [("causal", 0), ("prefix", 0), ("documents", 0), ("odd", 0), ("causal", 300)])
+@pytest.mark.parametrize("dim,cache", [(128, "bf16"), (112, "e4m3")])
+def test_prompts_long_enough_for_blocks_in_turns(dim, cache, kind, window):
+    """Rows enough for blocks of eight waves, of which one half weighs while the other multiplies; all that a mask hides stays without effect."""
+    news = [(100, 2100)]
+    cfg, arrays, table = make(news, 16, dim, 64, "bf16", cache, seed=48)
+    q = queries(49, 2100, 64, dim, "bf16")
+    a = run_and_check(cfg, arrays, q, table, news, kind, window, heads_only=[0, 37, 63])
+    b = run_and_check(cfg, arrays, q, table, news, kind, window, heads_only=[5])
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), "two runs differ"
+    bad = [None if t is None else t.clone() for t in arrays]
+    first, end, given = spans(kind, news)
+    at, token = np.arange(100, 2200), 1500
+    lo = np.maximum(np.maximum(first, 0), at - window + 1) if window else np.maximum(first, 0)
+    sees = torch.from_numpy((lo <= token) & (token < end)).cuda()
+    place = (table[0, token // 64].long(), 9, token % 64, 5)
+    bad[1].view(torch.uint8).view(*bad[1].shape, -1)[place] = 0x7f if cache == "e4m3" else torch.tensor([0x80, 0x7f], dtype=torch.uint8, device="cuda")
+    got, got_lse = run_prompt(cfg, bad, q, table, [2200], [0, 2100], first if given[0] else None, end if given[1] else None, window)
+    assert torch.equal(got_lse, a[1]) and torch.equal(got[~sees], a[0][~sees]) and not torch.isfinite(got[sees][:, 36:40, 5].float()).any()
+    got[:, 36:40, 5] = a[0][:, 36:40, 5]
+    assert torch.equal(got, a[0])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_many_sequences(dtype):
     """4096 of them, 0 to 5 new tokens each; and one among many that is longer than all others together."""
