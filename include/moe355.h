@@ -432,7 +432,7 @@ int moe_attn_decode_scored(const moe_kv_cfg* cfg, const moe_attn_cfg* attn, cons
 typedef struct moe_prompt_cfg {
     int32_t tokens;       /* rows of q and out; 0 <= tokens < 2^22 */
     int32_t B;            /* sequences, 0 to 4096 */
-    int32_t q_heads;      /* a multiple of heads, at most 1024; tokens * q_heads < 2^31 */
+    int32_t q_heads;      /* a multiple of heads, at most 1024; tokens * q_heads < 2^30 */
     int32_t table_pages;  /* pages a row of table has room for; table_pages * page_size <= 2^24 */
     int32_t window;       /* 0: no bound */
     float scale;          /* 0: 1 / sqrt(head_dim) */

@@ -95,8 +95,8 @@ int check_prompt(const moe_kv_cfg* kv, const moe_prompt_cfg* c) {
     if (c->tokens < 0 || c->tokens >= 1 << 22) return fail(MOE_ERR_INVALID_ARG, "tokens must be in [0, 2^22) (got %d)", c->tokens);
     const moe_attn_cfg as{c->B, c->q_heads, c->table_pages, c->window, c->scale};
     if (int rc = check_attn(kv, &as)) return rc;
-    if (static_cast<long long>(c->tokens) * c->q_heads >= 1LL << 31)
-        return fail(MOE_ERR_INVALID_ARG, "tokens * q_heads must be below 2^31 (got %d, q_heads = %d)", c->tokens, c->q_heads);
+    if (static_cast<long long>(c->tokens) * c->q_heads >= 1LL << 30)
+        return fail(MOE_ERR_INVALID_ARG, "tokens * q_heads must be below 2^30 (got %d, q_heads = %d)", c->tokens, c->q_heads);
     return MOE_OK;
 }
 

@@ -178,7 +178,11 @@ struct Wave {
     bf16x8 q16[kWide ? 1 : kPartsQ][kWide ? 1 : NT][kWide ? 1 : L::kPieces][kWide ? 1 : kSteps];
     f32x4 o[NT][L::kHalves][L::kOwn];                                               // O^T: dim 128 half + own (4 g + r) + j, head l % 16
     float m[NT], l[NT];                                                             // maximum (the same in all quarters), weight of the own tokens
-    HeadScores<false> of_head[SCORED ? NT : 0];
+    struct Head {
+        float slope, last;                                                          // times log2 e: what a step of distance costs; the bias of far keys
+        int row;                                                                    // of its biases
+    };
+    Head of_head[SCORED ? NT : 0];
 
     uint32_t k_at[L::kPieces], k_in[L::kPieces], k_out[L::kPieces], v_at[L::kHalves];    // of this lane: bytes from a run's first row, bytes in the LDS
     int row_bytes;
@@ -254,7 +258,10 @@ struct Wave {
     __device__ void load_scores(const Attn& a, int head0, int n_heads, int lane) {
         if constexpr (SCORED)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) of_head[t].load(a.scores, head0 + min(16 * t + lane % 16, n_heads - 1));
+            for (int t = 0; t < NT; ++t) {
+                const int h = head0 + min(16 * t + lane % 16, n_heads - 1), row = bias_row(a.scores, h);
+                of_head[t] = Head{a.scores.slopes != nullptr ? a.scores.slopes[h] * kLog2E : 0.f, a.scores.bias != nullptr ? bias_at(a.scores, row, a.scores.back) : 0.f, row};
+            }
     }
 
     // Once the queries are wanted.
@@ -315,7 +322,7 @@ struct Wave {
 
     // Sums of products of the t-th sixteen query heads to their logits; d: the distance of the first.
     __device__ void score(f32x4 (&s)[2], const f32x4 (&ks)[2], const Attn& a, int t, int d, bool near) const {
-        const HeadScores<false>& own = of_head[t];
+        const Head& own = of_head[t];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             float x[4];
@@ -329,7 +336,7 @@ struct Wave {
             for (int c = 0; c < 4; ++c) {
                 const int at = d - 16 * r - c;
                 if (a.scores.slopes != nullptr) x[c] = fmaf(-own.slope, fabsf(static_cast<float>(at)), x[c]);
-                if (a.scores.bias != nullptr) x[c] += own.bias(a.scores, at, near);
+                if (a.scores.bias != nullptr) x[c] += near ? bias_at(a.scores, own.row, at) : own.last;
                 s[r][c] = x[c];
             }
         }
@@ -403,7 +410,7 @@ struct Wave {
                 }
         }
 
-        const bool near = SCORED && a.scores.near(span.end - t0 - 32, span.end - 1 - t0);
+        const bool near = SCORED && span.end - t0 - 32 < a.scores.back;            // some key has a bias other than the last
         float p[NT][2][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {

@@ -88,9 +88,10 @@ __device__ inline float halves_sum(float v) {
 // How a block of WAVES waves holds its tiles.
 template <bool F32, int CACHE, int DIM, int WAVES>
 struct Shape {
-    // Rows of over 128 columns in 16 bits have two waves, which both make their weights and have half of the columns of O each: with all of them a wave has no room
-    // in 256 registers, and with 512 the compiler moves O from accumulation registers and back in every tile (8192 tokens in documents, 16 heads: 328 us).
-    static constexpr int kShare = !F32 && DIM > 128 ? 2 : 1;
+    // Rows of over 128 columns have two waves, which both make their weights and have half of the columns of O each: with all of them a 16-bit wave has no room
+    // in 256 registers, and with 512 the compiler moves O from accumulation registers and back in every tile (8192 tokens in documents, 16 heads: 328 us, so 280);
+    // in fp32 it would keep some in scratch memory.
+    static constexpr int kShare = DIM > 128 ? 2 : 1;
     static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES / kShare;
     static constexpr int kKeys = DIM > 128 ? 32 : 64;                               // keys of a tile
     static constexpr int kBlocks = kKeys / 32, kColumns = DIM / 32 / kShare;        // S in 32 keys, O of a wave in 32 columns
@@ -123,10 +124,11 @@ __device__ inline bool find(const Prompt& a, int index, int rows, Item& it) {
     int before = 0;
     for (int b0 = a.B - 1; b0 >= 0; b0 -= 64) {
         const int b = b0 - lane;
-        int s = 0, n = 0;
+        int s = 0, n = 0, len = 0;
         if (b >= 0) {
             s = min(max(a.starts[b], 0), a.tokens);
             n = max(min(max(a.starts[b + 1], 0), a.tokens) - s, 0);
+            len = a.lens[b];
         }
         const int tiles = (n * a.group + rows - 1) / rows;                          // (tokens * group < 2^31)
         int upto = tiles;
@@ -146,7 +148,7 @@ __device__ inline bool find(const Prompt& a, int index, int rows, Item& it) {
             it.rows = uniform(min(tile * each + each, all));
             it.token0 = uniform(__shfl(s, at));
             it.b = uniform(it.b);
-            it.len = uniform(min(max(a.lens[it.b], 0), a.table_pages << a.page_bits));
+            it.len = uniform(min(max(__shfl(len, at), 0), a.table_pages << a.page_bits));
             it.place0 = it.len - uniform(new_tokens);
             return true;
         }
@@ -409,7 +411,7 @@ struct Block {
     float m, l;
     int lo, hi, place, own;                                                         // of this lane's row; own: its query head in the group
     int wave_first, wave_end, whole_from, whole_to;                                 // keys that some of the wave's rows see; that all of them see
-    HeadScores<true> hs;
+    HeadScores hs;
 
     // A lane's part of S^T of a tile, as logits.
     __device__ void products(int buf, f32x16 (&s)[H::kBlocks]) const {
@@ -419,7 +421,8 @@ struct Block {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
 #pragma unroll
-        for (int st = 0; st < kSteps; ++st)
+        for (int st = 0; st < kSteps; ++st) {
+            if (F32 && 8 * st >= a.dim) break;
 #pragma unroll
             for (int kb = 0; kb < H::kBlocks; ++kb) {
                 const u32x4 u = *reinterpret_cast<const u32x4*>(lds.k[0] + (at ^ (32 * st)) + 32 * kb * H::kRowBytes);
@@ -430,6 +433,7 @@ struct Block {
                     s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u), __builtin_bit_cast(bf16x8, q[st]), s[kb], 0, 0, 0);
                 }
             }
+        }
     }
     // The key of sum i of a lane in block kb, from the tile's first.
     __device__ static constexpr int key_of(int kb, int i) { return 32 * kb + 8 * (i / 4) + i % 4; }
@@ -442,21 +446,6 @@ struct Block {
         const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(from)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(from + 8 * H::kRowBytes));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     }
-    // In fp32 a lane reads the kColumns (up to four) neighbouring columns of one key that are its row of as many blocks.
-    static constexpr int kNear = H::kColumns < 4 ? H::kColumns : 4;
-    __device__ void beside(const char* v, int key, int group4, float (&x)[kNear]) const {
-        const char* at = v + (key + 4 * (lane / 32)) * H::kRowBytes + 512 * group4 + 4 * kNear * (lane % 32);
-        if constexpr (kNear == 4) {
-            const f32x4 u = *reinterpret_cast<const f32x4*>(at);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) x[c] = u[c];
-        } else {
-            const f32x2 u = *reinterpret_cast<const f32x2*>(at);
-            x[0] = u[0];
-            x[1] = u[1];
-        }
-    }
-
     struct Weights {
         uint32_t u[H::kBlocks][16 / H::kPerWord];
         __device__ void set(int kb, int i, float x, float y) { u[kb][i / H::kPerWord] = F32 ? __float_as_uint(x) : to_bf16x2(x, y); }
@@ -563,18 +552,16 @@ struct Block {
     // O^T += V^T P^T.
     __device__ void values(int buf, const Weights& w) {
         if constexpr (F32) {
-            const char* const v = lds.v[buf];
+            const float* const v = reinterpret_cast<const float*>(lds.v[buf]) + 4 * (lane / 32) * DIM + 32 * wave_column + lane % 32;
 #pragma unroll
-            for (int kb = 0; kb < H::kBlocks; ++kb)
+            for (int c = 0; c < H::kColumns; ++c) {
+                if (32 * (wave_column + c) >= a.dim) break;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
+                for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
-                    for (int g = 0; g < H::kColumns / kNear; ++g) {
-                        float x[kNear];
-                        beside(v, key_of(kb, i), g, x);
-#pragma unroll
-                        for (int c = 0; c < kNear; ++c) o[kNear * g + c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[c], __uint_as_float(w.u[kb][i / H::kPerWord]), o[kNear * g + c], 0, 0, 0);
-                    }
+                    for (int i = 0; i < 16; ++i)
+                        o[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[key_of(kb, i) * DIM + 32 * c], __uint_as_float(w.u[kb][i / H::kPerWord]), o[c], 0, 0, 0);
+            }
         } else {
             const int at = v_at(buf);
 #pragma unroll
@@ -585,8 +572,7 @@ struct Block {
     }
     // The column of sum i of a lane in block c.
     __device__ int column_of(int c, int i) const {
-        const int row = 8 * (i / 4) + 4 * (lane / 32) + i % 4;
-        return F32 ? 128 * (c / kNear) + kNear * row + c % kNear : 32 * (wave_column + c) + row;
+        return 32 * (wave_column + c) + 8 * (i / 4) + 4 * (lane / 32) + i % 4;
     }
     // Values that are not finite under rows of which some may not see them: a weight of zero times such a value would be no number, so the product has zeros in
     // their places, and the rows that see them get them here.
@@ -641,7 +627,7 @@ struct Block {
         if (a.scores.bias != nullptr) {
             const bool behind = __all(d0 - (H::kKeys - 1) >= a.scores.back), ahead = __all(d0 <= -a.scores.ahead);
             if (behind || ahead) {
-                shift += behind ? hs.last : hs.first[0];
+                shift += behind ? hs.last : hs.first;
             } else if (tabled) {
                 const float* const from = &lds.bias[own * width + d0 + a.scores.ahead + kPad - (H::kKeys - 1)];
 #pragma unroll
@@ -650,10 +636,11 @@ struct Block {
                     for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(s[kb][i], mult, from[H::kKeys - 1 - key_of(kb, i)]);
                 mult = 1.f;
             } else {
+                const int row = bias_row(a.scores, head * a.group + own);
 #pragma unroll
                 for (int kb = 0; kb < H::kBlocks; ++kb)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(s[kb][i], mult, hs.bias(a.scores, d0 - key_of(kb, i), true));
+                    for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(s[kb][i], mult, bias_at(a.scores, row, d0 - key_of(kb, i)));
                 mult = 1.f;
             }
         }
@@ -730,37 +717,26 @@ struct Block {
             else if (a.lse != nullptr) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
         }
         if (part && first >= end) return;                                           // (a part without keys: its maximum says so)
-        if constexpr (F32) {
 #pragma unroll
-            for (int g = 0; g < H::kColumns / kNear; ++g)
+        for (int c = 0; c < H::kColumns; ++c)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int d = 128 * g + kNear * (8 * (i / 4) + 4 * h + i % 4);
-                    float* to = part ? part_o + d : static_cast<float*>(a.out) + at * a.dim + d;
-                    if (d >= a.dim) continue;
-                    if constexpr (kNear == 4) *reinterpret_cast<f32x4*>(to) = f32x4{o[4 * g][i], o[4 * g + 1][i], o[4 * g + 2][i], o[4 * g + 3][i]} * inv;
-                    else *reinterpret_cast<f32x2*>(to) = f32x2{o[0][i] * inv, o[1][i] * inv};
-                }
-        } else {
-#pragma unroll
-            for (int c = 0; c < H::kColumns; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const int d = 32 * (wave_column + c) + 8 * (i / 4) + 4 * h;
-                    if (d >= a.dim) continue;
-                    if (part) *reinterpret_cast<f32x4*>(part_o + d) = f32x4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]};
-                    else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at * a.dim + d) =
-                        u32x2{to_bf16x2(o[c][i] * inv, o[c][i + 1] * inv), to_bf16x2(o[c][i + 2] * inv, o[c][i + 3] * inv)};
-                }
-        }
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * (wave_column + c) + 8 * (i / 4) + 4 * h;
+                if (d >= a.dim) continue;
+                const f32x4 v = f32x4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]} * inv;
+                if (part) *reinterpret_cast<f32x4*>(part_o + d) = v;
+                else if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at * a.dim + d) = v;
+                else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at * a.dim + d) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+            }
     }
 
     // A wave weighs tile t (the exponentials), then multiplies: the keys of tile t + 1, the values of tile t.  With two waves of the block on a SIMD (kTurns) the
-    // second half of them, `late`, does it the other way round between two barriers, so that one of the two has the matrix pipes while the other weighs:
-    //     the first half   | weigh 0    multiply 0 | weigh 1    multiply 1 | ..
-    //     the second half  |            weigh 0    | multiply 0 weigh 1    | ..
-    // K of t + 1 and t and V of t and t - 1 are read between these barriers, and K of t + 2 and V of t + 1 put into LDS, by all waves while they weigh t: three
-    // buffers.  Where all waves are late, K of t and V of t - 1 are read, and K of t + 1 and V of t put there: two.
+    // second half of them, `late`, has its barrier between the two and the first half before them, so that one of the two has the matrix pipes while the other weighs:
+    //     the first half           | weigh 0    multiply 0 | weigh 1    multiply 1 | ..
+    //     the second half  weigh 0 | multiply 0 weigh 1    | multiply 1 weigh 2    | ..
+    // Between the barriers of t and t + 1, K of t + 1 and V of t are read; the first half, weighing t, puts its share of K of t + 2 and V of t + 1 into LDS, the second
+    // half, weighing t + 1, its share of K of t + 3 and V of t + 2: three buffers, and what is read after a barrier was put before it.
+    // Where all waves are late, K of t + 2 and V of t + 1 are put there: two buffers, K a tile less ahead.
     __device__ void run() {
         lay_out();
         begin();
@@ -898,12 +874,12 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(Prompt a) {
 
 template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED>
 int launch(const Prompt& a, const Plan& p, hipStream_t s) {
-    static_assert(Shape<F32, CACHE, DIM, WAVES>::kRows == (WAVES == 8 && DIM <= 128 ? 256 : 128), "as plan_of says");
+    static_assert(Shape<F32, CACHE, DIM, WAVES>::kRows == (F32 && DIM > 128 ? 64 : WAVES == 8 && DIM <= 128 ? 256 : 128), "as plan_of says");
     const dim3 blocks(static_cast<unsigned>(p.tiles * a.heads * a.parts));
     if (a.parts == 1) {
         hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED, false>), blocks, dim3(64 * WAVES), 0, s, a);
         MOE_LAUNCH_CHECK("prompt_kernel");
-    } else if constexpr (Shape<F32, CACHE, DIM, WAVES>::kRows == 128) {
+    } else if constexpr (WAVES == 4 || DIM > 128) {
         hipLaunchKernelGGL((prompt_kernel<F32, CACHE, DIM, WAVES, SCORED, true>), blocks, dim3(64 * WAVES), 0, s, a);
         MOE_LAUNCH_CHECK("prompt_kernel");
         const long rows = static_cast<long>(a.tokens) * a.heads * a.group, each = 1024 / DIM;
@@ -971,7 +947,7 @@ Plan plan_of(const moe_kv_cfg& kv, const moe_prompt_cfg& c, bool scored) {
     const int group = c.q_heads / kv.heads, sequences = std::max(1, std::min(c.B, c.tokens));
     const long rows = static_cast<long>(c.tokens) * group, each = (rows + sequences - 1) / sequences;      // of a key head; of a sequence, in the mean
     p.dim = kv.head_dim <= 64 ? 64 : kv.head_dim <= 128 ? 128 : 256;
-    p.rows = 128;
+    p.rows = f32 && p.dim > 128 ? 64 : 128;
     p.tiles = rows / p.rows + sequences;
     // Few items: their keys are cut, down to 256 of them.
     const long items = p.tiles * kv.heads, slots = (f32 || p.dim > 128 ? 1 : 2) * kUnits;
@@ -1025,7 +1001,7 @@ int launch_attn_prompt(const moe_kv_cfg& kv, const moe_prompt_cfg& c, const Scor
     a.pages = kv.pages;
     a.page_bits = __builtin_ctz(kv.page_size);
     a.table_pages = c.table_pages;
-    a.window = c.window;
+    a.window = std::min(c.window, 1 << 26);                                        // (of no effect from 2^24 + 2^22 on)
     a.scale = (c.scale > 0.f ? c.scale : 1.f / sqrtf(static_cast<float>(kv.head_dim))) * kLog2E;
     a.scores = ScoreArgs(scores, kv.dtype);
     const Plan p = plan_of(kv, c, scores.any());

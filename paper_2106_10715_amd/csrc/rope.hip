@@ -157,7 +157,7 @@ void launch(Rope a, hipStream_t s) {
     // Tokens per block: so that each thread has a sine and cosine to compute, where there are blocks enough (16384 x 40 heads of 128: four).
     // What is more than the caches hold does better without them, as the norm's arrays and the cache's.
     a.tokens = std::max(1, std::min(kThreads / (a.rot / 2), a.n / 2048));
-    const dim3 blocks((a.n + a.tokens - 1) / a.tokens);
+    const dim3 blocks(static_cast<unsigned>((static_cast<long>(a.n) + a.tokens - 1) / a.tokens));
     const size_t moved = 2 * static_cast<size_t>(a.n) * a.heads * a.dim * (BF16 ? 2 : 4);
     if (moved <= size_t(100) << 20) hipLaunchKernelGGL((rope_kernel<BF16, HALF, V, 0>), blocks, dim3(kThreads), 0, s, a);
     else if (moved <= size_t(300) << 20) hipLaunchKernelGGL((rope_kernel<BF16, HALF, V, 1>), blocks, dim3(kThreads), 0, s, a);

@@ -17,8 +17,6 @@ struct ScoreArgs {
     // dtype: of the activations.  With 16 bits and caps up to 64 a score may be off by 4 units of 2^-24 of the cap, 1.6e-5, as its weight may be by 2^-9.
     ScoreArgs(const Scores& s, int dtype)
         : cap(s.cap * kLog2E), over_cap(s.cap > 0.f ? 1.f / (s.cap * kLog2E) : 0.f), fine(dtype == MOE_F32 || s.cap > 64.f), back(s.back), ahead(s.ahead), slopes(s.slopes), bias(s.bias) {}
-    // Whether keys at distances from `least` to `most` can have biases other than the last or the first one's alone.
-    __device__ bool near(int least, int most) const { return bias != nullptr && least < back && most > -ahead; }
 };
 
 // tanh to a few units in the last place.  Below 0.75 an odd polynomial, fitted to tanh(z) / z in z^2 for the least relative error (1.5e-9; the sum of
@@ -63,22 +61,18 @@ __device__ inline void cap_scores(const ScoreArgs& a, float (&x)[N]) {
             if (!(fabsf(z[i]) < kSmall)) x[i] = a.cap * large_tanh(z[i]);
 }
 
-// What scores have of their query's head.  AHEAD: there may be keys behind the query.
-template <bool AHEAD>
+// Where the bias of a head for distance 0 lies, and the bias for distance d from there, times log2 e.
+__device__ inline int bias_row(const ScoreArgs& a, int head) { return head * (a.back + a.ahead + 1) + a.ahead; }
+__device__ inline float bias_at(const ScoreArgs& a, int row, int d) { return a.bias[row + min(max(d, -a.ahead), a.back)] * kLog2E; }
+
+// What scores have of their query's head.
 struct HeadScores {
-    float slope, last, first[AHEAD ? 1 : 0];    // times log2 e: what a step of distance costs; the bias of far keys, before the query and after it
-    int row;                                    // of the biases
+    float slope, last, first;               // times log2 e: what a step of distance costs; the bias of far keys, before the query and after it
     __device__ void load(const ScoreArgs& a, int head) {
-        row = head * (a.back + a.ahead + 1) + a.ahead;
+        const int row = bias_row(a, head);
         slope = a.slopes != nullptr ? a.slopes[head] * kLog2E : 0.f;
-        last = a.bias != nullptr ? a.bias[row + a.back] * kLog2E : 0.f;
-        if constexpr (AHEAD) first[0] = a.bias != nullptr ? a.bias[row - a.ahead] * kLog2E : 0.f;
-    }
-    // The bias of the key at distance d; not `near`: all of the wave's keys are far, on the same side.
-    __device__ float bias(const ScoreArgs& a, int d, bool near) const {
-        if (near) return a.bias[row + min(max(d, -a.ahead), a.back)] * kLog2E;
-        if constexpr (AHEAD) return d >= a.back ? last : first[0];
-        return last;
+        last = a.bias != nullptr ? bias_at(a, row, a.back) : 0.f;
+        first = a.bias != nullptr ? bias_at(a, row, -a.ahead) : 0.f;
     }
 };
 

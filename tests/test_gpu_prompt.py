@@ -158,6 +158,9 @@ def test_lengths_and_pages_outside_of_their_ranges():
     got, got_lse = run_prompt(cfg, arrays, q, table, [5, 48], [0, 20, 40])
     assert (got[:15] == 0).all() and (got_lse[:15] == -math.inf).all()
     assert torch.isfinite(got.float()).all() and torch.isfinite(got_lse[15:]).all()
+    every = dict(end=np.full(40, 48))                                          # a window of all there is hides nothing, of tokens before the first either
+    a, b = (run_prompt(cfg, arrays, q, table, [5, 48], [0, 20, 40], window=w, **every) for w in (0, 2 ** 31 - 1))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and torch.isfinite(a[1]).all()
     table[0, 1] = cfg.pages + 5                                                # the nearest page that exists
     far = torch.clone(table)
     far[0, 1] = cfg.pages - 1
