@@ -581,13 +581,19 @@ struct Block {
 #pragma unroll 1
         for (int key = 0; key < H::kKeys; ++key) {
             const bool counts = static_cast<uint32_t>(t0 + key - lo) < static_cast<uint32_t>(hi - lo);
+            int from = column_of(0, 0);
+            asm("" : "+v"(from));                                                   // (so that no places of this rare case are kept in registers)
 #pragma unroll
             for (int c = 0; c < H::kColumns; ++c)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int column = column_of(c, i);
-                    if (counts && lds.up[buf][key][column / kEach] >> column % kEach & 1) o[c][i] += INFINITY;
-                    if (counts && lds.down[buf][key][column / kEach] >> column % kEach & 1) o[c][i] -= INFINITY;
+                for (int i = 0; i < 16; i += 4) {
+                    const int column = from + 32 * c + 2 * i;
+                    const uint32_t up = lds.up[buf][key][column / kEach] >> column % kEach, down = lds.down[buf][key][column / kEach] >> column % kEach;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (counts && up >> e & 1) o[c][i + e] += INFINITY;
+                        if (counts && down >> e & 1) o[c][i + e] -= INFINITY;
+                    }
                 }
         }
     }
@@ -829,7 +835,7 @@ struct Block {
 constexpr int waves_of(bool f32) { return f32 ? 1 : 2; }
 
 template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED, bool PARTS>
-__global__ __launch_bounds__(64 * WAVES, waves_of(F32)) void prompt_kernel(Prompt a) {
+__global__ __launch_bounds__(64 * WAVES, SCORED && !F32 && DIM == 64 ? 3 : waves_of(F32)) void prompt_kernel(Prompt a) {
     using B = Block<F32, CACHE, DIM, WAVES, SCORED, PARTS>;
     __shared__ typename B::Lds lds;
     Item it;
