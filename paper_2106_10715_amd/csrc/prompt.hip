@@ -835,7 +835,7 @@ struct Block {
 constexpr int waves_of(bool f32) { return f32 ? 1 : 2; }
 
 template <bool F32, int CACHE, int DIM, int WAVES, bool SCORED, bool PARTS>
-__global__ __launch_bounds__(64 * WAVES, SCORED && !F32 && DIM == 64 ? 3 : waves_of(F32)) void prompt_kernel(Prompt a) {
+__global__ __launch_bounds__(64 * WAVES, waves_of(F32)) void prompt_kernel(Prompt a) {
     using B = Block<F32, CACHE, DIM, WAVES, SCORED, PARTS>;
     __shared__ typename B::Lds lds;
     Item it;
