@@ -940,12 +940,15 @@ namespace {
 
 constexpr int kUnits = 256;         // compute units, also of the plan that sizes the workspace
 // Blocks of four waves, two to a compute unit, or of eight that take turns, one to a unit: these read keys half as often, but all rows of a block wait for each other,
-// and where weights cost more than products nothing is gained by turns.  us with four / eight (ragged lengths where there are several):
-//   32 over 8 of 128, bf16:   1 x 2048 59.3 / 62.7, 4 x 2048 79.9 / 83.3, 40 x 500 90.4 / 102, but 1 x 4096 168.7 / 147.6, 8 x 4096 487 / 469, 1 x 8192 567 / 526;
-//                             with a cap 1 x 8192 778 / 800;  e4m3 cache: 64 x 500 (64 over 8) 307 / 348, but 1 x 16384 2457 / 2344
-//   64 heads of 64, bf16:     8 x 2048 176 / 208 (with a table of biases 246 / 278), 1 x 4096 177 / 188
-bool in_turns(const moe_kv_cfg& kv, const Plan& p, long rows, long each, bool scored) {
-    return kv.dtype == MOE_BF16 && p.dim == 128 && !scored && p.parts == 1 && each >= 8192 && rows * kv.heads >= 1 << 17;
+// so that short stretches are better off with four, and where weights cost more than products nothing is gained by turns.  us with four / eight, in 16 bits if no type
+// is named (ragged lengths where there are several; + n: after n cached tokens, of which the host knows what the table has room for):
+//   32 heads over 8 of 128:  1 x 2048 60.8 / 60.0, 40 x 500 84 / 93, 16 x 1500 158.5 / 158.2, but 8 x 2048 139 / 136, 1 x 4096 152 / 141, 1 x 8192 549 / 506, 4 x 2048 + 8000 1157 / 1060;
+//                            e4m3 1 x 16384 2335 / 2173, 8 x 4096 504 / 492;  with a cap 1 x 8192 778 / 800;  4 x 4096 in a window of 256 173 / 186, of 512 225 / 225, of 1024 325 / 314
+//   64 heads over 8 of 128:  32 x 1024 349 / 355, 40 x 640 227 / 245, but 1 x 2048 86 / 81, 8 x 512 + 8000 1063 / 974;  e4m3 64 x 500 297 / 333, but 4 x 1024 + 4000 668 / 620
+//   32 heads of 128:         1 x 2048 56.8 / 58.3, e4m3 8 x 1500 117 / 126, but 1 x 4096 153 / 144, e4m3 2 x 4096 177 / 161
+//   64 heads of 64:          8 x 2048 176 / 208 (with a table of biases 246 / 278), 1 x 4096 177 / 188
+bool in_turns(const moe_kv_cfg& kv, const Plan& p, long each, int group, long keys, bool scored) {
+    return kv.dtype == MOE_BF16 && p.dim == 128 && !scored && p.parts == 1 && each >= 2048 && keys >= 1536 && each >= (keys >= 4096 ? 512L : 1536L) * group;
 }
 Plan plan_of(const moe_kv_cfg& kv, const moe_prompt_cfg& c, bool scored) {
     Plan p;
@@ -960,7 +963,7 @@ Plan plan_of(const moe_kv_cfg& kv, const moe_prompt_cfg& c, bool scored) {
     const long room = static_cast<long>(c.table_pages) * kv.page_size, keys = c.window > 0 ? std::min(room, c.window + each / group + 64) : room;
     p.parts = static_cast<int>(std::max(1L, std::min({slots / std::max(items, 1L), keys / 256, 16L})));
     p.waves = !f32 && p.dim > 128 ? 8 : 4;
-    if (in_turns(kv, p, rows, each, scored)) {
+    if (in_turns(kv, p, each, group, keys, scored)) {
         p.waves = 8;
         p.rows = 256;
         p.tiles = rows / p.rows + sequences;

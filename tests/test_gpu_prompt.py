@@ -112,6 +112,18 @@ def test_prompts_long_enough_for_blocks_in_turns(dim, cache, kind, window):
     assert torch.equal(got, a[0])
 
 
+@pytest.mark.parametrize("kind,window", [("causal", 0), ("both", 0), ("causal", 1700)])
+@pytest.mark.parametrize("dim,cache", [(128, "e4m3"), (80, "bf16")])
+def test_prompts_after_long_ones_in_turns(dim, cache, kind, window):
+    """Rows of several sequences, one without new tokens, after thousands of cached ones, in blocks of eight waves."""
+    news = [(5000, 1200), (4100, 0), (4097, 700), (7001, 333)]
+    cfg, arrays, table = make(news, 16, dim, 64, "bf16", cache, seed=58)
+    q = queries(59, 2233, 64, dim, "bf16")
+    a = run_and_check(cfg, arrays, q, table, news, kind, window, heads_only=[1, 62])
+    b = run_and_check(cfg, arrays, q, table, news, kind, window, heads_only=[30])
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), "two runs differ"
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_many_sequences(dtype):
     """4096 of them, 0 to 5 new tokens each; and one among many that is longer than all others together."""
