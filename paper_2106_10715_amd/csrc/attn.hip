@@ -320,8 +320,17 @@ struct Wave {
         }
     }
 
+    // Biases of a lane's tokens, the first of distance d; near: some of the tile's have another than the last.
+    __device__ void biases(f32x4 (&bias)[NT][2], const Attn& a, int d, bool near) const {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) bias[t][r][c] = near ? bias_at(a.scores, of_head[t].row, d - 16 * r - c) : of_head[t].last;
+    }
     // Sums of products of the t-th sixteen query heads to their logits; d: the distance of the first.
-    __device__ void score(f32x4 (&s)[2], const f32x4 (&ks)[2], const Attn& a, int t, int d, bool near) const {
+    __device__ void score(f32x4 (&s)[2], const f32x4 (&ks)[2], const Attn& a, int t, int d, const f32x4 (&bias)[2]) const {
         const Head& own = of_head[t];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -336,7 +345,7 @@ struct Wave {
             for (int c = 0; c < 4; ++c) {
                 const int at = d - 16 * r - c;
                 if (a.scores.slopes != nullptr) x[c] = fmaf(-own.slope, fabsf(static_cast<float>(at)), x[c]);
-                if (a.scores.bias != nullptr) x[c] += near ? bias_at(a.scores, own.row, at) : own.last;
+                if (a.scores.bias != nullptr) x[c] += bias[r][c];
                 s[r][c] = x[c];
             }
         }
@@ -349,6 +358,14 @@ struct Wave {
         auto &k = x.k;
         auto &v = x.v;
         auto &ks = x.ks, &vs = x.vs;
+        const int distance = span.end - 1 - (t0 + 4 * g);      // of the lane's first token
+        const bool near = SCORED && span.end - t0 - 32 < a.scores.back;
+        // Requested before K is waited for (64 x 8192 tokens, 64 heads over 8 of 128 in e4m3, with a cap and so no biases: 107 us, requested where they are used 111); fp32 rows of over 128
+        // columns leave no registers for that.
+        constexpr bool kEarly = SCORED && !(F32 && DIM > 128);
+        f32x4 bias[SCORED ? NT : 1][2];
+        if constexpr (kEarly)
+            if (a.scores.bias != nullptr) biases(bias, a, distance, near);
         if constexpr (L::kStaged) {
             // A wave's LDS operations are done in their order: between what its lanes write and read only the compiler has to keep it.
             auto in_order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); };
@@ -410,12 +427,13 @@ struct Wave {
                 }
         }
 
-        const bool near = SCORED && span.end - t0 - 32 < a.scores.back;            // some key has a bias other than the last
         float p[NT][2][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             float top = -INFINITY;
-            if constexpr (SCORED) score(s[t], ks, a, t, span.end - 1 - (t0 + 4 * g), near);
+            if constexpr (SCORED && !kEarly)
+                if (a.scores.bias != nullptr) biases(bias, a, distance, near);
+            if constexpr (SCORED) score(s[t], ks, a, t, distance, bias[t]);
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
