@@ -98,6 +98,21 @@ class Decoder:
             M.moe_rope(self.rope, positions, self.freqs, q, q, k, k)
         return q, k, v
 
+    @staticmethod
+    def in_calls(counts, most):
+        """The counts of calls of prompt() that take these tokens in, up to `most` in each: the layer's buffers grow with a call's tokens."""
+        left, call = list(counts), [0] * len(counts)
+        for b in range(len(left)):
+            while left[b] > 0:
+                take = min(left[b], most - sum(call))
+                call[b] += take
+                left[b] -= take
+                if sum(call) == most:
+                    yield call
+                    call = [0] * len(counts)
+        if any(call):
+            yield call
+
     def prompt(self, x, counts, first=None, end=None):
         """counts[b] further tokens of each sequence, their embeddings x [sum, d] -> their hidden states [sum, d].  first, end: what moe_attn_prompt's mask takes."""
         n = x.shape[0]
@@ -162,12 +177,14 @@ def main():
     D = Decoder(a.batch, a.layers, a.heads * a.dim, a.heads, a.kv_heads, a.dim, a.d_ff, a.experts, a.top, a.length + a.steps + 8, a.page, a.cache, a.qkv,
                 rotary={} if a.rotary else None, cap=a.cap, slopes=a.slopes)
     if a.prompt:
-        x = torch.empty((a.batch * a.length, a.heads * a.dim), dtype=torch.bfloat16, device="cuda").normal_()
+        calls = list(D.in_calls([a.length] * a.batch, min(1 << 16, (2 ** 31 - 1) // (D.moe.k * max(D.moe.d, D.moe.f)))))
+        x = torch.empty((max(map(sum, calls)), a.heads * a.dim), dtype=torch.bfloat16, device="cuda").normal_()
         for _ in range(2):                                   # (the first is the warm-up)
             D.lens.zero_()
             torch.cuda.synchronize()
             t = time.perf_counter()
-            D.prompt(x, [a.length] * a.batch)
+            for counts in calls:
+                D.prompt(x[:sum(counts)], counts)
             torch.cuda.synchronize()
             s = time.perf_counter() - t
         print(f"{a.batch} prompts of {a.length} tokens, {a.layers} layers: {s * 1e3:.3f} ms, {a.batch * a.length / s:.0f} tokens/s")

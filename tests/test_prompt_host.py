@@ -1,7 +1,9 @@
 """Host-only checks of rotary positions, prompts and scores by distance: the oracle against its definitions, frequencies, workspace sizes, and every refusal of
 the library and of the binding, before anything is launched."""
 import ctypes as C
+import importlib.util
 import math
+import os
 
 import numpy as np
 import pytest
@@ -227,3 +229,20 @@ def test_what_the_marshalling_refuses_is_never_passed_on(monkeypatch):
         with pytest.raises(M.MoeError, match="not as its description says"):
             call()
     assert called == []
+
+
+@pytest.mark.parametrize("counts", [[0], [1], [7], [8], [0, 3, 9, 0, 17, 1], [2000] * 40, [70000, 1, 65536]])
+@pytest.mark.parametrize("most", [1, 8, 1 << 16])
+def test_the_example_takes_prompts_in_calls(counts, most):
+    spec = importlib.util.spec_from_file_location("decode_example", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    if sum(counts) // most > 100:
+        most = 8000
+    calls = [list(c) for c in example.Decoder.in_calls(counts, most)]
+    assert [sum(c) for c in zip(*calls)] == (counts if sum(counts) else [])
+    assert all(sum(c) == most for c in calls[:-1]) and all(0 < sum(c) <= most for c in calls)
+    done = [0] * len(counts)
+    for c in calls:                                                # a sequence begins when the one before it is done
+        done = [a + b for a, b in zip(done, c)]
+        assert sum(0 < a < b for a, b in zip(done, counts)) <= 1
