@@ -9,6 +9,11 @@
 // A lane's sums S are, of its row, the keys 8 a + 4 (lane / 32) + b, a and b from 0 to 3: what the second product wants of P^T in that lane, if V^T is given with
 // its keys in the same order.  So P never leaves its lane.  In 16 bits V^T comes from LDS by reads that turn blocks of 4 keys x 16 columns; in fp32 an operand
 // is one number and the order is that of the reads.
+//
+// Bound by the matrix pipes where sequences are long and scores plain (16384 tokens, 32 heads over 8 of 128: 1.95 ms, 1.13 PFLOP/s; the pipes are busy for 64 % of a
+// clock that the card lowers to 1.6 GHz meanwhile), else by what weights cost: at 64 columns a weight has as many cycles of exponential, bias and rounding as of products
+// (8 x 2048 tokens, 64 heads of 64, a table of biases: 240 us, vector instructions issue in 55 % of the cycles, products in 22 %; 8192 tokens in documents, 16 heads of
+// 256, capped: 212 us, 57 % and 27 %).  Few rows over a long cache are bound by making their tiles (16 x 33 tokens after 8000 in e4m3: 148 us, 1.8 TB/s).
 #include <math.h>
 
 #include <algorithm>
@@ -89,7 +94,7 @@ __device__ inline float halves_sum(float v) {
 template <bool F32, int CACHE, int DIM, int WAVES>
 struct Shape {
     // Rows of over 128 columns have two waves, which both make their weights and have half of the columns of O each: with all of them a 16-bit wave has no room
-    // in 256 registers, and with 512 the compiler moves O from accumulation registers and back in every tile (8192 tokens in documents, 16 heads: 328 us, so 280);
+    // in 256 registers, and with 512 the compiler moves O from accumulation registers and back in every tile (8192 tokens in documents, 16 heads, capped: 328 us, so, otherwise as it was then, 280);
     // in fp32 it would keep some in scratch memory.
     static constexpr int kShare = DIM > 128 ? 2 : 1;
     static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES / kShare;

@@ -21,7 +21,7 @@ struct ScoreArgs {
 
 // tanh to a few units in the last place.  Below 0.75 an odd polynomial, fitted to tanh(z) / z in z^2 for the least relative error (1.5e-9; the sum of
 // its rounding 1e-7): 1 - 2 / (e^2z + 1) alone, which is taken above it, is off by units of 1 and not of z.  Where that is enough it is taken for all
-// (attention of 8192 tokens in documents, 16 heads of 256, cap 30: 280 us with both, 226 with it alone).
+// (attention of 8192 tokens in documents, 16 heads of 256: 255 us with both, 205 with it alone, 167 without a cap).
 __device__ inline float small_tanh(float z) {
     const float u = z * z;
     float p = 0.00172035361f;
