@@ -432,7 +432,7 @@ int moe_attn_decode_scored(const moe_kv_cfg* cfg, const moe_attn_cfg* attn, cons
 typedef struct moe_prompt_cfg {
     int32_t tokens;       /* rows of q and out; 0 <= tokens < 2^22 */
     int32_t B;            /* sequences, 0 to 4096 */
-    int32_t q_heads;      /* a multiple of heads, at most 1024; tokens * q_heads < 2^30 */
+    int32_t q_heads;      /* a multiple of heads, at most 1024; tokens * q_heads < 2^29 */
     int32_t table_pages;  /* pages a row of table has room for; table_pages * page_size <= 2^24 */
     int32_t window;       /* 0: no bound */
     float scale;          /* 0: 1 / sqrt(head_dim) */
@@ -475,7 +475,7 @@ typedef struct moe_rope_cfg {
 int moe_rope_frequencies(const moe_rope_cfg* cfg, double* freqs);
 
 /*
- *   positions [n] int32, freqs [rot_dim / 2] fp64: device.
+ *   positions [n] int32, freqs [rot_dim / 2] fp64: device.  0 <= n <= 2^24.
  *   q, q_out [n, q_heads, head_dim], k, k_out [n, k_heads, head_dim]: device, dtype, token i's at element i * stride (strides as moe_kv_write's).
  *   q_out may be q itself (with the same stride), not overlap it otherwise; q and q_out may both be NULL (no queries); the same for k.
  */

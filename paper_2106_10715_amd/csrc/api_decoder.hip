@@ -95,8 +95,8 @@ int check_prompt(const moe_kv_cfg* kv, const moe_prompt_cfg* c) {
     if (c->tokens < 0 || c->tokens >= 1 << 22) return fail(MOE_ERR_INVALID_ARG, "tokens must be in [0, 2^22) (got %d)", c->tokens);
     const moe_attn_cfg as{c->B, c->q_heads, c->table_pages, c->window, c->scale};
     if (int rc = check_attn(kv, &as)) return rc;
-    if (static_cast<long long>(c->tokens) * c->q_heads >= 1LL << 30)
-        return fail(MOE_ERR_INVALID_ARG, "tokens * q_heads must be below 2^30 (got %d, q_heads = %d)", c->tokens, c->q_heads);
+    if (static_cast<long long>(c->tokens) * c->q_heads >= 1LL << 29)                     // (a launch has fewer than 2^32 threads)
+        return fail(MOE_ERR_INVALID_ARG, "tokens * q_heads must be below 2^29 (got %d, q_heads = %d)", c->tokens, c->q_heads);
     return MOE_OK;
 }
 
@@ -262,7 +262,7 @@ int moe_rope_frequencies(const moe_rope_cfg* cfg, double* freqs) {
 int moe_rope(const moe_rope_cfg* cfg, int32_t n, const int32_t* positions, const double* freqs, const void* q, int64_t q_stride, void* q_out,
              int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, void* stream) {
     if (int rc = check_rope(cfg)) return rc;
-    if (int rc = check_n(n)) return rc;
+    if (n < 0 || n > 1 << 24) return fail(MOE_ERR_INVALID_ARG, "n must be in [0, 2^24] (got %d)", n);     // (a launch has fewer than 2^32 threads)
     REQUIRE(freqs, "freqs");
     if (n == 0) return MOE_OK;
     if (int rc = check_turned(q, q_stride, q_out, q_out_stride, cfg->q_heads, cfg->head_dim, "q", "q_out")) return rc;

@@ -101,6 +101,7 @@ def test_rope_refuses_null_misaligned_and_contradicting_arguments():
     good = [al, al, al, 128, al + 512, 128, al, 64, al + 512, 64, None]                     # positions, freqs, q, stride, q_out, stride, k, ...
     refused(L.moe_rope(None, 1, *good), "cfg is NULL")
     refused(L.moe_rope(R, -1, *good), "n must be")
+    refused(L.moe_rope(R, (1 << 24) + 1, *good), "n must be")
     for at, frag in ((0, "positions is NULL"), (1, "freqs is NULL"), (2, "q is NULL"), (4, "q_out is NULL"), (6, "k is NULL"), (8, "k_out is NULL")):
         args = list(good)
         args[at] = None
@@ -119,7 +120,7 @@ def test_rope_refuses_null_misaligned_and_contradicting_arguments():
 
 
 @pytest.mark.parametrize("kw,frag", [
-    (dict(tokens=-1), "tokens must"), (dict(tokens=1 << 22), "tokens must"), (dict(tokens=1 << 21, q_heads=512), "tokens * q_heads"), (dict(B=-1), "B must"), (dict(B=4097), "B must"), (dict(q_heads=3), "q_heads"),
+    (dict(tokens=-1), "tokens must"), (dict(tokens=1 << 22), "tokens must"), (dict(tokens=1 << 21, q_heads=256), "tokens * q_heads"), (dict(B=-1), "B must"), (dict(B=4097), "B must"), (dict(q_heads=3), "q_heads"),
     (dict(q_heads=1026), "q_heads"), (dict(table_pages=0), "table_pages"), (dict(table_pages=(1 << 20) + 1), "table_pages"), (dict(window=-1), "window"),
     (dict(scale=-1.0), "scale"), (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale")])
 def test_prompts_refuse_a_bad_description(kw, frag):
