@@ -435,7 +435,7 @@ typedef struct moe_prompt_cfg {
     int32_t q_heads;      /* a multiple of heads, at most 1024; tokens * q_heads < 2^29 */
     int32_t table_pages;  /* pages a row of table has room for; table_pages * page_size <= 2^24 */
     int32_t window;       /* 0: no bound */
-    float scale;          /* 0: 1 / sqrt(head_dim) */
+    float scale;          /* 0: 1 / sqrt(head_dim); with slopes at least 2^-64, and these below 2^100 times the scale */
 } moe_prompt_cfg;
 int moe_attn_prompt_workspace_bytes(const moe_kv_cfg* cfg, const moe_prompt_cfg* prompt, size_t* bytes);
 int moe_attn_prompt(const moe_kv_cfg* cfg, const moe_prompt_cfg* prompt, const moe_scores_cfg* scores, const void* q, int64_t q_stride,

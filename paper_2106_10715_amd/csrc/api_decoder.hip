@@ -225,6 +225,8 @@ int moe_attn_prompt(const moe_kv_cfg* cfg, const moe_prompt_cfg* prompt, const m
     if (int rc = check_prompt(cfg, prompt)) return rc;
     Scores sc;
     if (int rc = scores_of(scores, slopes, bias, &sc)) return rc;
+    // (slopes are added to the sums of products, divided by the scale)
+    if (slopes != nullptr && prompt->scale > 0.f && prompt->scale < 0x1p-64f) return fail(MOE_ERR_INVALID_ARG, "with slopes scale must be 0 or at least 2^-64");
     if (int rc = check_pages(*cfg, k_pages, v_pages, k_scales, v_scales)) return rc;
     if (prompt->B == 0 || prompt->tokens == 0) return MOE_OK;
     if (int rc = check_rows(q, q_stride, static_cast<int64_t>(prompt->q_heads) * cfg->head_dim, "q")) return rc;

@@ -154,6 +154,8 @@ def test_attention_refuses_null_misaligned_and_contradicting_arguments():
         assert rc == code, L.moe_last_error()
         assert frag.encode() in L.moe_last_error()
 
+    tiny = M.PromptCfg.make(3, 1, 4, 4, scale=2.0 ** -65)
+    refused(L.moe_attn_prompt(K, C.addressof(tiny), None, al, 256, al, al, None, None, al, al, al, None, None, al, None, al, al, al, None), "scale must be 0 or at least 2^-64")
     # q, stride, pages, scales, table, lens, starts, first, end, slopes, bias, out, lse, ws, stream
     good = [al, 256, al, al, None, None, al, al, al, None, None, al, al, al, al, al, None]
     for at, frag in ((0, "q is NULL"), (2, "k_pages is NULL"), (3, "v_pages is NULL"), (6, "table is NULL"), (7, "lens is NULL"), (8, "starts is NULL"), (13, "out is NULL"),
