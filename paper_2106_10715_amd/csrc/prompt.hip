@@ -38,7 +38,7 @@ struct Prompt {
     float* lse;
     int tokens, B, heads, group, dim, pages, page_bits, table_pages, window;
     int parts;                              // stretches that an item's keys are cut into, each a block's
-    float *part_o, *part_ml;                // [parts][tokens * query heads][dim], [parts][tokens * query heads][2]: unscaled sums; their maximum and weight
+    float *part_o, *part_ml;                // [parts][tokens * query heads][dim], [parts][tokens * query heads][2]: unscaled sums; their maximum and weight (-1: no sums)
     float scale;                            // times log2 e
     ScoreArgs scores;
 };
@@ -724,10 +724,10 @@ struct Block {
         const float inv = part ? 1.f : l == 0.f ? 0.f : 1.f / l;
         float* const part_o = a.part_o + (static_cast<long>(it.part) * a.tokens * a.heads * a.group + at) * a.dim;
         if (h == 0 && wave_column == 0) {
-            if (part) *reinterpret_cast<f32x2*>(a.part_ml + (static_cast<long>(it.part) * a.tokens * a.heads * a.group + at) * 2) = f32x2{m, l};
+            if (part) *reinterpret_cast<f32x2*>(a.part_ml + (static_cast<long>(it.part) * a.tokens * a.heads * a.group + at) * 2) = f32x2{m, first < end ? l : -1.f};
             else if (a.lse != nullptr) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
         }
-        if (part && first >= end) return;                                           // (a part without keys: its maximum says so)
+        if (part && first >= end) return;                                           // (a part without keys: its weight says so)
 #pragma unroll
         for (int c = 0; c < H::kColumns; ++c)
 #pragma unroll
@@ -857,7 +857,8 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(F32)) void prompt_kernel(Promp
     block.run();
 }
 
-// Joins an item's parts: the row of a token and query head by DIM / 4 neighbouring threads, in the order of the keys.
+// Joins an item's parts: the row of a token and query head by DIM / 4 neighbouring threads, in the order of the keys.  All that have keys count, those whose
+// maximum is -infinity too: logits of -infinity add zeros, logits that are all NaN leave the maximum as it was and make the row NaN, as in a call that is not cut.
 template <bool F32, int DIM>
 __global__ __launch_bounds__(256) void prompt_join_kernel(Prompt a) {
     const long rows = static_cast<long>(a.tokens) * a.heads * a.group, row = static_cast<long>(blockIdx.x) * (1024 / DIM) + threadIdx.x / (DIM / 4);
@@ -867,11 +868,12 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(Prompt a) {
     if (token < a.starts[0] || token >= a.starts[a.B]) return;
     float top = -INFINITY, weight = 0.f;
     for (int i = 0; i < a.parts; ++i) top = fmaxf(top, a.part_ml[(i * rows + row) * 2]);
+    const float ref = top == -INFINITY ? 0.f : top;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < a.parts; ++i) {
         const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + (i * rows + row) * 2);
-        if (ml[0] == -INFINITY) continue;                                           // nothing counts there, and nothing may have been written
-        const float f = __builtin_amdgcn_exp2f(ml[0] - top);
+        if (ml[1] < 0.f) continue;                                                  // no sums were written there
+        const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
         const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + (i * rows + row) * a.dim + d);
         weight = fmaf(ml[1], f, weight);
 #pragma unroll
