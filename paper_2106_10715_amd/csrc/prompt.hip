@@ -108,10 +108,9 @@ struct Shape {
     static constexpr int kRowBytes = DIM * kWidth, kPieces = kRowBytes / 16;        // a row in LDS
     static constexpr int kFrom = DIM * kCached / 16;                                // 16-byte pieces of a row as it comes
     static constexpr int kTo = kWidth / kCached;                                    // of which each makes so many in LDS
-    static constexpr int kLoads = (kKeys * kFrom + kThreads - 1) / kThreads;
+    static constexpr int kLoads = kKeys * kFrom / kThreads;
     static constexpr int kTile = kKeys * kRowBytes;                                 // bytes
-    static constexpr bool kSpare = kKeys * kFrom < kThreads;                        // some of the waves have nothing to load
-    static_assert(64 / kFrom <= 16 && (kSpare || kLoads * kThreads == kKeys * kFrom), "a load of a wave lies in one run of 16 tokens");
+    static_assert(64 / kFrom <= 16 && kLoads * kThreads == kKeys * kFrom, "a load of a wave lies in one run of 16 tokens, and all waves load as much");
     static constexpr int kStep = kThreads / kFrom;                                  // rows from a lane's load to its next
     static_assert(kThreads % kFrom == 0 && kStep % 4 == 0, "a lane's loads have the same piece of their rows");
 };
@@ -237,7 +236,6 @@ struct Block {
         at_piece = i % H::kFrom;                                                    // (the same in all loads)
         from = 16 * at_piece < row_bytes ? (lane / H::kFrom) * row_bytes + 16 * at_piece : 0x7fffff00;
     }
-    __device__ bool idle() const { return H::kSpare && 64 * wave >= H::kKeys * H::kFrom; }
     // Where the rows of the wave's loads begin, looked up for kAsked tiles at once: lane kSlots s + j has load j of the s-th of them.
     static constexpr int kSlots = H::kLoads <= 1 ? 1 : H::kLoads <= 2 ? 2 : H::kLoads <= 4 ? 4 : 8, kAsked = 64 / kSlots;
     int ids, own_id;                                                                // the pages of the next kAsked tiles; kScaled, the first wave: of key `lane` of the next tile
@@ -279,7 +277,6 @@ struct Block {
         const int row_bytes = a.dim * H::kCached;
 #pragma unroll
         for (int j = 0; j < H::kLoads; ++j) {
-            if (idle()) break;
             const int t = t0 + (j * H::kThreads + 64 * wave) / H::kFrom + lane / H::kFrom;
             const bool there = WHOLE || (t >= first && t < end);
             const auto rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pages) + both(r.lo[j], r.hi[j]), 0, 16 * row_bytes, 0x00027000);
@@ -333,7 +330,6 @@ struct Block {
         char* const k = lds.k[to];
 #pragma unroll
         for (int j = 0; j < H::kLoads; ++j) {
-            if (idle()) break;
             u32x4 out[H::kTo];
             widen(k_raw[j], F32 ? k_scale[F32 ? j : 0] : 1.f, out);
 #pragma unroll
@@ -351,7 +347,6 @@ struct Block {
             uint32_t most = 0;                                                      // (bf16: of two, side by side)
 #pragma unroll
             for (int j = 0; j < H::kLoads; ++j) {
-                if (idle()) break;
                 u32x4 out[H::kTo];
                 widen(v_raw[j], F32 ? v_scale[F32 ? j : 0] : 1.f, out);
 #pragma unroll
@@ -379,7 +374,6 @@ struct Block {
         char* const v = lds.v[to];
 #pragma unroll
         for (int j = 0; j < H::kLoads; ++j) {
-            if (idle()) break;
             u32x4 out[H::kTo];
             widen(v_raw[j], F32 ? v_scale[F32 ? j : 0] : 1.f, out);
             if constexpr (ODD)
