@@ -422,8 +422,9 @@ int moe_attn_decode_scored(const moe_kv_cfg* cfg, const moe_attn_cfg* attn, cons
  * which is a causal mask as it stands, a prefix with end = max(p + 1, prefix), documents with first = where the token's document begins,
  * and a mask that lets all tokens see each other with end = lens[b].
  * Scores as moe_scores_cfg says (NULL: plain ones; slopes and bias may be NULL).  What a row's mask hides is of no effect, whatever it is, NaN
- * among it.  A row that sees no key, or whose l_t are all -infinity: out 0 and lse -infinity.  Sums and statistics are fp32; with dtype MOE_BF16 the weights exp(l_t) enter
- * the sum of values rounded to bf16, after they have entered that of the weights.
+ * among it.  A row that sees no key, or whose l_t are all -infinity: out 0 and lse -infinity; one with NaN among the l_t it sees: NaN in both.
+ * Sums and statistics are fp32; with dtype MOE_BF16 the weights exp(l_t) enter the sum of values rounded to bf16, after they have entered that
+ * of the weights.
  *   q: device, dtype, token i's [q_heads, head_dim] at element i * q_stride.  out [tokens, q_heads, head_dim]: dtype.  lse [tokens, q_heads]: fp32,
  *   may be NULL.  Rows before starts[0] and from starts[B] on are left as they were.
  *   table, lens: as moe_attn_decode's.  starts [B + 1] int32: device, ascending, taken as within [0, tokens].  first, end [tokens] int32: device.

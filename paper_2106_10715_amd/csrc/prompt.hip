@@ -11,9 +11,10 @@
 // is one number and the order is that of the reads.
 //
 // Bound by the matrix pipes where sequences are long and scores plain (16384 tokens, 32 heads over 8 of 128: 1.95 ms, 1.13 PFLOP/s; the pipes are busy for 64 % of a
-// clock that the card lowers to 1.6 GHz meanwhile), else by what weights cost: at 64 columns a weight has as many cycles of exponential, bias and rounding as of products
-// (8 x 2048 tokens, 64 heads of 64, a table of biases: 240 us, vector instructions issue in 55 % of the cycles, products in 22 %; 8192 tokens in documents, 16 heads of
-// 256, capped: 212 us, 57 % and 27 %).  Few rows over a long cache are bound by making their tiles (16 x 33 tokens after 8000 in e4m3: 148 us, 1.8 TB/s).
+// clock that the card lowers to 1.6 GHz meanwhile).  Elsewhere no pipe is full: at 64 columns a weight has as many cycles of exponential, bias and rounding as of products
+// (8 x 2048 tokens, 64 heads of 64, a table of biases: 240 us, vector instructions issue in 55 % of the cycles, products in 22 %; of its cycles a wave issues in 45 %, waits
+// for its turn in 21 % and for data or a barrier in 34 %; 8192 tokens in documents, 16 heads of 256, capped: 212 us, 57 % and 27 %; 42, 27 and 31 %).  Few rows over a long
+// cache are bound by making their tiles (16 x 33 tokens after 8000 in e4m3: 148 us, 1.8 TB/s).
 #include <math.h>
 
 #include <algorithm>
@@ -445,6 +446,8 @@ struct Block {
         const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(from)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(from + 8 * H::kRowBytes));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     }
+    // In 16 bits a weight is one bf16 value, rounded after it has entered the sum of weights: off by 2^-8 of itself at most, as an output by its own rounding.  Outputs
+    // are off by 0.0018 to 0.0024 of their norm, with fp32 weights by 0.0017; a second part would be half again as many products (heads of over 128: a third).
     struct Weights {
         uint32_t u[H::kBlocks][16 / H::kPerWord];
         __device__ void set(int kb, int i, float x, float y) { u[kb][i / H::kPerWord] = F32 ? __float_as_uint(x) : to_bf16x2(x, y); }
